@@ -389,6 +389,63 @@ dcut_status dcut_model_verify(dcut_ctx* ctx, const dcut_model* model, long long 
                               void* hidden_out, void* stream);
 
 /*
+ * Requests that share the beginning of their context (a system prompt, a common document).  The batch's requests fall
+ * into n_groups contiguous groups; group g = requests cu_group[g] .. cu_group[g+1]-1 (ascending, cu_group[0] = 0,
+ * cu_group[n_groups] = B; a group may be empty).  Positions j < prefix_lens[g] of all its requests are stored once, in
+ * the pages prefix_table[g][j / 16], slot j % 16 (the last of them may be partly used); position j >= prefix_lens[g] of
+ * request i is stored in block_table[i][(j - prefix_lens[g]) / 16], slot (j - prefix_lens[g]) % 16.  A prefix length of
+ * 0 leaves the requests of a group on their own.  All arrays DEVICE int32; the struct itself is HOST memory.
+ */
+typedef struct {
+    int n_groups;
+    const int* cu_group;       /* [n_groups + 1] */
+    const int* prefix_lens;    /* [n_groups] */
+    const int* prefix_table;   /* [n_groups, prefix_table_stride] */
+    int prefix_table_stride;
+} dcut_prefix_groups;
+
+/*
+ * Appends the new tokens' keys and values to the paged cache, rotating queries and keys on the way (the step between
+ * the QKV projection and the attention, Appendix C; dcut_layer_forward holds it for its own buffers, this call for any
+ * target's).  For packed token r with request i = tok_req[r] at position p = tok_pos[r] (as dcut_select writes them):
+ *   n = x / sqrt(mean(x^2) + rms_eps) * gain      per query / key head, where the gain is given
+ *   y_a = n_a cos - n_b sin,  y_b = n_b cos + n_a sin,  angle = p * inv_freq[e],  e = 0 .. rotary_dim/2 - 1
+ *   (a, b) = (e, e + rotary_dim/2), or (2e, 2e+1) with interleaved != 0; elements from rotary_dim on are not rotated
+ *   q_out[r, h, :] = y for query heads; the cache slot of position p gets y of every key head and v unchanged.
+ * The angle is formed in 64 bits, the rest in 32; one rounding to bf16 at the end.
+ * DEVICE in: q, k, v bf16, element (r, h, e) at r * token_stride + h * head_stride + e (strides in elements, multiples
+ *   of 8, >= 0; bases 16-byte aligned; T_cap rows readable), so the slices of a fused QKV row serve as they are; q may be
+ *   NULL (with q_out NULL: keys and values only, e.g. a prompt's prefix).  inv_freq fp64 [rotary_dim/2]; rotary_dim a
+ *   multiple of 16 in 0 .. head_dim (0: nothing rotates, inv_freq may be NULL); gains bf16 [head_dim], 16-byte
+ *   aligned, or NULL.  tok_req, tok_pos int32 [T_cap]; cu_q int32 [B+1] (rows from cu_q[B] on are not touched), or NULL:
+ *   all T_cap rows.  A row with tok_req < 0 is padding and is skipped.  groups: NULL, or the shared prefixes: the slot
+ *   then counts from the end of the request's prefix (prefix_table is not read here and may be NULL).
+ * DEVICE out: q_out bf16 [T_cap, n_q_heads, head_dim] dense, 16-byte aligned (may be q itself when q is dense; must not
+ *   overlap it in any other way); k_cache, v_cache (layout above, 128-byte aligned).
+ * T_cap is not bound by dcut_limits: prompts of any length can be appended.  The new tokens' (request, position) pairs
+ * must differ from one another.  A token whose request is >= B or whose position has no column in the block table sets
+ * device status 8, one whose page is outside [0, num_pages) status 2; nothing is written for such a token.
+ */
+typedef struct {
+    const void *q, *k, *v;
+    long long q_token_stride, q_head_stride;
+    long long k_token_stride, k_head_stride;
+    long long v_token_stride, v_head_stride;
+} dcut_qkv;
+typedef struct {
+    const double* inv_freq;
+    int rotary_dim;
+    int interleaved;
+    const void* q_gain;
+    const void* k_gain;
+    float rms_eps;
+} dcut_rope;
+dcut_status dcut_rope_append(dcut_ctx* ctx, const dcut_qkv* qkv, const dcut_rope* rope, void* q_out, void* k_cache,
+                             void* v_cache, long long num_pages, const int* block_table, int block_table_stride,
+                             const dcut_prefix_groups* groups, const int* cu_q, int B, const int* tok_req,
+                             const int* tok_pos, int T_cap, void* stream);
+
+/*
  * dcut_accept without any allocation.  (The paper has no counterpart: this entry point exists for
  * the way the library gets embedded, not for the method.)
  *
@@ -475,7 +532,8 @@ dcut_status dcut_verify_step_host(dcut_ctx* ctx, const dcut_host_step* step, voi
  * read instead), 3 = the attention work list did not fit the scratch, 4 = a bounded wait in the GEMM
  * kernel gave up, 5 = dcut_commit ran out of room, 6 = dcut_model_verify met a token id outside [0, vocab),
  * 7 = an acceptance call met a cu_q that is not a packing of B requests of 1 .. gamma + 1 rows inside T_cap
- * (rows at or past T_cap were left out: nothing outside the caller's T_cap rows is read or written). */
+ * (rows at or past T_cap were left out: nothing outside the caller's T_cap rows is read or written), 8 =
+ * dcut_rope_append met a token whose request or position has no place in the block table (it was left out). */
 dcut_status dcut_poll_device_status(dcut_ctx* ctx, int* code, void* stream);
 
 #ifdef __cplusplus

@@ -32,7 +32,8 @@ EXPORTS = ["dcut_create", "dcut_destroy", "dcut_last_error", "dcut_set_cost_dens
            "dcut_select_causal", "dcut_accept_rs", "dcut_commit", "dcut_model_verify", "dcut_poll_device_status",
            "dcut_enable_plan_in_select", "dcut_cost_grid_create", "dcut_cost_grid_destroy", "dcut_cost_grid_budget",
            "dcut_cost_grid_record", "dcut_cost_grid_get", "dcut_cost_grid_nearest", "dcut_cost_grid_buckets",
-           "dcut_set_cost_from_grid", "dcut_layer_attn_part", "dcut_layer_mlp_part", "dcut_residual_add"]
+           "dcut_set_cost_from_grid", "dcut_layer_attn_part", "dcut_layer_mlp_part", "dcut_residual_add",
+           "dcut_rope_append"]
 
 
 class Limits(C.Structure):
@@ -107,6 +108,22 @@ _lib.dcut_layer_mlp_part.argtypes = [_vp, C.POINTER(LayerWeights), _vp, _vp, _vp
 _lib.dcut_residual_add.argtypes = [_vp, _vp, _vp, _vp, _i, _vp, _i, _i, _vp]
 
 
+class PrefixGroupsRec(C.Structure):
+    _fields_ = [("n_groups", _i), ("cu_group", _vp), ("prefix_lens", _vp), ("prefix_table", _vp), ("prefix_table_stride", _i)]
+
+
+class Qkv(C.Structure):
+    _fields_ = [(n, _vp) for n in ("q", "k", "v")] + [(f"{t}_{s}_stride", _ll) for t in "qkv" for s in ("token", "head")]
+
+
+class Rope(C.Structure):
+    _fields_ = [("inv_freq", _vp), ("rotary_dim", _i), ("interleaved", _i), ("q_gain", _vp), ("k_gain", _vp), ("rms_eps", _f)]
+
+
+_lib.dcut_rope_append.argtypes = [_vp, C.POINTER(Qkv), C.POINTER(Rope), _vp, _vp, _vp, _ll, _vp, _i, C.POINTER(PrefixGroupsRec),
+                                  _vp, _i, _vp, _vp, _i, _vp]
+
+
 @dataclass
 class PreparedModel:
     rec: "Model"
@@ -128,6 +145,32 @@ def _ptr(t: Optional[torch.Tensor], dtype=None) -> Optional[int]:
     if dtype is not None:
         assert t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
     return t.data_ptr()
+
+
+def _heads(t: Optional[torch.Tensor], n_heads: int, head_dim: int):
+    """(pointer, token stride, head stride) of a bf16 [tokens, heads, head_dim] view whose last dimension is dense."""
+    if t is None:
+        return None, 0, 0
+    assert t.is_cuda and t.dtype == torch.bfloat16, "expected a CUDA bf16 tensor"
+    assert t.dim() == 3 and t.shape[1] == n_heads and t.shape[2] == head_dim and t.stride(2) == 1, \
+        f"expected [tokens, {n_heads}, {head_dim}] with dense heads, got {tuple(t.shape)} with strides {t.stride()}"
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def rope_inv_freq(theta: float, rotary_dim: int, device="cuda") -> torch.Tensor:
+    """The plain frequency table of rope_append: theta^(-2e / rotary_dim), fp64 (scaled variants: change its entries)."""
+    return torch.tensor([float(theta) ** (-2.0 * e / rotary_dim) for e in range(rotary_dim // 2)], dtype=torch.float64, device=device)
+
+
+class PrefixGroups:
+    """dcut_prefix_groups: contiguous groups of requests that share a prefix (CUDA int32 tensors, kept alive here)."""
+
+    def __init__(self, cu_group: torch.Tensor, prefix_lens: torch.Tensor, prefix_table: torch.Tensor):
+        G = prefix_lens.shape[0]
+        assert cu_group.shape == (G + 1,) and prefix_table.shape[0] == G
+        self.keep = (cu_group, prefix_lens, prefix_table)
+        self.rec = PrefixGroupsRec(G, _ptr(cu_group, torch.int32), _ptr(prefix_lens, torch.int32), _ptr(prefix_table, torch.int32),
+                                   prefix_table.shape[1])
 
 
 def _stream() -> int:
@@ -458,6 +501,29 @@ class Context:
         self._check(_lib.dcut_residual_add(self._h, _ptr(a, torch.bfloat16), _ptr(b, torch.bfloat16), _ptr(out, torch.bfloat16),
                                            a.shape[1], _ptr(cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, _stream()))
         return out
+
+    def rope_append(self, q, k, v, inv_freq, k_cache, v_cache, block_table, tok_req, tok_pos, T_cap: int, cu_q=None,
+                    interleaved: bool = False, q_gain=None, k_gain=None, rms_eps: float = 1e-6,
+                    groups: Optional[PrefixGroups] = None, q_out=None):
+        """dcut_rope_append: rotates q and k ([tokens, heads, head_dim] views of any token and head stride) and appends k, v
+        to the paged cache.  `inv_freq`: fp64 [rotary_dim / 2] (None: no rotation).  Returns q_out [T_cap, Hq, Dh]."""
+        l = self.limits
+        for t in (q, k, v):
+            assert t is None or t.shape[0] >= T_cap, "q, k and v need T_cap rows"
+        assert tok_req.shape[0] >= T_cap and tok_pos.shape[0] >= T_cap
+        if q is not None and q_out is None:
+            q_out = torch.empty((T_cap, l.n_q_heads, l.head_dim), dtype=torch.bfloat16, device=k.device)
+        (qp, qt, qh), (kp, kt, kh), (vp, vt, vh) = (_heads(t, n, l.head_dim) for t, n in
+                                                    ((q, l.n_q_heads), (k, l.n_kv_heads), (v, l.n_kv_heads)))
+        x = Qkv(qp, kp, vp, qt, qh, kt, kh, vt, vh)
+        r = Rope(_ptr(inv_freq, torch.float64), 2 * inv_freq.shape[0] if inv_freq is not None else 0, int(interleaved),
+                 _ptr(q_gain, torch.bfloat16), _ptr(k_gain, torch.bfloat16), rms_eps)
+        self._check(_lib.dcut_rope_append(self._h, C.byref(x), C.byref(r), _ptr(q_out, torch.bfloat16), _ptr(k_cache, torch.bfloat16),
+                                          _ptr(v_cache, torch.bfloat16), k_cache.shape[0], _ptr(block_table, torch.int32),
+                                          block_table.shape[1], C.byref(groups.rec) if groups is not None else None,
+                                          _ptr(cu_q, torch.int32), block_table.shape[0], _ptr(tok_req, torch.int32),
+                                          _ptr(tok_pos, torch.int32), T_cap, _stream()))
+        return q_out
 
     def make_model(self, layers: list, embed, g_final, w_lm, k_caches: list, v_caches: list, rms_eps: float = 1e-6,
                    rope_theta: float = 1e6) -> "PreparedModel":

@@ -533,6 +533,57 @@ dcut_status dcut_residual_add(dcut_ctx* c, const void* a, const void* b, void* o
     return dcut_launch_residual_add(c, a, b, out, width, cu_q, B, T_cap, static_cast<cudaStream_t>(stream));
 }
 
+// The arguments are checked before the device, so that every refusal is the same with or without a GPU.
+dcut_status dcut_rope_append(dcut_ctx* c, const dcut_qkv* x, const dcut_rope* r, void* q_out, void* k_cache, void* v_cache,
+                             long long num_pages, const int* block_table, int block_table_stride,
+                             const dcut_prefix_groups* groups, const int* cu_q, int B, const int* tok_req,
+                             const int* tok_pos, int T_cap, void* stream) {
+    if (!c) return DCUT_EINVAL;
+    const dcut_limits& l = c->lim;
+    if (l.n_q_heads <= 0) return dcut_fail(c, DCUT_EINVAL, "context was created without attention shapes");
+    if (!x || !r || !x->k || !x->v || !k_cache || !v_cache || !block_table || !tok_req || !tok_pos || (x->q != nullptr) != (q_out != nullptr))
+        return dcut_fail(c, DCUT_EINVAL, "null pointer argument (q and q_out go together)");
+    if (B < 1 || T_cap < 1 || num_pages < 1) return dcut_fail(c, DCUT_EINVAL, "need B, T_cap, num_pages >= 1");
+    if (B > l.max_B) return dcut_fail(c, DCUT_ECAPACITY, "B = %d exceeds the limit %d", B, l.max_B);
+    if (block_table_stride < 1 || block_table_stride > l.max_pages_per_req)
+        return dcut_fail(c, DCUT_ECAPACITY, "block_table_stride = %d outside [1, %d]", block_table_stride, l.max_pages_per_req);
+    if (r->rotary_dim < 0 || r->rotary_dim > l.head_dim || r->rotary_dim % 16 || (r->rotary_dim > 0 && !r->inv_freq))
+        return dcut_fail(c, DCUT_EINVAL, "rotary_dim = %d must be a multiple of 16 up to head_dim, with inv_freq", r->rotary_dim);
+    if ((r->q_gain || r->k_gain) && (!(r->rms_eps >= 0.0f) || isinf(r->rms_eps))) return dcut_fail(c, DCUT_EINVAL, "rms_eps must be >= 0 and finite");
+    const long long strides[6] = {x->q_token_stride, x->q_head_stride, x->k_token_stride, x->k_head_stride, x->v_token_stride, x->v_head_stride};
+    for (int i = x->q ? 0 : 2; i < 6; ++i)
+        if (strides[i] < 0 || strides[i] % 8) return dcut_fail(c, DCUT_EINVAL, "strides must be multiples of 8 elements and >= 0");
+    const uintptr_t al16 = reinterpret_cast<uintptr_t>(x->q) | reinterpret_cast<uintptr_t>(x->k) | reinterpret_cast<uintptr_t>(x->v) |
+                           reinterpret_cast<uintptr_t>(q_out) | reinterpret_cast<uintptr_t>(r->q_gain) | reinterpret_cast<uintptr_t>(r->k_gain);
+    if ((al16 & 15) || (reinterpret_cast<uintptr_t>(r->inv_freq) & 7)) return dcut_fail(c, DCUT_EINVAL, "q, k, v, q_out and gains must be 16-byte aligned, inv_freq 8-byte");
+    if ((reinterpret_cast<uintptr_t>(k_cache) | reinterpret_cast<uintptr_t>(v_cache)) & 127) return dcut_fail(c, DCUT_EINVAL, "caches must be 128-byte aligned");
+    if (groups && (groups->n_groups < 1 || groups->n_groups > B || !groups->cu_group || !groups->prefix_lens))
+        return dcut_fail(c, DCUT_EINVAL, "prefix groups: need 1 <= n_groups <= B, cu_group and prefix_lens");
+    DCUT_ON_DEVICE(c);
+    DcutRopeArgs a;
+    a.q = static_cast<const __nv_bfloat16*>(x->q);
+    a.k = static_cast<const __nv_bfloat16*>(x->k);
+    a.v = static_cast<const __nv_bfloat16*>(x->v);
+    a.q_token_stride = x->q_token_stride; a.q_head_stride = x->q_head_stride;
+    a.k_token_stride = x->k_token_stride; a.k_head_stride = x->k_head_stride;
+    a.v_token_stride = x->v_token_stride; a.v_head_stride = x->v_head_stride;
+    a.inv_freq = r->inv_freq; a.rotary_dim = r->rotary_dim; a.interleaved = r->interleaved != 0;
+    a.q_gain = static_cast<const __nv_bfloat16*>(r->q_gain);
+    a.k_gain = static_cast<const __nv_bfloat16*>(r->k_gain);
+    a.rms_eps = r->rms_eps;
+    a.n_groups = groups ? groups->n_groups : 0;
+    a.cu_group = groups ? groups->cu_group : nullptr;
+    a.prefix_lens = groups ? groups->prefix_lens : nullptr;
+    a.cu_q = cu_q; a.B = B; a.n_q_heads = l.n_q_heads; a.n_kv_heads = l.n_kv_heads;
+    a.tok_req = tok_req; a.tok_pos = tok_pos; a.block_table = block_table; a.block_table_stride = block_table_stride;
+    a.num_pages = num_pages;
+    a.q_out = static_cast<__nv_bfloat16*>(q_out);
+    a.k_cache = static_cast<__nv_bfloat16*>(k_cache);
+    a.v_cache = static_cast<__nv_bfloat16*>(v_cache);
+    a.status = c->d_status;
+    return dcut_launch_rope_append(c, a, T_cap, static_cast<cudaStream_t>(stream));
+}
+
 dcut_status dcut_poll_device_status(dcut_ctx* c, int* code, void* stream) {
     if (!c) return DCUT_EINVAL;
     DeviceGuard guard(c->device);

@@ -19,6 +19,7 @@
 #define DCUT_DEV_COMMIT_OVERFLOW 5      // dcut_commit: a context or a token stream ran out of room
 #define DCUT_DEV_BAD_TOKEN 6            // dcut_model_verify: a token id outside [0, vocab)
 #define DCUT_DEV_BAD_CU_Q 7             // acceptance: cu_q is not a packing of B requests of 1..gamma+1 rows within T_cap
+#define DCUT_DEV_BAD_APPEND 8           // dcut_rope_append: a token's request or position has no place in the block table
 
 // One row of the attention work table: a (request, row block of its query tile); it stands for n_kv_heads work items of
 // equal cost, one per kv head, each over the request's `pages` KV pages.
@@ -157,6 +158,26 @@ __device__ __forceinline__ unsigned int dcut_ordered_bits(float f) {
 dcut_status dcut_fail(dcut_ctx* ctx, dcut_status st, const char* fmt, ...);
 dcut_status dcut_check_cuda(dcut_ctx* ctx, cudaError_t e, const char* what);
 
+// dcut_rope_append's kernel arguments (strides in elements)
+struct DcutRopeArgs {
+    const __nv_bfloat16 *q, *k, *v;      // q may be null
+    long long q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    const double* inv_freq;              // [rotary_dim / 2]
+    int rotary_dim, interleaved;
+    const __nv_bfloat16 *q_gain, *k_gain;   // [head_dim] or null
+    float rms_eps;
+    int n_groups;                        // 0: no shared prefixes
+    const int *cu_group, *prefix_lens;
+    const int* cu_q;                     // or null: every row up to T_cap is a token
+    int B, n_q_heads, n_kv_heads;
+    const int *tok_req, *tok_pos;
+    const int* block_table;
+    int block_table_stride;
+    long long num_pages;
+    __nv_bfloat16 *q_out, *k_cache, *v_cache;
+    int* status;
+};
+
 // per-device set-up (function attributes), called from dcut_create with the device current
 dcut_status dcut_init_select(dcut_ctx* ctx);
 dcut_status dcut_init_accept(dcut_ctx* ctx);
@@ -204,5 +225,6 @@ dcut_status dcut_launch_layer(dcut_ctx* ctx, const dcut_layer_weights* w, const 
                               void* v_cache, long long num_pages, const int* block_table, int block_table_stride,
                               const int* ctx_lens, const int* cu_q, const int* tok_req, const int* tok_pos, int B,
                               int T_cap, int reuse_plan, int part, cudaStream_t stream);
+dcut_status dcut_launch_rope_append(dcut_ctx* ctx, const DcutRopeArgs& a, int T_cap, cudaStream_t stream);
 dcut_status dcut_launch_residual_add(dcut_ctx* ctx, const void* a, const void* b, void* out, int width, const int* cu_q, int B,
                                      int T_cap, cudaStream_t stream);
