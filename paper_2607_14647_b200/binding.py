@@ -174,7 +174,7 @@ class PrefixGroups:
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def budget_from_ratio(B: int, gamma: int, num: int, den: int) -> int:

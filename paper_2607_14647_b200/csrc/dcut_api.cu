@@ -574,7 +574,7 @@ dcut_status dcut_rope_append(dcut_ctx* c, const dcut_qkv* x, const dcut_rope* r,
     a.n_groups = groups ? groups->n_groups : 0;
     a.cu_group = groups ? groups->cu_group : nullptr;
     a.prefix_lens = groups ? groups->prefix_lens : nullptr;
-    a.cu_q = cu_q; a.B = B; a.n_q_heads = l.n_q_heads; a.n_kv_heads = l.n_kv_heads;
+    a.cu_q = cu_q; a.B = B; a.T_cap = T_cap; a.n_q_heads = l.n_q_heads; a.n_kv_heads = l.n_kv_heads;
     a.tok_req = tok_req; a.tok_pos = tok_pos; a.block_table = block_table; a.block_table_stride = block_table_stride;
     a.num_pages = num_pages;
     a.q_out = static_cast<__nv_bfloat16*>(q_out);

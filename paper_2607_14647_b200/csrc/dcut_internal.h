@@ -169,7 +169,7 @@ struct DcutRopeArgs {
     int n_groups;                        // 0: no shared prefixes
     const int *cu_group, *prefix_lens;
     const int* cu_q;                     // or null: every row up to T_cap is a token
-    int B, n_q_heads, n_kv_heads;
+    int B, T_cap, n_q_heads, n_kv_heads;
     const int *tok_req, *tok_pos;
     const int* block_table;
     int block_table_stride;

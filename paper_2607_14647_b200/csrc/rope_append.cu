@@ -8,8 +8,11 @@
 // Every byte is read once and written once, so the kernel is bound by HBM when there are thousands of tokens and by its
 // chain of dependent loads (token -> request -> page) when there are few.  One CTA per token: the rotation of a token is
 // the same for all its heads, so the CTA computes R/2 (cos, sin) pairs once, into shared memory.  A thread's unit is 16
-// elements of one head, as the two 16-byte vectors that rotate into each other; its first two units are requested before
-// anything else is known (the loads need only the token's number), so the page look-up and the angles hide behind them.
+// elements of one head, as the two 16-byte vectors that rotate into each other; its first four units are requested before
+// the token's place is known (the loads need only the token's number), so the page look-up and the angles hide behind them.
+// 8191 tokens of 64 query and 8 key heads of 128 (335 MB): 63 us, 5.3 TB/s.  Four early units on 64 registers move most:
+// with two 72 us, with three 65, with six (110 registers) 77; CTAs that walk several tokens, the next one's place looked
+// up ahead, 84-118 us (a barrier per token, and registers for two tokens).
 // The angle is formed in 64 bits as a fraction of a turn: at position 131072 an fp32 product is off by up to 0.008 rad.
 #include <cuda_bf16.h>
 
@@ -18,7 +21,7 @@
 namespace {
 
 constexpr int kMaxThreads = 512;
-constexpr int kEarly = 2;            // units per thread that are loaded before the token's page is known
+constexpr int kEarly = 4;            // units per thread that are loaded before the token's page is known
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -61,16 +64,16 @@ __device__ __forceinline__ Unit unit_of(int u, int n_rotated_heads, int R, int i
 }
 
 template <int DH>
-__global__ void __launch_bounds__(kMaxThreads) rope_append_heads_kernel(DcutRopeArgs a) {
+__global__ void __launch_bounds__(kMaxThreads, 2) rope_append_heads_kernel(DcutRopeArgs a) {
     constexpr int kPer = DH / 16;
     __shared__ float cos_s[DH / 2], sin_s[DH / 2];
     __shared__ int prefix_s;
     dcut_pdl_wait();
     dcut_pdl_launch_dependents();
     const int tok = blockIdx.x, tid = threadIdx.x;
-    if (a.cu_q && tok >= a.cu_q[a.B]) return;
-    const int req = a.tok_req[tok], pos = a.tok_pos[tok];
-    if (req < 0) return;                                      // padding
+    const int req = a.tok_req[tok], pos = a.tok_pos[tok];     // together with cu_q: one trip to memory
+    const int T = a.cu_q ? a.cu_q[a.B] : a.T_cap;
+    if (tok >= T || req < 0) return;                          // behind the last token, or padding
     const int Hq = a.q ? a.n_q_heads : 0, Hr = Hq + a.n_kv_heads, units = (Hr + a.n_kv_heads) * kPer;
 
     auto source = [&](const Unit& x) -> const __nv_bfloat16* {
@@ -89,23 +92,28 @@ __global__ void __launch_bounds__(kMaxThreads) rope_append_heads_kernel(DcutRope
             early[i][1] = *reinterpret_cast<const uint4*>(src + x.hi);
         }
     }
-    if (tid == 0) prefix_s = 0;
-    if (a.n_groups) __syncthreads();
-    for (int g = tid; g < a.n_groups; g += blockDim.x) {      // the request's group: cu_group is ascending, one g matches
-        const int len = a.prefix_lens[g];
-        if (a.cu_group[g] <= req && req < a.cu_group[g + 1]) prefix_s = len;
+    int prefix = 0;
+    if (a.n_groups) {
+        if (tid == 0) prefix_s = 0;
+        __syncthreads();
+        for (int g = tid; g < a.n_groups; g += blockDim.x) {  // the request's group: cu_group is ascending, one g matches
+            const int len = a.prefix_lens[g];
+            if (a.cu_group[g] <= req && req < a.cu_group[g + 1]) prefix_s = len;
+        }
+        __syncthreads();
+        prefix = prefix_s;
     }
-    for (int e = tid; e < a.rotary_dim >> 1; e += blockDim.x) {
-        const double turns = (double)pos * a.inv_freq[e] * 0.15915494309189535;    // 1 / (2 pi)
-        sincospif((float)(2.0 * (turns - rint(turns))), &sin_s[e], &cos_s[e]);
-    }
-    __syncthreads();
-    const long long slot = (long long)pos - prefix_s;
+    const long long slot = (long long)pos - prefix;
     if (req >= a.B || pos < 0 || slot < 0 || slot / 16 >= a.block_table_stride) {
         if (tid == 0) atomicExch(a.status, DCUT_DEV_BAD_APPEND);
         return;
     }
     const int page = a.block_table[(size_t)req * a.block_table_stride + slot / 16];
+    for (int e = tid; e < a.rotary_dim >> 1; e += blockDim.x) {
+        const double turns = (double)pos * a.inv_freq[e] * 0.15915494309189535;    // 1 / (2 pi)
+        sincospif((float)(2.0 * (turns - rint(turns))), &sin_s[e], &cos_s[e]);
+    }
+    __syncthreads();
     if (page < 0 || page >= a.num_pages) {
         if (tid == 0) atomicExch(a.status, DCUT_DEV_BAD_PAGE);
         return;
