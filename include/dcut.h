@@ -446,6 +446,25 @@ dcut_status dcut_rope_append(dcut_ctx* ctx, const dcut_qkv* qkv, const dcut_rope
                              const int* tok_pos, int T_cap, void* stream);
 
 /*
+ * Verification attention of a batch whose requests share prefixes: dcut_verify_attn's result (the same formula, mask,
+ * types and layouts, softmax over all positions j = 0 .. L_i + t) where position j lies as dcut_prefix_groups says.  The
+ * shared positions of a group are read once for all its rows, on the tensor cores; ctx_lens[i] = L_i counts the prefix, so
+ * L_i >= prefix_lens of the request's group.  Slots behind prefix_lens[g] in the prefix's last page may hold anything.
+ * DEVICE in: q bf16 [T_cap rows readable, n_q_heads, head_dim], the caches, block_table (own pages), ctx_lens, cu_q, the
+ *   arrays of `groups` (n_groups <= B; the struct is read during the call only).  DEVICE out: out, lse as dcut_verify_attn;
+ *   rows from cu_q[B] on are not touched.
+ * dcut_enable_prefix_attn reserves the scratch, once, outside of any stream capture: fp32 outputs of the own parts
+ * (max_T * n_q_heads * (head_dim + 1) * 4 bytes) and the pieces of cut work items (512 rows per SM); max_groups <= max_B bounds
+ * n_groups (a later call may raise it).  Without it dcut_prefix_attn returns DCUT_ECAPACITY.
+ * A cu_q that does not pack B requests of 1 .. max_gamma + 1 rows into T_cap sets device status 7; groups that do not cover
+ * the batch, a prefix longer than its table or than a context of its group set status 9; the call then writes nothing.
+ */
+dcut_status dcut_enable_prefix_attn(dcut_ctx* ctx, int max_groups);
+dcut_status dcut_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, long long num_pages,
+                             const int* block_table, int block_table_stride, const int* ctx_lens, const int* cu_q, int B,
+                             int T_cap, const dcut_prefix_groups* groups, float scale, void* out, float* lse, void* stream);
+
+/*
  * dcut_accept without any allocation.  (The paper has no counterpart: this entry point exists for
  * the way the library gets embedded, not for the method.)
  *
@@ -533,7 +552,9 @@ dcut_status dcut_verify_step_host(dcut_ctx* ctx, const dcut_host_step* step, voi
  * kernel gave up, 5 = dcut_commit ran out of room, 6 = dcut_model_verify met a token id outside [0, vocab),
  * 7 = an acceptance call met a cu_q that is not a packing of B requests of 1 .. gamma + 1 rows inside T_cap
  * (rows at or past T_cap were left out: nothing outside the caller's T_cap rows is read or written), 8 =
- * dcut_rope_append met a token whose request or position has no place in the block table (it was left out). */
+ * dcut_rope_append met a token whose request or position has no place in the block table (it was left out), 9 =
+ * dcut_prefix_attn met groups that do not cover the batch or a prefix that does not fit (nothing was written; 7 there: a
+ * cu_q that does not pack the batch). */
 dcut_status dcut_poll_device_status(dcut_ctx* ctx, int* code, void* stream);
 
 #ifdef __cplusplus

@@ -33,7 +33,7 @@ EXPORTS = ["dcut_create", "dcut_destroy", "dcut_last_error", "dcut_set_cost_dens
            "dcut_enable_plan_in_select", "dcut_cost_grid_create", "dcut_cost_grid_destroy", "dcut_cost_grid_budget",
            "dcut_cost_grid_record", "dcut_cost_grid_get", "dcut_cost_grid_nearest", "dcut_cost_grid_buckets",
            "dcut_set_cost_from_grid", "dcut_layer_attn_part", "dcut_layer_mlp_part", "dcut_residual_add",
-           "dcut_rope_append"]
+           "dcut_rope_append", "dcut_enable_prefix_attn", "dcut_prefix_attn"]
 
 
 class Limits(C.Structure):
@@ -122,6 +122,9 @@ class Rope(C.Structure):
 
 _lib.dcut_rope_append.argtypes = [_vp, C.POINTER(Qkv), C.POINTER(Rope), _vp, _vp, _vp, _ll, _vp, _i, C.POINTER(PrefixGroupsRec),
                                   _vp, _i, _vp, _vp, _i, _vp]
+
+_lib.dcut_enable_prefix_attn.argtypes = [_vp, _i]
+_lib.dcut_prefix_attn.argtypes = [_vp, _vp, _vp, _vp, _ll, _vp, _i, _vp, _vp, _i, _i, C.POINTER(PrefixGroupsRec), _f, _vp, _vp, _vp]
 
 
 @dataclass
@@ -524,6 +527,24 @@ class Context:
                                           _ptr(cu_q, torch.int32), block_table.shape[0], _ptr(tok_req, torch.int32),
                                           _ptr(tok_pos, torch.int32), T_cap, _stream()))
         return q_out
+
+    def enable_prefix_attn(self, max_groups: int):
+        """dcut_enable_prefix_attn: reserves the scratch of prefix_attn (once, outside of any graph capture)."""
+        self._check(_lib.dcut_enable_prefix_attn(self._h, max_groups))
+
+    def prefix_attn(self, q, k_cache, v_cache, block_table, ctx_lens, cu_q, T_cap: int, groups: PrefixGroups,
+                    scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """dcut_prefix_attn: verify_attn for requests that share prefixes; `block_table` holds their own pages only."""
+        assert q.shape[0] >= T_cap, "q needs T_cap rows"
+        if out is None:
+            out = torch.empty_like(q)
+        if scale is None:
+            scale = 1.0 / float(np.sqrt(self.limits.head_dim))
+        self._check(_lib.dcut_prefix_attn(self._h, _ptr(q, torch.bfloat16), _ptr(k_cache, torch.bfloat16), _ptr(v_cache, torch.bfloat16),
+                                          k_cache.shape[0], _ptr(block_table, torch.int32), block_table.shape[1], _ptr(ctx_lens, torch.int32),
+                                          _ptr(cu_q, torch.int32), ctx_lens.shape[0], T_cap, C.byref(groups.rec), float(scale),
+                                          _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), _stream()))
+        return out
 
     def make_model(self, layers: list, embed, g_final, w_lm, k_caches: list, v_caches: list, rms_eps: float = 1e-6,
                    rope_theta: float = 1e6) -> "PreparedModel":

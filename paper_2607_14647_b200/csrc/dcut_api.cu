@@ -69,6 +69,7 @@ void free_all(dcut_ctx* c) {
     cudaFree(c->d_row_key);
     cudaFree(c->d_rs_scratch);
     cudaFree(c->d_status);
+    cudaFree(c->prefix_scratch);
     cudaFree(c->ly_norm);
     cudaFree(c->ly_qkv);
     cudaFree(c->ly_q);
@@ -325,7 +326,7 @@ dcut_status dcut_verify_attn(dcut_ctx* c, const void* q, const void* k_cache, co
         return dcut_fail(c, DCUT_ECAPACITY, "cache has too many token rows for 32-bit tile coordinates");
     if (!(scale > 0.0f) || isinf(scale)) return dcut_fail(c, DCUT_EINVAL, "scale must be positive and finite");
     return dcut_launch_verify_attn(c, q, k_cache, v_cache, num_pages, block_table, block_table_stride, ctx_lens, cu_q, B,
-                                   T_cap, scale, out, lse, 0, static_cast<cudaStream_t>(stream));
+                                   T_cap, scale, out, lse, 0, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 dcut_status dcut_accept(dcut_ctx* c, const void* logits, int V, const int* draft_ids, const int* cu_q, int B, int gamma,
@@ -582,6 +583,43 @@ dcut_status dcut_rope_append(dcut_ctx* c, const dcut_qkv* x, const dcut_rope* r,
     a.v_cache = static_cast<__nv_bfloat16*>(v_cache);
     a.status = c->d_status;
     return dcut_launch_rope_append(c, a, T_cap, static_cast<cudaStream_t>(stream));
+}
+
+dcut_status dcut_enable_prefix_attn(dcut_ctx* c, int max_groups) {
+    if (!c) return DCUT_EINVAL;
+    if (c->lim.n_q_heads <= 0) return dcut_fail(c, DCUT_EINVAL, "context was created without attention shapes");
+    if (max_groups < 1) return dcut_fail(c, DCUT_EINVAL, "max_groups must be >= 1");
+    if (max_groups > c->lim.max_B) return dcut_fail(c, DCUT_ECAPACITY, "max_groups = %d exceeds max_B = %d", max_groups, c->lim.max_B);
+    DCUT_ON_DEVICE(c);
+    return dcut_enable_prefix(c, max_groups);
+}
+
+dcut_status dcut_prefix_attn(dcut_ctx* c, const void* q, const void* k_cache, const void* v_cache, long long num_pages,
+                             const int* block_table, int block_table_stride, const int* ctx_lens, const int* cu_q, int B,
+                             int T_cap, const dcut_prefix_groups* groups, float scale, void* out, float* lse, void* stream) {
+    if (!c) return DCUT_EINVAL;
+    const dcut_limits& l = c->lim;
+    if (l.n_q_heads <= 0) return dcut_fail(c, DCUT_EINVAL, "context was created without attention shapes");
+    if (!q || !k_cache || !v_cache || !block_table || !ctx_lens || !cu_q || !out || !groups || !groups->cu_group || !groups->prefix_lens || !groups->prefix_table)
+        return dcut_fail(c, DCUT_EINVAL, "null pointer argument");
+    if (B < 1 || T_cap < B || num_pages < 1) return dcut_fail(c, DCUT_EINVAL, "need B >= 1, T_cap >= B, num_pages >= 1");
+    if (B > l.max_B || T_cap > l.max_B * (l.max_gamma + 1)) return dcut_fail(c, DCUT_ECAPACITY, "B = %d, T_cap = %d exceed the limits", B, T_cap);
+    if (block_table_stride < 1 || block_table_stride > l.max_pages_per_req)
+        return dcut_fail(c, DCUT_ECAPACITY, "block_table_stride = %d outside [1, %d]", block_table_stride, l.max_pages_per_req);
+    if (groups->n_groups < 1 || groups->n_groups > B) return dcut_fail(c, DCUT_EINVAL, "n_groups = %d outside [1, B]", groups->n_groups);
+    if (groups->prefix_table_stride < 1 || groups->prefix_table_stride > l.max_pages_per_req || groups->prefix_table_stride > (1 << 26))
+        return dcut_fail(c, DCUT_ECAPACITY, "prefix_table_stride = %d outside [1, %d]", groups->prefix_table_stride, l.max_pages_per_req);
+    if ((reinterpret_cast<uintptr_t>(k_cache) & 127) || (reinterpret_cast<uintptr_t>(v_cache) & 127) ||
+        (reinterpret_cast<uintptr_t>(q) & 15) || (reinterpret_cast<uintptr_t>(out) & 15))
+        return dcut_fail(c, DCUT_EINVAL, "k_cache / v_cache must be 128-byte aligned, q / out 16-byte aligned");
+    if ((num_pages * l.n_kv_heads * l.page_size) >= (1ll << 31))
+        return dcut_fail(c, DCUT_ECAPACITY, "cache has too many token rows for 32-bit tile coordinates");
+    if (!(scale > 0.0f) || isinf(scale)) return dcut_fail(c, DCUT_EINVAL, "scale must be positive and finite");
+    DCUT_ON_DEVICE(c);
+    if (groups->n_groups > c->prefix_max_groups)
+        return dcut_fail(c, DCUT_ECAPACITY, "%d groups, but dcut_enable_prefix_attn reserved %d", groups->n_groups, c->prefix_max_groups);
+    return dcut_launch_prefix_attn(c, q, k_cache, v_cache, num_pages, block_table, block_table_stride, ctx_lens, cu_q, B, T_cap, groups,
+                                   scale, out, lse, static_cast<cudaStream_t>(stream));
 }
 
 dcut_status dcut_poll_device_status(dcut_ctx* c, int* code, void* stream) {

@@ -20,6 +20,7 @@
 #define DCUT_DEV_BAD_TOKEN 6            // dcut_model_verify: a token id outside [0, vocab)
 #define DCUT_DEV_BAD_CU_Q 7             // acceptance: cu_q is not a packing of B requests of 1..gamma+1 rows within T_cap
 #define DCUT_DEV_BAD_APPEND 8           // dcut_rope_append: a token's request or position has no place in the block table
+#define DCUT_DEV_BAD_GROUPS 9           // dcut_prefix_attn: the groups do not cover the batch, or a prefix does not fit its table or contexts
 
 // One row of the attention work table: a (request, row block of its query tile); it stands for n_kv_heads work items of
 // equal cost, one per kv head, each over the request's `pages` KV pages.
@@ -95,6 +96,10 @@ struct dcut_ctx {
     // rejection-sampling acceptance scratch (vocab > 0 only)
     void* d_rs_scratch;
     int rs_n_seg;
+
+    // shared-prefix attention (dcut_enable_prefix_attn)
+    unsigned char* prefix_scratch;
+    int prefix_max_groups;  // 0: not enabled
 
     int* d_status;          // device status word
 
@@ -203,7 +208,11 @@ dcut_status dcut_launch_accept_rs(dcut_ctx* ctx, const void* target_logits, cons
 dcut_status dcut_launch_verify_attn(dcut_ctx* ctx, const void* q, const void* k_cache, const void* v_cache,
                                     long long num_pages, const int* block_table, int block_table_stride,
                                     const int* ctx_lens, const int* cu_q, int B, int T_cap, float scale,
-                                    void* out, float* lse, int reuse_plan, cudaStream_t stream);
+                                    void* out, float* lse, int reuse_plan, float* out_f32, cudaStream_t stream);
+// tensor maps of the paged cache: whole (page, kv head) tiles, and the K tiles of the tcgen05 paths (head_dim 128)
+struct CUtensorMap_st;
+dcut_status dcut_make_cache_map(dcut_ctx* ctx, CUtensorMap_st* map, const void* base, long long num_pages);
+dcut_status dcut_make_k_group_map(dcut_ctx* ctx, CUtensorMap_st* map, const void* base, long long num_pages);
 dcut_status dcut_launch_gemm(dcut_ctx* ctx, const void* a, const void* w, const void* w2, int mode, int N, int K,
                              const int* cu_q, int B, int T_cap, void* out, const void* residual, cudaStream_t stream);
 dcut_status dcut_launch_lm_head_argmax(dcut_ctx* ctx, const void* x, const void* w_lm, int V, int K, const int* cu_q, int B,
@@ -225,6 +234,10 @@ dcut_status dcut_launch_layer(dcut_ctx* ctx, const dcut_layer_weights* w, const 
                               void* v_cache, long long num_pages, const int* block_table, int block_table_stride,
                               const int* ctx_lens, const int* cu_q, const int* tok_req, const int* tok_pos, int B,
                               int T_cap, int reuse_plan, int part, cudaStream_t stream);
+dcut_status dcut_enable_prefix(dcut_ctx* ctx, int max_groups);
+dcut_status dcut_launch_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, long long num_pages,
+                                    const int* block_table, int block_table_stride, const int* ctx_lens, const int* cu_q, int B,
+                                    int T_cap, const dcut_prefix_groups* groups, float scale, void* out, float* lse, cudaStream_t stream);
 dcut_status dcut_launch_rope_append(dcut_ctx* ctx, const DcutRopeArgs& a, int T_cap, cudaStream_t stream);
 dcut_status dcut_launch_residual_add(dcut_ctx* ctx, const void* a, const void* b, void* out, int width, const int* cu_q, int B,
                                      int T_cap, cudaStream_t stream);

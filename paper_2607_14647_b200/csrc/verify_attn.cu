@@ -323,6 +323,7 @@ struct AttnArgs {
     int q_row_bytes;           // head_dim * 2
     int tail_on;               // query tiles above 128 rows can occur with this context's shapes: the tail warps take part
     __nv_bfloat16* out;
+    float* out_f32;            // not null: the output stays in fp32, here (shared-prefix attention merges it with more keys)
     float* lse;                // [T, Hq] or null
     float* part_o;
     float* part_lse;
@@ -780,7 +781,8 @@ __device__ __forceinline__ void mma_phase(const CUtensorMap& k_map, const CUtens
                     uint2 pk;
                     pk.x = pack_bf16(acc.x, acc.y);
                     pk.y = pack_bf16(acc.z, acc.w);
-                    *reinterpret_cast<uint2*>(a.out + orow * DH + c4 * 4) = pk;
+                    if (a.out_f32) *reinterpret_cast<float4*>(a.out_f32 + orow * DH + c4 * 4) = acc;
+                    else *reinterpret_cast<uint2*>(a.out + orow * DH + c4 * 4) = pk;
                     if (a.lse && c4 == 0) a.lse[orow] = lse_nat;
                 } else {
                     const size_t prow = (size_t)item.part_row + R;
@@ -1142,7 +1144,11 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
                 for (int e = 0; e < 32; ++e)   // a team without groups (or without visible keys) has weight 0: its O is not read as a number
                     v[e] = (w_s > 0.0f ? __uint_as_float(os[e]) * f_s : 0.0f) + (w_o > 0.0f ? __uint_as_float(oo[e]) * f_o : 0.0f);
                 if (R < M) {
-                    if (item.n_chunks == 1) {
+                    if (item.n_chunks == 1 && a.out_f32) {
+                        float* po = a.out_f32 + orow * 128 + cc;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(po + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                    } else if (item.n_chunks == 1) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 8) {
                             uint32_t w[4];
@@ -1518,7 +1524,8 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
                     const size_t orow = (size_t)(q0 + t) * a.n_q_heads + kvh * group + hl;
                     const float lse_nat = l_all > 0.0f ? (m_all * cs + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
                     if (item.n_chunks == 1) {
-                        *reinterpret_cast<uint2*>(a.out + orow * 128 + c4) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+                        if (a.out_f32) *reinterpret_cast<float4*>(a.out_f32 + orow * 128 + c4) = v;
+                        else *reinterpret_cast<uint2*>(a.out + orow * 128 + c4) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
                         if (a.lse && c4 == 0) a.lse[orow] = lse_nat;
                     } else {
                         const size_t prow = (size_t)item.part_row + 128 + rr;
@@ -1548,8 +1555,9 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
 #pragma unroll
                             for (int j = 0; j < 16; ++j) {
                                 const float2 v = *reinterpret_cast<const float2*>(po + j * 8);
-                                *reinterpret_cast<uint32_t*>(a.out + orow * 128 + j * 8 + c0) =
-                                    pack_bf16(o[j][2 * r] * f_s + v.x * f_o, o[j][2 * r + 1] * f_s + v.y * f_o);
+                                const float x0 = o[j][2 * r] * f_s + v.x * f_o, x1 = o[j][2 * r + 1] * f_s + v.y * f_o;
+                                if (a.out_f32) *reinterpret_cast<float2*>(a.out_f32 + orow * 128 + j * 8 + c0) = make_float2(x0, x1);
+                                else *reinterpret_cast<uint32_t*>(a.out + orow * 128 + j * 8 + c0) = pack_bf16(x0, x1);
                             }
                             if (a.lse && (lane & 3) == 0) a.lse[orow] = lse_nat;
                         } else {
@@ -1660,6 +1668,7 @@ struct CombineArgs {
     const float* part_lse;
     int n_q_heads, n_kv_heads;
     __nv_bfloat16* out;
+    float* out_f32;
     float* lse;
 };
 
@@ -1701,7 +1710,8 @@ __global__ void __launch_bounds__(1024) attn_combine_kernel(CombineArgs a) {
 #pragma unroll
             for (int e = 0; e < kPer; e += 2) {
                 const float x0 = fmaf(w1, o1[e], fmaf(w0, o0[e], 0.0f)), x1 = fmaf(w1, o1[e + 1], fmaf(w0, o0[e + 1], 0.0f));
-                *reinterpret_cast<uint32_t*>(op + e) = pack_bf16(x0 * inv, x1 * inv);
+                if (a.out_f32) *reinterpret_cast<float2*>(a.out_f32 + orow * DH + lane * kPer + e) = make_float2(x0 * inv, x1 * inv);
+                else *reinterpret_cast<uint32_t*>(op + e) = pack_bf16(x0 * inv, x1 * inv);
             }
             if (a.lse && lane == 0) a.lse[orow] = wsum > 0.0f ? m_all + logf(wsum) : -INFINITY;
             continue;
@@ -1726,7 +1736,10 @@ __global__ void __launch_bounds__(1024) attn_combine_kernel(CombineArgs a) {
         }
         const float inv = wsum > 0.0f ? 1.0f / wsum : 0.0f;
 #pragma unroll
-        for (int e = 0; e < kPer; e += 2) *reinterpret_cast<uint32_t*>(op + e) = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+        for (int e = 0; e < kPer; e += 2) {
+            if (a.out_f32) *reinterpret_cast<float2*>(a.out_f32 + orow * DH + lane * kPer + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
+            else *reinterpret_cast<uint32_t*>(op + e) = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+        }
         if (a.lse && lane == 0) a.lse[orow] = wsum > 0.0f ? m_all + logf(wsum) : -INFINITY;
     }
 }
@@ -1738,7 +1751,9 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-dcut_status make_cache_map(dcut_ctx* ctx, CUtensorMap* map, const void* base, long long num_pages) {
+}  // namespace
+
+dcut_status dcut_make_cache_map(dcut_ctx* ctx, CUtensorMap* map, const void* base, long long num_pages) {
     // The cache seen as a 3-D tensor {64 columns, token rows, head_dim / 64 column halves}: one box
     // {64, 16, halves} is a whole (page, kv head) tile and lands in shared memory as
     // [half][16 rows][64 columns] with the 128-byte swizzle the ldmatrix addressing expects.
@@ -1754,6 +1769,23 @@ dcut_status make_cache_map(dcut_ctx* ctx, CUtensorMap* map, const void* base, lo
     if (r != CUDA_SUCCESS) return dcut_fail(ctx, DCUT_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
     return DCUT_OK;
 }
+
+dcut_status dcut_make_k_group_map(dcut_ctx* ctx, CUtensorMap* map, const void* base, long long num_pages) {
+    // The K cache for tcgen05 operands at head_dim 128: token rows of 128 columns seen as (64 columns, 8 rows, 2 halves,
+    // groups of 8 rows), so that a {64, 8, 2, 2} box (one page: 16 rows, 4 KB) arrives as [group][half][row][64 columns]:
+    // each half is a K-major tile of 128-byte rows whose 8-row groups are 2048 bytes apart.
+    cuuint64_t dims[4] = {64, 8, 2, (cuuint64_t)num_pages * ctx->lim.n_kv_heads * kPage / 8};
+    cuuint64_t strides[3] = {256, 128, 2048};
+    cuuint32_t box[4] = {64, 8, 2, 2}, estr[4] = {1, 1, 1, 1};
+    CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(
+        map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return dcut_fail(ctx, DCUT_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+    return DCUT_OK;
+}
+
+namespace {
 
 template <int DH>
 dcut_status launch_t(dcut_ctx* ctx, const CUtensorMap& km, const CUtensorMap& vm, const CUtensorMap& k2m, const AttnArgs& aa,
@@ -1829,26 +1861,14 @@ void dcut_fill_plan_args(dcut_ctx* ctx, const int* ctx_lens, const int* cu_q, in
 dcut_status dcut_launch_verify_attn(dcut_ctx* ctx, const void* q, const void* k_cache, const void* v_cache,
                                     long long num_pages, const int* block_table, int block_table_stride,
                                     const int* ctx_lens, const int* cu_q, int B, int T_cap, float scale,
-                                    void* out, float* lse, int reuse_plan, cudaStream_t stream) {
+                                    void* out, float* lse, int reuse_plan, float* out_f32, cudaStream_t stream) {
     CUtensorMap km, vm, k2m;
-    dcut_status st = make_cache_map(ctx, &km, k_cache, num_pages);
+    dcut_status st = dcut_make_cache_map(ctx, &km, k_cache, num_pages);
     if (st != DCUT_OK) return st;
-    st = make_cache_map(ctx, &vm, v_cache, num_pages);
+    st = dcut_make_cache_map(ctx, &vm, v_cache, num_pages);
     if (st != DCUT_OK) return st;
     k2m = km;
-    if (ctx->lim.head_dim == 128) {
-        // The K cache for the tcgen05 phase: token rows of 128 columns seen as (64 columns, 8 rows, 2 halves, groups of
-        // 8 rows), so that a {64, 8, 2, 2} box (one page: 16 rows, 4 KB) arrives as [group][half][row][64 columns]:
-        // each half is a K-major tile of 128-byte rows whose 8-row groups are 2048 bytes apart.
-        cuuint64_t dims[4] = {64, 8, 2, (cuuint64_t)num_pages * ctx->lim.n_kv_heads * kPage / 8};
-        cuuint64_t strides[3] = {256, 128, 2048};
-        cuuint32_t box[4] = {64, 8, 2, 2}, estr[4] = {1, 1, 1, 1};
-        CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(
-            &k2m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(k_cache), dims, strides, box, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-        if (r != CUDA_SUCCESS) return dcut_fail(ctx, DCUT_ECUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
-    }
+    if (ctx->lim.head_dim == 128 && (st = dcut_make_k_group_map(ctx, &k2m, k_cache, num_pages)) != DCUT_OK) return st;
 
     PlanArgs pa;
     dcut_fill_plan_args(ctx, ctx_lens, cu_q, B, &pa);
@@ -1878,6 +1898,7 @@ dcut_status dcut_launch_verify_attn(dcut_ctx* ctx, const void* q, const void* k_
     aa.q_row_bytes = ctx->lim.head_dim * 2;
     aa.tail_on = ctx->attn_tail_rows > 0 && (ctx->lim.max_gamma + 1) * (ctx->lim.n_q_heads / ctx->lim.n_kv_heads) > 128;
     aa.out = static_cast<__nv_bfloat16*>(out);
+    aa.out_f32 = out_f32;
     aa.lse = lse;
     aa.part_o = ctx->d_part_o;
     aa.part_lse = ctx->d_part_lse;
@@ -1890,6 +1911,7 @@ dcut_status dcut_launch_verify_attn(dcut_ctx* ctx, const void* q, const void* k_
     ca.n_q_heads = ctx->lim.n_q_heads;
     ca.n_kv_heads = ctx->lim.n_kv_heads;
     ca.out = static_cast<__nv_bfloat16*>(out);
+    ca.out_f32 = out_f32;
     ca.lse = lse;
 
     if (ctx->lim.head_dim == 128) return launch_t<128>(ctx, km, vm, k2m, aa, ca, T_cap, stream);

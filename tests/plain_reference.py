@@ -26,10 +26,11 @@ def prefix_len_of(req, cu_group, prefix_lens):
 
 
 def prefix_attn(q, k_cache, v_cache, block_table, ctx_lens, cu_q, cu_group, prefix_lens, prefix_table, scale):
-    """out fp64 [T, Hq, D], lse [T, Hq]: softmax over the group's shared positions and the request's own ones."""
+    """out fp64 [T, Hq, D], lse [T, Hq]: softmax over the group's shared positions and the request's own ones; also the
+    weighted mean of |v| (what relative errors of the weights act on) and the largest sum_c |q_c k_c| of a row's scores."""
     T, Hq, D = q.shape
     Hkv = k_cache.shape[1]
-    out, lse = np.zeros((T, Hq, D)), np.zeros((T, Hq))
+    out, lse, mean_abs, abs_score = np.zeros((T, Hq, D)), np.zeros((T, Hq)), np.zeros((T, Hq, D)), np.zeros((T, Hq))
     G = np.asarray(cu_group)
     for i in range(len(ctx_lens)):
         g = int(np.searchsorted(G, i, side="right") - 1)
@@ -45,7 +46,9 @@ def prefix_attn(q, k_cache, v_cache, block_table, ctx_lens, cu_q, cu_group, pref
             p = np.exp(s - m)
             out[cu_q[i]:cu_q[i + 1], h] = np.where(p > 0, p, 0) @ v[:, h // (Hq // Hkv)] / p.sum(1, keepdims=True)
             lse[cu_q[i]:cu_q[i + 1], h] = (m + np.log(p.sum(1, keepdims=True)))[:, 0]
-    return out, lse
+            mean_abs[cu_q[i]:cu_q[i + 1], h] = p @ np.abs(v[:, h // (Hq // Hkv)]) / p.sum(1, keepdims=True)
+            abs_score[cu_q[i]:cu_q[i + 1], h] = (np.abs(q[cu_q[i]:cu_q[i + 1], h]) @ np.abs(k[:, h // (Hq // Hkv)]).T * scale).max(1)
+    return out, lse, mean_abs, abs_score
 
 
 def linear(a, w, bias=None, act="none", w2=None, bias2=None, residual=None):
