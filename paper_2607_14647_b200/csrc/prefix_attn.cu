@@ -12,18 +12,18 @@
 //   prefix_combine_kernel  merges the pieces of the items that a segment boundary cuts, and the own part's result
 //
 // prefix_attn_kernel, persistent, one CTA per SM, 384 threads.  An item is 256 query rows (two tiles of 128) of a kv head
-// against a run of 128-key blocks:
-//   warp 0      TMA: the item's Q tiles, and K and V of each block page by page into a ring of four 128-key slots
-//   warp 1      issues tcgen05.mma (one elected lane): S_t = Q_t K^T (A and B from shared memory), O_t += P_t V (P from
-//               tensor memory, V read MN-major).  Per tile a 128 x 128 fp32 S, whose first 64 columns P takes over as
-//               bf16, and a 128 x DH fp32 O: two tiles fill the 512 columns of tensor memory.
-//   warps 4-11  two softmax teams, one per tile, a thread per row: while one team exponentiates, the tensor cores work
-//               for the other.  The running maximum only moves when it would grow by more than 2^8 (then O is rescaled in
-//               tensor memory); row sums are kept in fp32 over the unrounded weights.
+// against a run of 64-key blocks:
+//   warp 0      TMA: the item's Q tiles, and K and V of each block page by page into a ring of eight 64-key slots
+//   warps 1-2   issue tcgen05.mma, one elected lane per tile t: S_t = Q_t K^T (A and B from shared memory), O_t += P_t V
+//               (P from tensor memory, V read MN-major)
+//   warps 4-11  two softmax teams, one per tile, a thread per row.  The running maximum only moves when it would grow by
+//               more than 2^8 (then O is rescaled in tensor memory); row sums are kept in fp32 over the unrounded weights.
+// Tensor memory holds, per tile, a 128 x DH fp32 O and two 128 x 64 fp32 S, each of which its P replaces in place: while a
+// team exponentiates one block, the tensor cores fill its other buffer, and a step has two hand-overs only (S to the
+// softmax, P to the MMAs), each of about 190 cycles between warps.
 // An odd last tile is a single: both teams work on the one tile, taking its key blocks in turn, and merge at the end.
-// Two tiles share each K and V byte that comes from L2: 64 KB per 2 x 128 x 128 keys x rows, 32 bytes per cycle and SM at
-// the full MMA rate.  P is rounded to bf16 (relative 2^-9, as V's type asks of the MMA); everything else stays in fp32
-// until the one rounding of the output.
+// P is rounded to bf16 (relative 2^-9, as V's type asks of the MMA); everything else stays in fp32 until the one rounding
+// of the output.
 //
 // Every wait is bounded; on expiry a role sets the device status word, the others see the CTA's abort flag.
 #include <cuda.h>
@@ -38,14 +38,13 @@ namespace {
 using namespace dcut_prefix;
 
 constexpr int kThreads = 384;
-constexpr int kRegsControl = 88, kRegsSoftmax = 208;   // per thread of the warpgroups: 88 + 2 x 208 = 3 x 168, what 384 threads start with
 constexpr int kTeamThreads = 128;
-constexpr int kSlots = 4;             // ring of K and V blocks (a single's MMAs reach four blocks ahead: prefix order K V K V)
+constexpr int kSlots = 8;             // ring of K and V blocks, in the order K V K V
 constexpr int kPage = dcut_plan::kPage;
 constexpr int kPagesPerBlock = kBlock / kPage;
 constexpr int kStageBytes = 2048;     // epilogue staging of a warp: 32 rows x 16 fp32
 constexpr int kSpinLimit = 1 << 21;
-constexpr int kTmemCols = 512, kColO = 256;    // S of tile t: 128 t, O of tile t: 256 + DH t
+constexpr int kTmemCols = 512, kColS = 256;    // tile t: O at 128 t, S / P buffer b at 256 + 128 t + 64 b
 constexpr float kRescaleLog2 = 8.0f;
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 
@@ -65,6 +64,14 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// whether the phase is over, without waiting for it
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
@@ -139,6 +146,11 @@ __device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t* r) {
           "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
         : "memory");
 }
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                 "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -150,24 +162,6 @@ __device__ __forceinline__ float fast_exp2(float x) {     // 2 ulp; -inf -> 0
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-__device__ __forceinline__ unsigned long long pack_f32x2(float lo, float hi) {
-    unsigned long long r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack_f32x2(unsigned long long v, float& lo, float& hi) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ unsigned long long fma_f32x2(unsigned long long a, unsigned long long b, unsigned long long c) {
-    unsigned long long r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, unsigned long long b) {
-    unsigned long long r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
 }
 __device__ __forceinline__ float fmax3(float a, float b, float c) {
     float r;
@@ -207,8 +201,8 @@ struct PrefixArgs {
 struct __align__(16) Ctrl {
     unsigned long long kv_full[kSlots], kv_empty[kSlots];
     unsigned long long q_full, q_free;
-    unsigned long long s_full[2], p_full[2], pv_done[2], o_full[2];
-    unsigned long long o_free, x_ready, drain;
+    unsigned long long s_full[2][2], p_full[2][2], pv_done[2], o_full[2];   // [team][buffer], [team]
+    unsigned long long o_free, x_ready, drain[2];
     float xm[2][kTileRows], xl[2][kTileRows];      // a single's teams: running maximum and sum of each row
     uint32_t tmem_base;
     int abort;
@@ -262,7 +256,7 @@ __device__ __forceinline__ void produce(const CUtensorMap& q_map, const CUtensor
             if (blk + 1 < it.b1 && lane < pages_of_block(it.len, blk + 1)) page = table[(blk + 1) * kPagesPerBlock + lane];
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv, ++pos) {
-                const int slot = pos & (kSlots - 1), use = pos / kSlots;
+                const int slot = pos % kSlots, use = pos / kSlots;
                 if (use > 0 && !__all_sync(0xffffffffu, mbar_wait(kv_empty + 8 * slot, (use - 1) & 1, &c->abort))) {
                     failed = true;
                     break;
@@ -303,103 +297,239 @@ __device__ __forceinline__ void produce(const CUtensorMap& q_map, const CUtensor
         atomicExch(a.status, DCUT_DEV_ATTN_WAIT_TIMEOUT);
         c->abort = 1;
         // nothing of this CTA's is in flight when it leaves
-        for (int p = pos > kSlots ? pos - kSlots : 0; p < pos; ++p) mbar_wait(kv_full + 8 * (p & (kSlots - 1)), (p / kSlots) & 1, nullptr);
+        for (int p = pos > kSlots ? pos - kSlots : 0; p < pos; ++p) mbar_wait(kv_full + 8 * (p % kSlots), (p / kSlots) & 1, nullptr);
         if (n_items > 0) mbar_wait(smem_u32(&c->q_full), (n_items - 1) & 1, nullptr);
     }
 }
 
+// The issuer of one team's products.  One elected lane (not `lane == 0`: the compiler then keeps the operands of
+// tcgen05.mma in uniform registers) runs the whole role.  Each team has an issuer of its own: issuing an MMA lasts as long
+// as the MMA (about 51 cycles for Q K^T of 80 keys, 54-61 for P V of 16), a wait for a barrier about 150 even when its
+// phase is over, and while one issuer waits the other feeds the tensor pipe.
 template <int DH>
-__device__ __forceinline__ void issue(const PrefixArgs& a, unsigned char* smem, Ctrl* c, Walk w) {
+__device__ __forceinline__ void issue(const PrefixArgs& a, unsigned char* smem, Ctrl* c, Walk w, const int team) {
     using L = Smem<DH>;
     constexpr uint32_t kIdescPV = kIdescBase | (1u << 16) | ((uint32_t)(DH >> 3) << 17);
     const uint32_t kv_full = smem_u32(c->kv_full), kv_empty = smem_u32(c->kv_empty);
-    const uint32_t s_full = smem_u32(c->s_full), p_full = smem_u32(c->p_full), pv_done = smem_u32(c->pv_done), o_full = smem_u32(c->o_full);
-    const uint32_t tmem = c->tmem_base;
-    const uint32_t q_addr = smem_u32(smem);
+    const uint32_t s_full = smem_u32(c->s_full[team]), p_full = smem_u32(c->p_full[team]);
+    const uint32_t pv_done = smem_u32(c->pv_done) + 8 * team, o_full = smem_u32(c->o_full) + 8 * team;
+    const uint32_t t_o = c->tmem_base + 128 * team, t_s = c->tmem_base + kColS + 128 * team;
+    const uint32_t ring = smem_u32(smem + L::kRing);
     Item it;
-    int n_items = 0, first = 0;           // first: K/V block number of the item's first block
-    int n_pv[2] = {0, 0};
+    int n_items = 0, n_qk = 0, n_pv = 0;  // this team's steps so far: step n uses buffer n % 2, for the (n / 2)th time
+    int base = 0, base_phase = 0;         // ring slot of the item's first K block, and its phase
     bool ok = true;
-    auto wait = [&](uint32_t bar, int parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, &c->abort)); };
+    auto wait = [&](uint32_t bar, int parity) { return mbar_wait(bar, parity & 1, &c->abort); };
+    // both phases, asked for together: two answers in the time of one
+    auto wait2 = [&](uint32_t bar0, int parity0, uint32_t bar1, int parity1) {
+        return wait(bar0, parity0) && wait(bar1, parity1);
+    };
     while (ok && next_item(w, a.groups, &it)) {
         if (it.blocks == 0) continue;
-        const int nblk = it.b1 - it.b0, steps = it.dual ? nblk : (nblk + 1) >> 1;
-        int qk_left = it.dual ? 2 * nblk : nblk;
-        ok = wait(smem_u32(&c->q_full), n_items);
-        // S = Q K^T of block b for `team`: its S columns hold the P of the team's block before until that P V has completed
-        auto qk = [&](int team, int b) -> bool {
-            const int pos = 2 * (first + b), slot = pos & (kSlots - 1);
-            if (!wait(kv_full + 8 * slot, pos / kSlots)) return false;
-            if (n_pv[team] > 0 && !wait(pv_done + 8 * team, n_pv[team] - 1)) return false;
-            tc_fence_after();
-            --qk_left;
-            if (elect_one()) {
-                const uint32_t k_addr = smem_u32(smem + L::kRing + slot * L::kBlockBytes), q_tile = q_addr + (it.dual ? team * L::kQTile : 0);
-                const uint32_t idesc = kIdescBase | ((uint32_t)(pages_of_block(it.len, it.b0 + b) * kPage >> 3) << 17);
-#pragma unroll
-                for (int half = 0; half < DH / 64; ++half) {
-                    const uint64_t dq = desc_kmajor(q_tile + half * kTileRows * 128, 1024);
-                    const uint64_t dk = DH == 128 ? desc_kmajor(k_addr + half * 1024, 2048) : desc_kmajor(k_addr, 1024);
-#pragma unroll
-                    for (int ks = 0; ks < 4; ++ks) tc_mma_ss(tmem + 128 * team, dq + 2 * ks, dk + 2 * ks, idesc, (half | ks) ? 1u : 0u);
-                }
-                tc_commit(s_full + 8 * team);
-                if (!it.dual || team == 1) tc_commit(kv_empty + 8 * slot);
-                if (qk_left == 0) tc_commit(smem_u32(&c->q_free));
+        const int nblk = it.b1 - it.b0;
+        const int steps = it.dual ? nblk : (nblk + 1 - team) >> 1;            // this team's blocks: all, or every other one
+        const int last_pages = pages_of_block(it.len, it.b1 - 1);
+        const bool ends_here = it.dual || ((nblk - 1) & 1) == team;           // the piece's last block is this team's
+        const int ahead = it.dual ? 2 : 4;                                    // ring slots from one of its blocks to the next
+        const uint32_t q_tile = smem_u32(smem) + (it.dual ? team * L::kQTile : 0);
+        int k_slot = base, k_phase = base_phase;
+        auto move = [&](int& slot, int& phase, int by) {
+            slot += by;
+            if (slot >= kSlots) {
+                slot -= kSlots;
+                phase ^= 1;
             }
-            __syncwarp();
-            return true;
         };
-        auto block_of = [&](int team, int s) { return it.dual ? s : 2 * s + team; };
-        for (int team = 0; ok && team < 2; ++team)
-            if (block_of(team, 0) < nblk) ok = qk(team, block_of(team, 0));
-        for (int s = 0; ok && s < steps; ++s) {
+        if (!it.dual) move(k_slot, k_phase, 2 * team);
+        int v_slot = k_slot, v_phase = k_phase;
+        move(v_slot, v_phase, 1);
+        if (!wait(smem_u32(&c->q_full), n_items)) {
+            ok = false;
+            break;
+        }
+        // S = Q K^T of the team's next block (the P V that read this buffer's last P has completed)
+        auto qk = [&](bool last) {
+            tc_fence_after();
+            const uint32_t k_addr = ring + k_slot * L::kBlockBytes, d = t_s + 64 * (n_qk & 1);
+            const int np = last && ends_here ? last_pages : kPagesPerBlock;
+            const uint32_t idesc = kIdescBase | ((uint32_t)(np * kPage >> 3) << 17);
 #pragma unroll
-            for (int team = 0; team < 2; ++team) {
-                const int b = block_of(team, s);
-                if (!ok || b >= nblk) continue;
-                const int pos = 2 * (first + b) + 1, slot = pos & (kSlots - 1);
-                ok = wait(p_full + 8 * team, n_pv[team]);
-                // the first P V of an item overwrites O: the epilogues of the item before must have read both
-                if (ok && s == 0 && team == 0 && n_items > 0) ok = wait(smem_u32(&c->o_free), n_items - 1);
-                if (ok) ok = wait(kv_full + 8 * slot, pos / kSlots);
-                if (!ok) continue;
-                tc_fence_after();
-                if (elect_one()) {
-                    const int np = pages_of_block(it.len, it.b0 + b);
-                    const uint64_t dv = desc_mnmajor(smem_u32(smem + L::kRing + slot * L::kBlockBytes));
-                    const uint32_t d = tmem + kColO + DH * team, p = tmem + 128 * team;
-                    if (np == kPagesPerBlock) {
+            for (int half = 0; half < DH / 64; ++half) {
+                const uint64_t dq = desc_kmajor(q_tile + half * kTileRows * 128, 1024);
+                const uint64_t dk = DH == 128 ? desc_kmajor(k_addr + half * 1024, 2048) : desc_kmajor(k_addr, 1024);
 #pragma unroll
-                        for (int j = 0; j < kPagesPerBlock; ++j) tc_mma_ts(d, p + 8 * j, dv + (L::kPageBytes >> 4) * j, kIdescPV, (s | j) ? 1u : 0u);
-                    } else {
-                        for (int j = 0; j < np; ++j) tc_mma_ts(d, p + 8 * j, dv + (L::kPageBytes >> 4) * j, kIdescPV, (s | j) ? 1u : 0u);
-                    }
-                    if (!it.dual || team == 1) tc_commit(kv_empty + 8 * slot);
-                    tc_commit(pv_done + 8 * team);
-                    if (it.dual && s == steps - 1) tc_commit(o_full + 8 * team);
-                }
-                __syncwarp();
-                ++n_pv[team];
-                if (block_of(team, s + 1) < nblk) ok = qk(team, block_of(team, s + 1));
+                for (int ks = 0; ks < 4; ++ks) tc_mma_ss(d, dq + 2 * ks, dk + 2 * ks, idesc, (half | ks) ? 1u : 0u);
             }
+            tc_commit(s_full + 8 * (n_qk & 1));
+            if (last) tc_commit(smem_u32(&c->q_free));
+            ++n_qk;
+            move(k_slot, k_phase, ahead);
+        };
+        for (int s = 0; ok && s < 2 && s < steps; ++s)
+            if ((ok = wait(kv_full + 8 * k_slot, k_phase))) qk(s == steps - 1);
+        for (int s = 0; ok && s < steps; ++s) {
+            // O += P V; the first of an item overwrites O: the epilogues of the item before must have read it
+            if (!wait2(kv_full + 8 * v_slot, v_phase, p_full + 8 * (n_pv & 1), n_pv >> 1) ||
+                (s == 0 && n_items > 0 && !wait(smem_u32(&c->o_free), n_items - 1))) {
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            const uint64_t dv = desc_mnmajor(ring + v_slot * L::kBlockBytes);
+            const uint32_t p = t_s + 64 * (n_pv & 1);
+            const int np = s == steps - 1 && ends_here ? last_pages : kPagesPerBlock;
+            if (np == kPagesPerBlock) {
+#pragma unroll
+                for (int j = 0; j < kPagesPerBlock; ++j) tc_mma_ts(t_o, p + 8 * j, dv + (L::kPageBytes >> 4) * j, kIdescPV, (s || j) ? 1u : 0u);
+            } else {
+                for (int j = 0; j < np; ++j) tc_mma_ts(t_o, p + 8 * j, dv + (L::kPageBytes >> 4) * j, kIdescPV, (s || j) ? 1u : 0u);
+            }
+            tc_commit(pv_done);
+            const bool more = s + 2 < steps;
+            if (!(more ? wait2(pv_done, n_pv, kv_full + 8 * k_slot, k_phase) : wait(pv_done, n_pv))) {
+                ok = false;
+                break;
+            }
+            mbar_arrive(kv_empty + 8 * v_slot);
+            if (!it.dual) mbar_arrive(kv_empty + 8 * v_slot);     // (a slot waits for two arrivals)
+            ++n_pv;
+            move(v_slot, v_phase, ahead);
+            if (more) qk(s + 2 == steps - 1);
         }
         if (!ok) break;
-        if (!it.dual && elect_one()) {
-            tc_commit(o_full);
-            tc_commit(o_full + 8);
-        }
-        __syncwarp();
-        first += nblk;
+        if (steps == 0) tc_commit(smem_u32(&c->q_free));                      // (a single's second team may have no block)
+        tc_commit(o_full);
+        const int pos = base + 2 * nblk;
+        base = pos % kSlots;
+        base_phase ^= (pos / kSlots) & 1;
         ++n_items;
     }
     if (!ok) {
         atomicExch(a.status, DCUT_DEV_ATTN_WAIT_TIMEOUT);
         c->abort = 1;
-        if (elect_one()) tc_commit(smem_u32(&c->drain));          // the MMAs issued so far end before tensor memory is freed
-        __syncwarp();
-        mbar_wait(smem_u32(&c->drain), 0, nullptr);
+        tc_commit(smem_u32(&c->drain) + 8 * team);                            // the MMAs issued so far end before tensor memory is freed
+        mbar_wait(smem_u32(&c->drain) + 8 * team, 0, nullptr);
     }
+}
+
+// A softmax thread's steps over an item: its team's blocks of the piece, one after the other.  Not inlined: the loop then
+// has the registers to itself (64 scores, 32 words of P), and what the caller keeps for the epilogue is saved once per item.
+struct Steps {
+    uint32_t t_s, t_o;            // this lane's S / P buffers and O in tensor memory
+    uint32_t s_full, p_full, pv_done, kv_full, kv_empty;
+    int steps, last_cols;         // blocks; columns of the last of them (kBlock unless the prefix ends in it)
+    int n;                        // the team's steps before these
+    int pos, ahead;               // ring position of the first K block, positions from one of the team's blocks to the next
+    int live;                     // some of this warp's rows exist
+    int releases;                 // arrivals this lane owes the ring for every K block: 0, 1, or 2 (a single's only reader)
+    float cs;
+    const volatile int* abort_flag;
+};
+template <int DH>
+__device__ __noinline__ bool softmax_steps(const Steps p, unsigned char* smem_ring, float* m_out, float* l_out) {
+    constexpr int kPageBytes = Smem<DH>::kPageBytes;
+    const int lane = threadIdx.x & 31;
+    auto warp_wait = [&](uint32_t bar, int parity) {              // one lane polls
+        return __any_sync(0xffffffffu, lane == 0 && mbar_wait(bar, parity, p.abort_flag));
+    };
+    auto warp_arrive = [&](uint32_t bar) {                        // one arrival for the warp's 32
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+    };
+    float m_run = -INFINITY, l_run = 0.0f;
+    int n = p.n, pos = p.pos;
+    bool s_over = false;                                          // (lane 0) the next S is known to be there
+#pragma unroll 1
+    for (int s = 0; s < p.steps; ++s, ++n, pos += p.ahead) {
+        const uint32_t t_s = p.t_s + 64 * (n & 1), p_bar = p.p_full + 8 * (n & 1);
+        if (!__any_sync(0xffffffffu, s_over) && !warp_wait(p.s_full + 8 * (n & 1), (n >> 1) & 1)) return false;
+        s_over = false;
+        // (a committed S: K has been read)
+        if (p.releases > 0) mbar_arrive(p.kv_empty + 8 * (pos & (kSlots - 1)));
+        if (p.releases > 1) mbar_arrive(p.kv_empty + 8 * (pos & (kSlots - 1)));
+        if (s == p.steps - 1 && p.last_cols < kBlock) {
+            if (p.last_cols & (kPage - 1)) {
+                // The prefix ends inside this block's last page.  What lies behind it has weight 0, but 0 x NaN is NaN: the
+                // V rows of the unused slots are cleared before the MMA reads them (in a dual by both teams, each for its own).
+                const int slot = (pos + 1) & (kSlots - 1);
+                if (!warp_wait(p.kv_full + 8 * slot, ((pos + 1) / kSlots) & 1)) return false;
+                unsigned char* page = smem_ring + slot * Smem<DH>::kBlockBytes + (p.last_cols / kPage) * kPageBytes;
+                const int r0 = p.last_cols & (kPage - 1), chunks = (kPage - r0) * 8;       // 16-byte chunks of a 64-element half
+                for (int i = threadIdx.x & (kTeamThreads - 1); i < chunks * (DH / 64); i += kTeamThreads) {
+                    const int half = i / chunks, rest = i - half * chunks;
+                    *reinterpret_cast<uint4*>(page + half * (kPage * 128) + r0 * 128 + rest * 16) = make_uint4(0, 0, 0, 0);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            // the columns behind the prefix become -inf, in tensor memory: the common path has one version of the scores
+            tc_fence_after();
+#pragma unroll 1
+            for (int cc = 0; cc < kBlock; cc += 16) {
+                uint32_t x[16];
+                tc_ld16(t_s + cc, x);
+                tc_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = cc + e < p.last_cols ? x[e] : 0xff800000u;
+                tc_st16(t_s + cc, x);
+            }
+            tc_wait_st();
+        }
+        if (!p.live) {                                            // P keeps what it holds
+            warp_arrive(p_bar);
+            continue;
+        }
+        tc_fence_after();
+        uint32_t sr[kBlock];
+        tc_ld32(t_s, sr);
+        tc_ld32(t_s + 32, sr + 32);
+        tc_wait_ld();
+        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < kBlock; e += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mx4[k] = fmax3(mx4[k], __uint_as_float(sr[e + k]), __uint_as_float(sr[e + 4 + k]));
+        const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
+        const bool grows = mx > m_run && (m_run == -INFINITY || (mx - m_run) * p.cs > kRescaleLog2);
+        if (__any_sync(0xffffffffu, grows)) {
+            const float alpha = grows ? fast_exp2((m_run - mx) * p.cs) : 1.0f;
+            if (grows) m_run = mx;
+            l_run *= alpha;
+            if (s > 0) {
+                if (!warp_wait(p.pv_done, (n - 1) & 1)) return false;              // the team's last P V: O is at rest
+                tc_fence_after();
+#pragma unroll 1
+                for (int cc = 0; cc < DH; cc += 16) {             // (S is in registers: no more of O at once)
+                    uint32_t o[16];
+                    tc_ld16(p.t_o + cc, o);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+                    tc_st16(p.t_o + cc, o);
+                }
+                tc_wait_st();
+            }
+        }
+        const float cs = p.cs, mc = (m_run == -INFINITY ? 0.0f : m_run) * cs;
+        float sum4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        uint32_t pw[kBlock / 2];
+#pragma unroll
+        for (int e = 0; e < kBlock / 2; ++e) {
+            const float p0 = fast_exp2(fmaf(__uint_as_float(sr[2 * e]), cs, -mc)), p1 = fast_exp2(fmaf(__uint_as_float(sr[2 * e + 1]), cs, -mc));
+            sum4[(2 * e) & 3] += p0;
+            sum4[(2 * e + 1) & 3] += p1;
+            pw[e] = pack_bf16(p0, p1);
+        }
+        tc_st32(t_s, pw);                                         // P over the first half of S
+        // (asked for now, read at the next step's beginning: the answer takes more than 100 cycles)
+        s_over = lane == 0 && s + 1 < p.steps && mbar_test(p.s_full + 8 * ((n + 1) & 1), ((n + 1) >> 1) & 1);
+        l_run += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+        tc_wait_st();
+        tc_fence_before();
+        warp_arrive(p_bar);
+    }
+    *m_out = m_run;
+    *l_out = l_run;
+    return true;
 }
 
 template <int DH>
@@ -410,132 +540,66 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
     const int R = quarter * 32 + lane;                            // tensor-memory lane = row of the tile
     const int gs = a.group_size, tpt = tile_tokens(gs), row_tok = R / gs, row_head = R - row_tok * gs;
     const uint32_t lanes = c->tmem_base + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t t_s = lanes + 128 * team, t_o = lanes + kColO + DH * team, t_oo = lanes + kColO + DH * (team ^ 1);
-    const uint32_t s_full = smem_u32(c->s_full) + 8 * team, p_full = smem_u32(c->p_full) + 8 * team, o_full = smem_u32(c->o_full) + 8 * team;
+    const uint32_t t_o = lanes + 128 * team, t_oo = lanes + 128 * (team ^ 1);
+    const uint32_t o_full = smem_u32(c->o_full) + 8 * team;
     float* stage = reinterpret_cast<float*>(smem + L::kStage + (warp - 4) * kStageBytes);
     const float cs = a.scale_log2;
     Item it;
     int n_items = 0, n_s = 0, n_x = 0, first = 0;
     bool failed = false;
+    auto warp_wait = [&](uint32_t bar, int parity) { return __any_sync(0xffffffffu, lane == 0 && mbar_wait(bar, parity, &c->abort)); };
+    auto warp_arrive = [&](uint32_t bar) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+    };
     while (next_item(w, a.groups, &it)) {
         const int nblk = it.b1 - it.b0, tile = it.dual ? team : 0;
         const int tok = tile * tpt + row_tok;
         const bool valid = row_tok < tpt && tok < it.tokens;
         const bool live = __any_sync(0xffffffffu, valid);
         float m_run = -INFINITY, l_run = 0.0f;
-        for (int s = 0;; ++s) {
-            const int b = it.dual ? s : 2 * s + team;
-            if (b >= nblk) break;
-            failed = !mbar_wait(s_full, n_s & 1, &c->abort);
-            if (__any_sync(0xffffffffu, failed)) {
+        const int steps = it.dual ? nblk : (nblk + 1 - team) >> 1;
+        if (steps > 0) {
+            Steps p;
+            p.t_s = lanes + kColS + 128 * team;
+            p.t_o = t_o;
+            p.s_full = smem_u32(c->s_full[team]);
+            p.p_full = smem_u32(c->p_full[team]);
+            p.pv_done = smem_u32(c->pv_done) + 8 * team;
+            p.kv_full = smem_u32(c->kv_full);
+            p.kv_empty = smem_u32(c->kv_empty);
+            p.steps = steps;
+            p.last_cols = it.dual || ((nblk - 1) & 1) == team ? min(kBlock, it.len - (it.b1 - 1) * kBlock) : kBlock;
+            p.n = n_s;
+            p.pos = 2 * (first + (it.dual ? 0 : team));
+            p.ahead = it.dual ? 2 : 4;
+            p.live = live;
+            p.releases = quarter == 0 && lane == 0 ? (it.dual ? 1 : 2) : 0;
+            p.cs = cs;
+            p.abort_flag = &c->abort;
+            if (!softmax_steps<DH>(p, smem + L::kRing, &m_run, &l_run)) {
                 failed = true;
                 break;
             }
-            ++n_s;
-            const int ncols = min(kBlock, it.len - (it.b0 + b) * kBlock);
-            if ((ncols & (kPage - 1)) && (team == 0 || !it.dual)) {
-                // The prefix ends inside this block's last page.  What lies behind it has weight 0, but 0 x NaN is NaN: the
-                // V rows of the unused slots are cleared before the MMA reads them (in a dual, team 0's P V comes first).
-                const int pos = 2 * (first + b) + 1, slot = pos & (kSlots - 1);
-                failed = !mbar_wait(smem_u32(c->kv_full) + 8 * slot, (pos / kSlots) & 1, &c->abort);
-                if (__any_sync(0xffffffffu, failed)) {
-                    failed = true;
-                    break;
-                }
-                unsigned char* page = smem + L::kRing + slot * L::kBlockBytes + (ncols / kPage) * L::kPageBytes;
-                const int r0 = ncols & (kPage - 1), n = (kPage - r0) * 8;       // 16-byte chunks of a 64-element half
-                for (int i = threadIdx.x - 128 - kTeamThreads * team; i < n * (DH / 64); i += kTeamThreads) {
-                    const int half = i / n, rest = i - half * n;
-                    *reinterpret_cast<uint4*>(page + half * (kPage * 128) + r0 * 128 + rest * 16) = make_uint4(0, 0, 0, 0);
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            }
-            if (!live) {                                          // none of this warp's rows exists: P keeps what it holds
-                mbar_arrive(p_full);
-                continue;
-            }
-            uint32_t sr[kBlock];
-            tc_fence_after();
-#pragma unroll
-            for (int e = 0; e < kBlock; e += 32) tc_ld32(t_s + e, sr + e);
-            tc_wait_ld();
-            if (ncols < kBlock) {
-#pragma unroll
-                for (int e = 0; e < kBlock; ++e) sr[e] = e < ncols ? sr[e] : 0xff800000u;
-            }
-            float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int e = 0; e < kBlock; e += 8)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mx4[k] = fmax3(mx4[k], __uint_as_float(sr[e + k]), __uint_as_float(sr[e + 4 + k]));
-            const float mx = fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
-            float alpha = 1.0f;
-            bool moved = false;
-            if (mx > m_run && (m_run == -INFINITY || (mx - m_run) * cs > kRescaleLog2)) {
-                alpha = fast_exp2((m_run - mx) * cs);
-                m_run = mx;
-                l_run *= alpha;
-                moved = s > 0;
-            }
-            if (__any_sync(0xffffffffu, moved)) {
-                // (this S was issued after the team's last P V had completed: O is at rest)
-#pragma unroll 1
-                for (int cc = 0; cc < DH; cc += 32) {
-                    uint32_t o[32];
-                    tc_ld32(t_o + cc, o);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                    tc_st32(t_o + cc, o);
-                }
-                tc_wait_st();
-            }
-            const float mc = (m_run == -INFINITY ? 0.0f : m_run) * cs;
-            const unsigned long long cs2 = pack_f32x2(cs, cs), nmc2 = pack_f32x2(-mc, -mc);
-            unsigned long long sum2[2] = {0ull, 0ull};
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t pw[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    float x0, x1;
-                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sr[64 * h + 2 * e]), __uint_as_float(sr[64 * h + 2 * e + 1])), cs2, nmc2), x0, x1);
-                    const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-                    sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(p0, p1));
-                    pw[e] = pack_bf16(p0, p1);
-                }
-                tc_st32(t_s + 32 * h, pw);
-            }
-            {
-                float s0, s1, s2, s3;
-                unpack_f32x2(sum2[0], s0, s1);
-                unpack_f32x2(sum2[1], s2, s3);
-                l_run += (s0 + s1) + (s2 + s3);
-            }
-            tc_wait_st();
-            tc_fence_before();
-            mbar_arrive(p_full);
+            n_s += steps;
         }
-        if (failed) break;
 
         // ---------------------------------------------------------------- epilogue
         const bool has = it.blocks > 0, whole = is_whole(it);
         float m_o = -INFINITY, l_o = 0.0f;                        // the other team's part of a single's row
         if (has) {
-            failed = !mbar_wait(o_full, n_items & 1, &c->abort);
+            failed = !warp_wait(o_full, n_items & 1);
+            if (!it.dual && !failed) failed = !warp_wait(smem_u32(c->o_full) + 8 * (team ^ 1), n_items & 1);
             if (!it.dual && !failed) {
                 c->xm[team][R] = m_run;
                 c->xl[team][R] = l_run;
-                mbar_arrive(smem_u32(&c->x_ready));
-                failed = !mbar_wait(smem_u32(&c->x_ready), n_x & 1, &c->abort);
+                warp_arrive(smem_u32(&c->x_ready));
+                failed = !warp_wait(smem_u32(&c->x_ready), n_x & 1);
                 ++n_x;
                 m_o = c->xm[team ^ 1][R];
                 l_o = c->xl[team ^ 1][R];
             }
-            if (__any_sync(0xffffffffu, failed)) {
-                failed = true;
-                break;
-            }
+            if (failed) break;
             tc_fence_after();
         }
         const int orow = valid ? (it.q0 + tok) * a.n_q_heads + it.h * gs + row_head : 0;
@@ -557,20 +621,26 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
         if (!whole && valid && (it.dual || team == 0)) a.part_lse[prow0 + R] = lp * kLn2;
         const int c0 = it.dual ? 0 : team * (DH / 2), c1 = it.dual ? DH : c0 + DH / 2;
         const int v = lane & 3, rsub = lane >> 2;                 // this lane's vector of four columns, its row of eight
-#pragma unroll 1
-        for (int cc = c0; cc < c1 && live; cc += 16) {
-            // 16 columns of the warp's 32 rows through shared memory, so that global memory sees 64 bytes of a row at a time
-            float4 own[4];
-            int row[4];
-            bool ok[4];
+        // 16 columns of the warp's 32 rows at a time go through shared memory, so that global memory sees 64 bytes of a row
+        // at once; the own part's columns are fetched two chunks ahead
+        int row[4];
+        bool row_ok[4];
+        float f_row[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 8 * i + rsub;
+            row[i] = __shfl_sync(0xffffffffu, orow, r);
+            row_ok[i] = __shfl_sync(0xffffffffu, (int)valid, r);
+            f_row[i] = __shfl_sync(0xffffffffu, f_own, r);
+        }
+        auto fetch = [&](float4 (&own)[4], int cc) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int r = 8 * i + rsub;
-                row[i] = __shfl_sync(0xffffffffu, orow, r);
-                ok[i] = __shfl_sync(0xffffffffu, (int)valid, r);
                 own[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (whole && ok[i]) own[i] = *reinterpret_cast<const float4*>(a.own_o + (size_t)row[i] * DH + cc + 4 * v);
+                if (whole && row_ok[i] && cc < c1) own[i] = *reinterpret_cast<const float4*>(a.own_o + (size_t)row[i] * DH + cc + 4 * v);
             }
+        };
+        auto chunk = [&](const float4 (&own)[4], int cc) {
             if (has) {
                 uint32_t os[16], oo[16];
                 tc_ld16(t_o + cc, os);
@@ -592,20 +662,32 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
                 const int r = 8 * i + rsub;
                 float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (has) y = *reinterpret_cast<const float4*>(stage + r * 16 + ((v ^ ((r >> 1) & 3)) << 2));
-                const float f = __shfl_sync(0xffffffffu, f_own, r);
-                if (!ok[i]) continue;
+                if (!row_ok[i]) continue;
                 if (whole) {
                     *reinterpret_cast<uint2*>(a.out + (size_t)row[i] * DH + cc + 4 * v) =
-                        make_uint2(pack_bf16(fmaf(own[i].x, f, y.x), fmaf(own[i].y, f, y.y)), pack_bf16(fmaf(own[i].z, f, y.z), fmaf(own[i].w, f, y.w)));
+                        make_uint2(pack_bf16(fmaf(own[i].x, f_row[i], y.x), fmaf(own[i].y, f_row[i], y.y)),
+                                   pack_bf16(fmaf(own[i].z, f_row[i], y.z), fmaf(own[i].w, f_row[i], y.w)));
                 } else {
                     *reinterpret_cast<float4*>(a.part_o + (prow0 + quarter * 32 + r) * DH + cc + 4 * v) = y;
                 }
             }
             __syncwarp();
+        };
+        if (live) {
+            float4 own0[4], own1[4];
+            fetch(own0, c0);
+            fetch(own1, c0 + 16);
+#pragma unroll 1
+            for (int cc = c0; cc < c1; cc += 32) {                // (32 divides a team's share of the columns)
+                chunk(own0, cc);
+                fetch(own0, cc + 32);
+                chunk(own1, cc + 16);
+                fetch(own1, cc + 48);
+            }
         }
         if (has) {
             tc_fence_before();
-            mbar_arrive(smem_u32(&c->o_free));
+            warp_arrive(smem_u32(&c->o_free));
             first += nblk;
             ++n_items;
         }
@@ -627,19 +709,22 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     if (threadIdx.x == 0) {
         for (int s = 0; s < kSlots; ++s) {
             mbar_init(smem_u32(&c->kv_full[s]), 1);
-            mbar_init(smem_u32(&c->kv_empty[s]), 1);
+            mbar_init(smem_u32(&c->kv_empty[s]), 2);
         }
         mbar_init(smem_u32(&c->q_full), 1);
-        mbar_init(smem_u32(&c->q_free), 1);
+        mbar_init(smem_u32(&c->q_free), 2);
         for (int t = 0; t < 2; ++t) {
-            mbar_init(smem_u32(&c->s_full[t]), 1);
-            mbar_init(smem_u32(&c->p_full[t]), kTeamThreads);
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(smem_u32(&c->s_full[t][b]), 1);
+                mbar_init(smem_u32(&c->p_full[t][b]), kTeamThreads / 32);
+            }
             mbar_init(smem_u32(&c->pv_done[t]), 1);
             mbar_init(smem_u32(&c->o_full[t]), 1);
+            mbar_init(smem_u32(&c->drain[t]), 1);
+
         }
-        mbar_init(smem_u32(&c->o_free), 2 * kTeamThreads);
-        mbar_init(smem_u32(&c->x_ready), 2 * kTeamThreads);
-        mbar_init(smem_u32(&c->drain), 1);
+        mbar_init(smem_u32(&c->o_free), 2 * kTeamThreads / 32);
+        mbar_init(smem_u32(&c->x_ready), 2 * kTeamThreads / 32);
         c->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -658,14 +743,10 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
     w.G = a.n_groups;
     w.group_size = a.group_size;
     w.n_kv_heads = a.n_kv_heads;
-    if (warp < 4) {                        // (a softmax thread holds a row's 128 scores)
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsControl));
-        if (warp == 0) produce<DH>(q_map, k_map, v_map, a, smem, c, w);
-        else if (warp == 1) issue<DH>(a, smem, c, w);
-    } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-        softmax<DH>(a, smem, c, w);
-    }
+    if (warp == 0) produce<DH>(q_map, k_map, v_map, a, smem, c, w);
+    else if (warp == 1 || warp == 2) {
+        if (elect_one()) issue<DH>(a, smem, c, w, warp - 1);
+    } else if (warp >= 4) softmax<DH>(a, smem, c, w);
     __syncwarp();
     dcut_pdl_launch_dependents();
     tc_fence_before();

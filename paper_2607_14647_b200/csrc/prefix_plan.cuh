@@ -4,7 +4,7 @@
 // A group of requests with a shared prefix is a matrix of query rows per kv head: its tokens x the q heads of the kv
 // head, row R = token * group_size + head.  A tile is floor(128 / group_size) whole tokens (at most 128 rows, the lanes
 // of tensor memory); a unit is two tiles (dual: both see every key block) or the last odd tile (single: its key blocks
-// are dealt to the CTA's two softmax teams in turn).  An item is (group, kv head, unit): `blocks` blocks of 128 keys.
+// are dealt to the CTA's two softmax teams in turn).  An item is (group, kv head, unit): `blocks` blocks of kBlock keys.
 // The items of a call, in this order, are a stream of known cost that is cut into one segment of equal cost per CTA; a
 // cut may fall inside an item, between two key blocks.  An item cut m times is computed in m + 1 pieces: the first in
 // slot 2 s + 1 of the segment s it begins in, every other in slot 2 s of its segment.
@@ -18,7 +18,7 @@
 
 namespace dcut_prefix {
 
-constexpr int kBlock = 128;           // keys per block
+constexpr int kBlock = 64;            // keys per block: four pages (why 64: prefix_attn.cu)
 constexpr int kTileRows = 128;
 constexpr int kSlotRows = 2 * kTileRows;
 constexpr int kMaxSegs = 256;
