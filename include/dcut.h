@@ -465,6 +465,38 @@ dcut_status dcut_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_cache, 
                              int T_cap, const dcut_prefix_groups* groups, float scale, void* out, float* lse, void* stream);
 
 /*
+ * A linear layer over the packed rows, with everything that follows it in the epilogue (dcut_gemm_bf16 has no bias, one
+ * activation, and shapes of its own decoder layer):
+ *   out[r, :] = residual[r, :] + act(a[r, :] . w^T + bias)                                    w2 NULL
+ *   out[r, :] = residual[r, :] + act(a[r, :] . w^T + bias) * (a[r, :] . w2^T + bias2)         gated
+ * for rows r < cu_q[B] (rows from there on are not touched).  bf16 in, fp32 accumulation, bias, activation, gate and residual
+ * in fp32, one rounding to bf16.  Any N, K >= 1.
+ *   act: none; relu; gelu = x Phi(x); gelu_tanh = x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2; silu = x / (1 + e^-x).
+ * DEVICE: a [T_cap rows readable, K] with lda elements from row to row, w and w2 [N, K] with ldw; both strides multiples of 8
+ * and >= K, bases 16-byte aligned.  bias, bias2 [N] or NULL; residual [T, N] with ldr or NULL; out [T, N] with ldo (>= N; any
+ * alignment: 16-byte aligned rows are stored in vectors).  out may be the residual itself (same stride); it must not
+ * overlap a or the weights.  The struct is HOST memory, read during the call.  Needs a context with attention shapes;
+ * N, K and T_cap are not bound by dcut_limits.
+ */
+typedef enum { DCUT_ACT_NONE = 0, DCUT_ACT_RELU = 1, DCUT_ACT_GELU = 2, DCUT_ACT_GELU_TANH = 3, DCUT_ACT_SILU = 4 } dcut_act;
+typedef struct {
+    const void* a;
+    long long lda;
+    const void* w;
+    const void* w2;
+    long long ldw;
+    const void* bias;
+    const void* bias2;
+    const void* residual;
+    long long ldr;
+    void* out;
+    long long ldo;
+    int N, K;
+    int act;                   /* dcut_act */
+} dcut_linear_args;
+dcut_status dcut_linear(dcut_ctx* ctx, const dcut_linear_args* args, const int* cu_q, int B, int T_cap, void* stream);
+
+/*
  * dcut_accept without any allocation.  (The paper has no counterpart: this entry point exists for
  * the way the library gets embedded, not for the method.)
  *
@@ -554,7 +586,7 @@ dcut_status dcut_verify_step_host(dcut_ctx* ctx, const dcut_host_step* step, voi
  * (rows at or past T_cap were left out: nothing outside the caller's T_cap rows is read or written), 8 =
  * dcut_rope_append met a token whose request or position has no place in the block table (it was left out), 9 =
  * dcut_prefix_attn met groups that do not cover the batch or a prefix that does not fit (nothing was written; 7 there: a
- * cu_q that does not pack the batch). */
+ * cu_q that does not pack the batch), 10 = dcut_linear met a cu_q[B] above T_cap (rows from T_cap on were left out). */
 dcut_status dcut_poll_device_status(dcut_ctx* ctx, int* code, void* stream);
 
 #ifdef __cplusplus

@@ -33,7 +33,7 @@ EXPORTS = ["dcut_create", "dcut_destroy", "dcut_last_error", "dcut_set_cost_dens
            "dcut_enable_plan_in_select", "dcut_cost_grid_create", "dcut_cost_grid_destroy", "dcut_cost_grid_budget",
            "dcut_cost_grid_record", "dcut_cost_grid_get", "dcut_cost_grid_nearest", "dcut_cost_grid_buckets",
            "dcut_set_cost_from_grid", "dcut_layer_attn_part", "dcut_layer_mlp_part", "dcut_residual_add",
-           "dcut_rope_append", "dcut_enable_prefix_attn", "dcut_prefix_attn"]
+           "dcut_rope_append", "dcut_enable_prefix_attn", "dcut_prefix_attn", "dcut_linear"]
 
 
 class Limits(C.Structure):
@@ -123,6 +123,13 @@ class Rope(C.Structure):
 _lib.dcut_rope_append.argtypes = [_vp, C.POINTER(Qkv), C.POINTER(Rope), _vp, _vp, _vp, _ll, _vp, _i, C.POINTER(PrefixGroupsRec),
                                   _vp, _i, _vp, _vp, _i, _vp]
 
+class LinearArgs(C.Structure):
+    _fields_ = [("a", _vp), ("lda", _ll), ("w", _vp), ("w2", _vp), ("ldw", _ll), ("bias", _vp), ("bias2", _vp), ("residual", _vp), ("ldr", _ll),
+                ("out", _vp), ("ldo", _ll), ("N", _i), ("K", _i), ("act", _i)]
+
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+_lib.dcut_linear.argtypes = [_vp, C.POINTER(LinearArgs), _vp, _i, _i, _vp]
 _lib.dcut_enable_prefix_attn.argtypes = [_vp, _i]
 _lib.dcut_prefix_attn.argtypes = [_vp, _vp, _vp, _vp, _ll, _vp, _i, _vp, _vp, _i, _i, C.POINTER(PrefixGroupsRec), _f, _vp, _vp, _vp]
 
@@ -158,6 +165,15 @@ def _heads(t: Optional[torch.Tensor], n_heads: int, head_dim: int):
     assert t.dim() == 3 and t.shape[1] == n_heads and t.shape[2] == head_dim and t.stride(2) == 1, \
         f"expected [tokens, {n_heads}, {head_dim}] with dense heads, got {tuple(t.shape)} with strides {t.stride()}"
     return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _rows(t: Optional[torch.Tensor]):
+    """(pointer, row stride) of a bf16 [rows, columns] view whose rows are dense."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), \
+        "expected a CUDA bf16 matrix with dense rows"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8     # (one row: its stride says nothing)
 
 
 def rope_inv_freq(theta: float, rotary_dim: int, device="cuda") -> torch.Tensor:
@@ -544,6 +560,23 @@ class Context:
                                           k_cache.shape[0], _ptr(block_table, torch.int32), block_table.shape[1], _ptr(ctx_lens, torch.int32),
                                           _ptr(cu_q, torch.int32), ctx_lens.shape[0], T_cap, C.byref(groups.rec), float(scale),
                                           _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), _stream()))
+        return out
+
+    def linear(self, a, w, cu_q, T_cap: int, out=None, bias=None, act: str = "none", w2=None, bias2=None, residual=None):
+        """dcut_linear: out = residual + act(a w^T + bias) [* (a w2^T + bias2)] over the packed rows; a, w, residual and out may
+        be views with padded rows (a and w: a multiple of 8 elements apart)."""
+        N, K = w.shape
+        assert a.shape[1] == K and a.shape[0] >= T_cap, "a must be [T_cap rows, K]"
+        assert w2 is None or (w2.shape == w.shape and _rows(w2)[1] == _rows(w)[1]), "w2 must have the shape and strides of w"
+        assert all(t is None or t.shape == (N,) for t in (bias, bias2))
+        assert residual is None or (residual.shape[0] >= T_cap and residual.shape[1] == N)
+        if out is None:
+            out = torch.empty((T_cap, N), dtype=torch.bfloat16, device=a.device)
+        assert out.shape[0] >= T_cap and out.shape[1] == N
+        (ap, lda), (wp, ldw), (rp, ldr), (op, ldo) = _rows(a), _rows(w), _rows(residual), _rows(out)
+        l = LinearArgs(ap, lda, wp, _rows(w2)[0], ldw, _ptr(bias, torch.bfloat16), _ptr(bias2, torch.bfloat16), rp, ldr, op, ldo, N, K,
+                       ACTIVATIONS[act])
+        self._check(_lib.dcut_linear(self._h, C.byref(l), _ptr(cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, _stream()))
         return out
 
     def make_model(self, layers: list, embed, g_final, w_lm, k_caches: list, v_caches: list, rms_eps: float = 1e-6,

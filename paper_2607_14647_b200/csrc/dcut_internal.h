@@ -20,6 +20,7 @@
 #define DCUT_DEV_BAD_TOKEN 6            // dcut_model_verify: a token id outside [0, vocab)
 #define DCUT_DEV_BAD_CU_Q 7             // acceptance: cu_q is not a packing of B requests of 1..gamma+1 rows within T_cap
 #define DCUT_DEV_BAD_APPEND 8           // dcut_rope_append: a token's request or position has no place in the block table
+#define DCUT_DEV_BAD_ROWS 10            // dcut_linear: cu_q[B] above T_cap
 #define DCUT_DEV_BAD_GROUPS 9           // dcut_prefix_attn: the groups do not cover the batch, or a prefix does not fit its table or contexts
 
 // One row of the attention work table: a (request, row block of its query tile); it stands for n_kv_heads work items of
@@ -238,6 +239,7 @@ dcut_status dcut_enable_prefix(dcut_ctx* ctx, int max_groups);
 dcut_status dcut_launch_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, long long num_pages,
                                     const int* block_table, int block_table_stride, const int* ctx_lens, const int* cu_q, int B,
                                     int T_cap, const dcut_prefix_groups* groups, float scale, void* out, float* lse, cudaStream_t stream);
+dcut_status dcut_launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, const int* cu_q, int B, int T_cap, cudaStream_t stream);
 dcut_status dcut_launch_rope_append(dcut_ctx* ctx, const DcutRopeArgs& a, int T_cap, cudaStream_t stream);
 dcut_status dcut_launch_residual_add(dcut_ctx* ctx, const void* a, const void* b, void* out, int width, const int* cu_q, int B,
                                      int T_cap, cudaStream_t stream);

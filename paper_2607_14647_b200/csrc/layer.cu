@@ -14,7 +14,7 @@
 //                         are staged by TMA as 128-byte-swizzled K-major tiles (BK = 64); one elected lane issues the
 //                         MMAs and releases stages with tcgen05.commit; two accumulators in tensor memory let the four
 //                         epilogue warps (tcgen05.ld) work on one tile while the next is being multiplied.
-//                         Epilogues: plain bf16, + residual, SwiGLU (the B tile is 128 gate rows and the 128 matching
+//                         Epilogues: plain bf16, + residual, bias / activation / gate / residual (dcut_linear), SwiGLU (the B tile is 128 gate rows and the 128 matching
 //                         up rows, so silu(g) * u is formed in registers and the [T, 2I] intermediate never exists),
 //                         or row argmax (the LM head fused with acceptance: the logits are never stored).
 // M is ragged and known only on the device (T = cu_q[B]): grids are sized for T_cap, CTAs without work fall through,
@@ -40,7 +40,9 @@ constexpr int kMaxStages = 12;                 // a narrow tile's stage is small
 constexpr int kGemmSmem = kGemmStages * kGemmStageBytes + 1024 /* align */ + 512 /* two sets of barriers, tmem ptr */;
 constexpr int kWaitLimit = 1 << 22;
 
-enum GemmMode { kPlain = 0, kResidual = 1, kSwiGLU = 2, kArgmax = 3 };
+enum GemmMode { kPlain = 0, kResidual = 1, kSwiGLU = 2, kArgmax = 3, kLinear = 4, kLinearGated = 5 };
+__host__ __device__ constexpr bool is_gated(int mode) { return mode == kSwiGLU || mode == kLinearGated; }        // two weights share a tile
+__host__ __device__ constexpr bool may_split_k(int mode) { return mode == kPlain || mode == kResidual || mode == kLinear; }
 
 // Widths of the output tile that the one-SM mode may use: 256, 224, ..., 64 columns.  A narrower tile costs a little
 // efficiency per flop and buys more tiles, which is what a GEMM with fewer than one wave of 128 x 256 tiles needs
@@ -157,6 +159,11 @@ struct GemmArgs {
     const __nv_bfloat16* residual;   // [T, N_out] or null
     unsigned long long* row_key;     // kArgmax: one packed (ordered maximum, ~column) word per row
     int V;                           // kArgmax: live columns (rows of the weight)
+    const __nv_bfloat16 *bias, *bias2;   // kLinear*: [N_out] or null
+    long long ldo, ldr;              // kLinear*: elements from one row of out / residual to the next
+    int T_cap;                       // kLinear*: rows that out has
+    int act;                         // kLinear*: dcut_act
+    int vec;                         // kLinear*: 1: out, 2: residual, 4: bias and bias2 take 16-byte accesses at multiples of 8 columns
     int pairs;                       // launched as clusters of two CTAs: the pair mode may be chosen
     unsigned bn_mask;                // tile widths whose tensor maps were supplied (bit i: bn_of(i)); bit 0 always
     int force;                       // experiments: -1 = let gemm_plan choose, 0..6 = that width on one SM, 8..14 = on a pair
@@ -177,11 +184,99 @@ __device__ __forceinline__ const CUtensorMap* pick_map(const BMaps& s, int i) {
     }
 }
 
+// ------------------------------------------------------------------------------------------------ dcut_linear's epilogue
+
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, int n, bool vec, float (&x)[8]) {
+    if (vec && n >= 8) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[2 * j] = bf_lo(w[j]);
+            x[2 * j + 1] = bf_hi(w[j]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = j < n ? __bfloat162float(p[j]) : 0.0f;
+    }
+}
+__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }    // (exp overflows to inf: 0)
+__device__ __forceinline__ void activate8(int act, float (&x)[8]) {
+    if (act == DCUT_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = x[j] < 0.0f ? 0.0f : x[j];                        // (a NaN stays)
+    } else if (act == DCUT_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= 0.5f * erfcf(x[j] * -0.7071067811865476f);       // Phi(x) without cancellation
+    } else if (act == DCUT_ACT_GELU_TANH) {
+        // (1 + tanh u) / 2 = sigmoid(2 u), u = sqrt(2 / pi) (x + 0.044715 x^3)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= sigmoid(1.5957691216057308f * x[j] * fmaf(0.044715f * x[j], x[j], 1.0f));
+    } else if (act == DCUT_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= sigmoid(x[j]);
+    }
+}
+// x (and, gated, u): eight columns of a row as the MMAs left them.  Everything in fp32, one rounding at the store.
+template <bool GATED>
+__device__ __forceinline__ void linear_finish8(const GemmArgs& g, int row, int col, float (&x)[8], const float (&u)[8]) {
+    const int n = g.N_out - col;
+    float t[8];
+    if (g.bias) {
+        load8(g.bias + col, n, g.vec & 4, t);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] += t[j];
+    }
+    activate8(g.act, x);
+    if (GATED) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = 0.0f;
+        if (g.bias2) load8(g.bias2 + col, n, g.vec & 4, t);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] *= u[j] + t[j];
+    }
+    if (g.residual) {
+        load8(g.residual + (size_t)row * g.ldr + col, n, g.vec & 2, t);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] += t[j];
+    }
+    __nv_bfloat16* o = g.out + (size_t)row * g.ldo + col;
+    if ((g.vec & 1) && n >= 8) {
+        *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) o[j] = __float2bfloat16_rn(x[j]);
+    }
+}
+
 // Epilogue of one 128 x bn accumulator (this thread: tensor-memory lane = output row `row`), for every mode.  Columns
 // past N_out (a ragged last tile of a narrow width) were computed on zero weight rows and are not stored.
 template <int MODE>
 __device__ __forceinline__ void gemm_epilogue(const GemmArgs& g, int T, int row, int n_tile, uint32_t t_row, int bn) {
-    if (MODE == kSwiGLU) {
+    if (MODE == kLinear || MODE == kLinearGated) {
+        const int width = MODE == kLinearGated ? bn >> 1 : bn, col0 = n_tile * width;
+#pragma unroll 1
+        for (int c = 0; c < width; c += 32) {
+            uint32_t av[32], uv[32];
+            tc_ld32(t_row + c, av);
+            if (MODE == kLinearGated) tc_ld32(t_row + width + c, uv);
+            tc_wait_ld();
+            if (row < T) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                    if (col0 + c + e >= g.N_out) break;
+                    float x[8], u[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        x[j] = __uint_as_float(av[e + j]);
+                        u[j] = MODE == kLinearGated ? __uint_as_float(uv[e + j]) : 0.0f;
+                    }
+                    linear_finish8<MODE == kLinearGated>(g, row, col0 + c + e, x, u);
+                }
+            }
+        }
+    } else if (MODE == kSwiGLU) {
         const int half = bn >> 1, col0 = n_tile * half;
         __nv_bfloat16* orow = g.out + (size_t)row * g.N_out + col0;
 #pragma unroll 1
@@ -406,7 +501,12 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
     // everything above overlaps the previous kernel of the stream; nothing it wrote is read before this wait
     dcut_pdl_wait();
     dcut_pdl_launch_dependents();
-    const int T = g.cu_q[g.B];
+    int T_packed = g.cu_q[g.B];
+    if ((MODE == kLinear || MODE == kLinearGated) && T_packed > g.T_cap) {
+        T_packed = g.T_cap;
+        if (blockIdx.x == 0 && threadIdx.x == 0) atomicExch(g.status, DCUT_DEV_BAD_ROWS);
+    }
+    const int T = T_packed;
     // rows 64..127 of the A tile are not loaded when no row of them exists: they hold whatever shared memory held, and
     // the accumulator rows computed from them are never stored (one-SM and split modes; a pair always loads full boxes)
     const bool a_half = T <= BM / 2;
@@ -418,7 +518,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
     const bool pairs = plan_all >= kPlanPair && !split;
     const int plan = plan_all & 7;                                  // width index
     const int bn = bn_of(plan), half_rows = bn >> 1;                // tile width; a B tile is loaded as two halves
-    const int per = MODE == kSwiGLU ? half_rows : bn;               // output columns per tile
+    const int per = is_gated(MODE) ? half_rows : bn;                // output columns per tile
     const int n_tiles = (g.N_out + per - 1) / per;
     // one-SM and split modes: a stage is this tile's A and B bytes, and as many stages as fit the operand area (a
     // 64-wide tile at T <= 64 moves 8 KB of weights per stage: with four stages too few bytes were in flight per SM to
@@ -553,6 +653,13 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                             asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
                                          : "=f"(add[4 * v]), "=f"(add[4 * v + 1]), "=f"(add[4 * v + 2]), "=f"(add[4 * v + 3]) : "r"(src));
                         }
+                        if (MODE == kLinear) {
+                            float x[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) x[j] = rank ? add[j] + __uint_as_float(av[e + j]) : __uint_as_float(av[e + j]) + add[j];
+                            linear_finish8<false>(g, row, col0 + c + e, x, x);
+                            continue;
+                        }
                         uint4 res = make_uint4(0, 0, 0, 0);
                         if (MODE == kResidual) res = *reinterpret_cast<const uint4*>(rrow + c + e);
                         const uint32_t rw[4] = {res.x, res.y, res.z, res.w};
@@ -589,7 +696,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                         const uint32_t bar = full_bar + 8 * s;
                         mbar_arrive_expect_tx(bar, stage_tx);
                         tma_load_2d(a_dst, a_map1, kb * BK, m0, bar);
-                        if (MODE == kSwiGLU) {   // the gate rows, then the up rows of the same features
+                        if (is_gated(MODE)) {    // the gate rows, then the up rows of the same features
                             tma_load_2d(b_dst, b_map, kb * BK, n_tile * half_rows, bar);
                             tma_load_2d(b_dst + half_rows * BK * 2, b2_map, kb * BK, n_tile * half_rows, bar);
                         } else {                 // (weight rows past N read as zeros)
@@ -688,7 +795,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                         if (rank == 0) mbar_arrive_expect_tx(full_bar + 8 * s, pair_tx);
                         const uint32_t bar = lead_full + 8 * s;
                         tma_load_2d_pair(a_dst, &a_maps.full, kb * BK, m0, bar);
-                        if (MODE == kSwiGLU)      // the leader's half: 128 gate rows; the peer's: the 128 up rows of the same features
+                        if (is_gated(MODE))       // the leader's half: 128 gate rows; the peer's: the 128 up rows of the same features
                             tma_load_2d_pair(b_dst, rank == 0 ? b_map : b2_map, kb * BK, n_tile * half_rows, bar);
                         else
                             tma_load_2d_pair(b_dst, b_map, kb * BK, n_tile * bn + (int)rank * half_rows, bar);
@@ -875,9 +982,9 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 // K-major bf16 matrix [rows, cols] as a 2-D tensor map with a {64 columns, box_rows} box and 128-byte swizzle
-dcut_status make_kmajor_map(dcut_ctx* ctx, CUtensorMap* map, const void* base, long long rows, long long cols, int box_rows) {
+dcut_status make_kmajor_map(dcut_ctx* ctx, CUtensorMap* map, const void* base, long long rows, long long cols, int box_rows, long long ld = 0) {
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)cols * 2};
+    cuuint64_t strides[1] = {(cuuint64_t)(ld ? ld : cols) * 2};
     cuuint32_t box[2] = {BK, (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1, 1};
     CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(
@@ -904,10 +1011,9 @@ dcut_status make_weight_maps(dcut_ctx* ctx, BMaps* maps, const void* w, long lon
     return DCUT_OK;
 }
 
+// Fills in how a launch runs (GemmArgs::plan_by_m and what goes with it); returns its grid
 template <int MODE>
-dcut_status launch_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMaps& b2, int n_tiles,
-                        int T_cap, unsigned bn_mask, const GemmArgs& g, cudaStream_t stream) {
-    GemmArgs ga = g;
+int plan_gemm(dcut_ctx* ctx, int n_tiles, int T_cap, unsigned bn_mask, GemmArgs& ga) {
     ga.n_tiles = n_tiles;
     ga.bn_mask = bn_mask | 1u;
 
@@ -926,14 +1032,26 @@ dcut_status launch_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMa
         ga.pairs = ctx->ly_gemm_pair_mode;
         ga.force = ctx->ly_gemm_force;
         if (ga.force >= 0 && (ga.force > 22 || (ga.force & 7) == 7 || !((ga.bn_mask >> (ga.force & 7)) & 1) || (ga.force >= 8 && !ga.pairs) ||
-                              (ga.force >= 16 && !((MODE == kPlain || MODE == kResidual) && ga.K >= 2 * BK))))
+                              (ga.force >= 16 && !(may_split_k(MODE) && ga.K >= 2 * BK))))
             ga.force = -1;
         const int m_cap = (T_cap + BM - 1) / BM;   // no launch has more row blocks than that: the rest of the table repeats
         for (int m = 1; m <= kPlanRows; ++m)
             ga.plan_by_m[m - 1] = m > m_cap && m > 1 ? ga.plan_by_m[m - 2]
                                                     : (unsigned char)gemm_plan(m, ga.N_out, ga.bn_mask, ga.pairs != 0,
-                                                                               ga.pairs != 0 && (MODE == kPlain || MODE == kResidual) && ga.K >= 2 * BK,
-                                                                               ga.force, MODE == kSwiGLU, grid);
+                                                                               ga.pairs != 0 && may_split_k(MODE) && ga.K >= 2 * BK,
+                                                                               ga.force, is_gated(MODE), grid);
+        return grid;
+    }
+    for (int m = 1; m <= kPlanRows; ++m)
+        ga.plan_by_m[m - 1] = m > (T_cap + BM - 1) / BM && m > 1
+                                  ? ga.plan_by_m[m - 2]
+                                  : (unsigned char)gemm_plan(m, ga.N_out, ga.bn_mask, false, false, ga.force, is_gated(MODE), grid);
+    return grid;
+}
+
+template <int MODE>
+dcut_status launch_planned_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMaps& b2, int grid, const GemmArgs& ga, cudaStream_t stream) {
+    if (ctx->ly_gemm_pairs > 0) {
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim.x = 2;
@@ -950,12 +1068,38 @@ dcut_status launch_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMa
         lc.numAttrs = 2;
         return dcut_check_cuda(ctx, cudaLaunchKernelEx(&lc, gemm_tcgen05_kernel<MODE>, a, b, b2, ga), "launch gemm_tcgen05_kernel");
     }
-    for (int m = 1; m <= kPlanRows; ++m)
-        ga.plan_by_m[m - 1] = m > (T_cap + BM - 1) / BM && m > 1
-                                  ? ga.plan_by_m[m - 2]
-                                  : (unsigned char)gemm_plan(m, ga.N_out, ga.bn_mask, false, false, ga.force, MODE == kSwiGLU, grid);
     return dcut_check_cuda(ctx, dcut_launch_pdl(gemm_tcgen05_kernel<MODE>, dim3(grid), dim3(kGemmThreads), kGemmSmem, stream, a, b, b2, ga),
                            "launch gemm_tcgen05_kernel");
+}
+
+template <int MODE>
+dcut_status launch_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMaps& b2, int n_tiles,
+                        int T_cap, unsigned bn_mask, const GemmArgs& g, cudaStream_t stream) {
+    GemmArgs ga = g;
+    const int grid = plan_gemm<MODE>(ctx, n_tiles, T_cap, bn_mask, ga);
+    return launch_planned_gemm<MODE>(ctx, a, b, b2, grid, ga, stream);
+}
+
+// dcut_linear: any N and K (the tensor maps' zero fill completes the last tile and the last k-block), rows of any stride.
+// Encodes maps for the tile widths that the plan can pick only (about 0.3 us of host time each).
+template <int MODE>
+dcut_status launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, int T_cap, GemmArgs& g, cudaStream_t stream) {
+    const unsigned mask = (is_gated(MODE) ? ctx->ly_gemm_bn_mask & kBnMaskSwiGLU : ctx->ly_gemm_bn_mask) | 1u;
+    const int per = is_gated(MODE) ? BN / 2 : BN;
+    const int grid = plan_gemm<MODE>(ctx, (l->N + per - 1) / per, T_cap, mask, g);
+    unsigned used = 0;
+    for (int m = 0; m < kPlanRows && m <= (T_cap - 1) / BM; ++m) used |= 1u << (g.plan_by_m[m] & 7);
+    AMaps am;
+    BMaps bm = {}, b2m = {};
+    dcut_status st;
+    if ((st = make_kmajor_map(ctx, &am.full, l->a, T_cap, l->K, BM, l->lda)) != DCUT_OK) return st;
+    if ((st = make_kmajor_map(ctx, &am.half, l->a, T_cap, l->K, BM / 2, l->lda)) != DCUT_OK) return st;
+    for (int i = 0; i < kNumBn; ++i) {
+        if (!((used >> i) & 1)) continue;
+        if ((st = make_kmajor_map(ctx, &bm.m[i], l->w, l->N, l->K, bn_of(i) / 2, l->ldw)) != DCUT_OK) return st;
+        if (is_gated(MODE) && (st = make_kmajor_map(ctx, &b2m.m[i], l->w2, l->N, l->K, bn_of(i) / 2, l->ldw)) != DCUT_OK) return st;
+    }
+    return launch_planned_gemm<MODE>(ctx, am, bm, b2m, grid, g, stream);
 }
 
 // Tensor maps of the layers seen so far: the weights' (for every tile width) in a small direct-mapped cache keyed by the
@@ -978,6 +1122,8 @@ dcut_status dcut_init_layer(dcut_ctx* ctx) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kResidual>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kSwiGLU>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kArgmax>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kLinear>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kLinearGated>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
     if (e != cudaSuccess) return dcut_check_cuda(ctx, e, "cudaFuncSetAttribute(gemm)");
     {
         // The GEMM is launched as clusters of two CTAs so that it can run tiles on pairs of SMs where that pays
@@ -1113,6 +1259,26 @@ dcut_status dcut_launch_gemm(dcut_ctx* ctx, const void* a, const void* w, const 
     if (mode == kSwiGLU) return launch_gemm<kSwiGLU>(ctx, am, bm, b2m, N / (BN / 2), T_cap, mask, g, stream);
     if (mode == kResidual) return launch_gemm<kResidual>(ctx, am, bm, b2m, N / BN, T_cap, mask, g, stream);
     return launch_gemm<kPlain>(ctx, am, bm, b2m, N / BN, T_cap, mask, g, stream);
+}
+
+dcut_status dcut_launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, const int* cu_q, int B, int T_cap, cudaStream_t stream) {
+    GemmArgs g = {};
+    g.cu_q = cu_q;
+    g.B = B;
+    g.N_out = l->N;
+    g.K = (l->K + BK - 1) / BK * BK;      // whole k-blocks: the tail reads as zeros in both operands
+    g.out = static_cast<__nv_bfloat16*>(l->out);
+    g.residual = static_cast<const __nv_bfloat16*>(l->residual);
+    g.bias = static_cast<const __nv_bfloat16*>(l->bias);
+    g.bias2 = static_cast<const __nv_bfloat16*>(l->bias2);
+    g.ldo = l->ldo;
+    g.ldr = l->ldr;
+    g.act = l->act;
+    g.T_cap = T_cap;
+    auto vec = [](const void* p, long long ld) { return !(reinterpret_cast<uintptr_t>(p) & 15) && ld % 8 == 0; };
+    g.vec = (vec(l->out, l->ldo) ? 1 : 0) | (vec(l->residual, l->ldr) ? 2 : 0) | (vec(l->bias, 0) && vec(l->bias2, 0) ? 4 : 0);
+    g.status = ctx->d_status;
+    return l->w2 ? launch_linear<kLinearGated>(ctx, l, T_cap, g, stream) : launch_linear<kLinear>(ctx, l, T_cap, g, stream);
 }
 
 dcut_status dcut_launch_layer(dcut_ctx* ctx, const dcut_layer_weights* w, const void* x, void* y, void* k_cache,

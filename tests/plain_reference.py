@@ -57,9 +57,10 @@ def linear(a, w, bias=None, act="none", w2=None, bias2=None, residual=None):
     if act == "relu":
         z = np.maximum(z, 0)
     elif act == "gelu":
-        z = 0.5 * z * (1 + np.vectorize(math.erf)(z / math.sqrt(2)))
+        z = 0.5 * z * np.vectorize(math.erfc)(-z / math.sqrt(2))               # (1 + erf cancels far below zero)
     elif act == "gelu_tanh":
-        z = 0.5 * z * (1 + np.tanh(math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)))
+        with np.errstate(over="ignore"):                                       # (1 + tanh u) / 2 = 1 / (1 + e^-2u)
+            z = z / (1 + np.exp(-2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)))
     elif act == "silu":
         with np.errstate(over="ignore"):
             z = z / (1 + np.exp(-z))
