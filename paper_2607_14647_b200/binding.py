@@ -171,9 +171,9 @@ def _rows(t: Optional[torch.Tensor]):
     """(pointer, row stride) of a bf16 [rows, columns] view whose rows are dense."""
     if t is None:
         return None, 0
-    assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), \
-        "expected a CUDA bf16 matrix with dense rows"
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8     # (one row: its stride says nothing)
+    (rows, cols), (ld, step) = t.shape, t.stride()
+    assert t.is_cuda and t.dtype == torch.bfloat16 and (step == 1 or cols == 1), "expected a CUDA bf16 matrix with dense rows"
+    return t.data_ptr(), ld if rows > 1 else (cols + 7) // 8 * 8                         # (one row: its stride says nothing)
 
 
 def rope_inv_freq(theta: float, rotary_dim: int, device="cuda") -> torch.Tensor:
@@ -567,14 +567,15 @@ class Context:
         be views with padded rows (a and w: a multiple of 8 elements apart)."""
         N, K = w.shape
         assert a.shape[1] == K and a.shape[0] >= T_cap, "a must be [T_cap rows, K]"
-        assert w2 is None or (w2.shape == w.shape and _rows(w2)[1] == _rows(w)[1]), "w2 must have the shape and strides of w"
-        assert all(t is None or t.shape == (N,) for t in (bias, bias2))
+        assert bias is None or bias.shape == (N,)
+        assert bias2 is None or bias2.shape == (N,)
         assert residual is None or (residual.shape[0] >= T_cap and residual.shape[1] == N)
         if out is None:
             out = torch.empty((T_cap, N), dtype=torch.bfloat16, device=a.device)
         assert out.shape[0] >= T_cap and out.shape[1] == N
-        (ap, lda), (wp, ldw), (rp, ldr), (op, ldo) = _rows(a), _rows(w), _rows(residual), _rows(out)
-        l = LinearArgs(ap, lda, wp, _rows(w2)[0], ldw, _ptr(bias, torch.bfloat16), _ptr(bias2, torch.bfloat16), rp, ldr, op, ldo, N, K,
+        (ap, lda), (wp, ldw), (w2p, ldw2), (rp, ldr), (op, ldo) = _rows(a), _rows(w), _rows(w2), _rows(residual), _rows(out)
+        assert w2 is None or (w2.shape == w.shape and ldw2 == ldw), "w2 must have the shape and strides of w"
+        l = LinearArgs(ap, lda, wp, w2p, ldw, _ptr(bias, torch.bfloat16), _ptr(bias2, torch.bfloat16), rp, ldr, op, ldo, N, K,
                        ACTIVATIONS[act])
         self._check(_lib.dcut_linear(self._h, C.byref(l), _ptr(cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, _stream()))
         return out

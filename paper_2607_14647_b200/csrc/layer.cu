@@ -20,6 +20,7 @@
 // M is ragged and known only on the device (T = cu_q[B]): grids are sized for T_cap, CTAs without work fall through,
 // rows past T are computed on whatever the buffers hold and never stored.  Every kernel is launched with programmatic
 // dependent launch and waits for its predecessor before touching global memory.
+#include <cstddef>
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <limits.h>
@@ -38,6 +39,7 @@ constexpr int kGemmThreads = 192;              // warp 0: TMA, warp 1: MMA + TME
 constexpr int kTmemCols = 512;              // two 128 x 256 fp32 accumulators
 constexpr int kMaxStages = 12;                 // a narrow tile's stage is smaller: more of them fit the same operand area
 constexpr int kGemmSmem = kGemmStages * kGemmStageBytes + 1024 /* align */ + 512 /* two sets of barriers, tmem ptr */;
+constexpr int kLinearSmem = kGemmSmem + 4 * (32 * 33 + 32 + BN) * 4;   // + LinearShared of four epilogue warps
 constexpr int kWaitLimit = 1 << 22;
 
 enum GemmMode { kPlain = 0, kResidual = 1, kSwiGLU = 2, kArgmax = 3, kLinear = 4, kLinearGated = 5 };
@@ -53,11 +55,12 @@ __host__ __device__ constexpr int bn_of(int i) { return BN - 32 * i; }
 struct BMaps {
     CUtensorMap m[kNumBn];
 };
-// The activations' tensor map with the full 128-row box and with a 64-row box: with at most 64 packed rows a tile's
-// lower half would only be fetched to be ignored (at T = 64 the A tiles were more than half of what the SMs took in).
+// The activations' tensor map with the full 128-row box, a 64-row box and a 16-row box: with at most 64 (16) packed rows
+// the rest of a tile would only be fetched to be ignored (at T = 64 the A tiles were more than half of what the SMs took in).
 struct AMaps {
-    CUtensorMap full, half;
+    CUtensorMap full, half, small;
 };
+constexpr int kSmallRows = 16;
 constexpr unsigned kBnMaskAll = (1u << kNumBn) - 1;
 constexpr int kPlanRows = 72;
 constexpr int kSplitCost = 50;             // gemm_plan: what the exchange of partial sums between the two SMs costs
@@ -163,7 +166,7 @@ struct GemmArgs {
     long long ldo, ldr;              // kLinear*: elements from one row of out / residual to the next
     int T_cap;                       // kLinear*: rows that out has
     int act;                         // kLinear*: dcut_act
-    int vec;                         // kLinear*: 1: out, 2: residual, 4: bias and bias2 take 16-byte accesses at multiples of 8 columns
+    int vec;                         // kLinear*: out and residual take 16-byte accesses at multiples of 8 columns
     int pairs;                       // launched as clusters of two CTAs: the pair mode may be chosen
     unsigned bn_mask;                // tile widths whose tensor maps were supplied (bit i: bn_of(i)); bit 0 always
     int force;                       // experiments: -1 = let gemm_plan choose, 0..6 = that width on one SM, 8..14 = on a pair
@@ -186,95 +189,145 @@ __device__ __forceinline__ const CUtensorMap* pick_map(const BMaps& s, int i) {
 
 // ------------------------------------------------------------------------------------------------ dcut_linear's epilogue
 
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, int n, bool vec, float (&x)[8]) {
-    if (vec && n >= 8) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            x[2 * j] = bf_lo(w[j]);
-            x[2 * j + 1] = bf_hi(w[j]);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = j < n ? __bfloat162float(p[j]) : 0.0f;
-    }
-}
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }    // (exp overflows to inf: 0)
-__device__ __forceinline__ void activate8(int act, float (&x)[8]) {
+// (e^-x overflows to infinity: 0.  The fast quotient returns 0 for a divisor above 2^126, where the value is below 2^-126.)
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
+// A function of its own: inlined for every column of the epilogue, the five cases made a loop body larger than the
+// instruction cache (gelu_tanh over 1088 x 12288, K = 4096: 108 us against 97).
+__device__ __noinline__ float4 activate4(int act, float4 v) {
+    float x[4] = {v.x, v.y, v.z, v.w};
     if (act == DCUT_ACT_RELU) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = x[j] < 0.0f ? 0.0f : x[j];                        // (a NaN stays)
+        for (int j = 0; j < 4; ++j) x[j] = x[j] < 0.0f ? 0.0f : x[j];                        // (a NaN stays)
     } else if (act == DCUT_ACT_GELU) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= 0.5f * erfcf(x[j] * -0.7071067811865476f);       // Phi(x) without cancellation
+        for (int j = 0; j < 4; ++j) x[j] *= 0.5f * erfcf(x[j] * -0.7071067811865476f);       // Phi(x) without cancellation
     } else if (act == DCUT_ACT_GELU_TANH) {
         // (1 + tanh u) / 2 = sigmoid(2 u), u = sqrt(2 / pi) (x + 0.044715 x^3)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= sigmoid(1.5957691216057308f * x[j] * fmaf(0.044715f * x[j], x[j], 1.0f));
-    } else if (act == DCUT_ACT_SILU) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= sigmoid(x[j]);
-    }
-}
-// x (and, gated, u): eight columns of a row as the MMAs left them.  Everything in fp32, one rounding at the store.
-template <bool GATED>
-__device__ __forceinline__ void linear_finish8(const GemmArgs& g, int row, int col, float (&x)[8], const float (&u)[8]) {
-    const int n = g.N_out - col;
-    float t[8];
-    if (g.bias) {
-        load8(g.bias + col, n, g.vec & 4, t);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] += t[j];
-    }
-    activate8(g.act, x);
-    if (GATED) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = 0.0f;
-        if (g.bias2) load8(g.bias2 + col, n, g.vec & 4, t);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= u[j] + t[j];
-    }
-    if (g.residual) {
-        load8(g.residual + (size_t)row * g.ldr + col, n, g.vec & 2, t);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] += t[j];
-    }
-    __nv_bfloat16* o = g.out + (size_t)row * g.ldo + col;
-    if ((g.vec & 1) && n >= 8) {
-        *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+        for (int j = 0; j < 4; ++j) x[j] *= sigmoid(1.5957691216057308f * x[j] * fmaf(0.044715f * x[j], x[j], 1.0f));
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) o[j] = __float2bfloat16_rn(x[j]);
+        for (int j = 0; j < 4; ++j) x[j] *= sigmoid(x[j]);
     }
+    return make_float4(x[0], x[1], x[2], x[3]);
+}
+
+// Shared memory of one epilogue warp: 32 rows x 32 columns of results on their way to rows that take no vectors, and the
+// biases of the tile's columns.
+constexpr int kStageRow = 33;
+struct LinearShared {
+    float stage[32 * kStageRow];
+    float pad[32];                       // (16-byte alignment of what follows, whatever the row)
+    float bias[BN];                      // gated: bias, then bias2, half each
+};
+static_assert(sizeof(LinearShared) % 16 == 0 && offsetof(LinearShared, bias) % 16 == 0, "read in vectors");
+static_assert(kLinearSmem - kGemmSmem == 4 * sizeof(LinearShared), "one per epilogue warp");
+
+// Before the accumulator is complete: the biases of a tile's columns, zeros where there are none.
+template <bool GATED>
+__device__ __forceinline__ void linear_stage_bias(const GemmArgs& g, int n_tile, int bn, LinearShared& sh) {
+    const int lane = threadIdx.x & 31, width = GATED ? bn >> 1 : bn, col0 = n_tile * width;
+    __syncwarp();                                                      // (the previous tile's have been read)
+    for (int c = lane; c < width; c += 32) {
+        const bool there = col0 + c < g.N_out;
+        sh.bias[c] = there && g.bias ? __bfloat162float(g.bias[col0 + c]) : 0.0f;
+        if (GATED) sh.bias[BN / 2 + c] = there && g.bias2 ? __bfloat162float(g.bias2[col0 + c]) : 0.0f;
+    }
+    __syncwarp();
+}
+__device__ __forceinline__ bool linear_by_vector(const GemmArgs& g, int col) { return g.vec && col + 32 <= g.N_out; }
+// The residual that linear_finish32 adds in 32 columns of the warp's 32 rows, fetched before the accumulators are read: 32 columns
+// of this thread's row, or column `lane` of every row.
+struct LinearAhead {
+    uint32_t r[32];
+};
+__device__ __forceinline__ void linear_fetch(const GemmArgs& g, int T, int row0, int col, LinearAhead& f) {
+    const int lane = threadIdx.x & 31;
+    if (!g.residual) return;
+    if (linear_by_vector(g, col)) {
+        if (row0 + lane >= T) return;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const uint4 r = *reinterpret_cast<const uint4*>(g.residual + (size_t)(row0 + lane) * g.ldr + col + 8 * v);
+            f.r[4 * v] = r.x, f.r[4 * v + 1] = r.y, f.r[4 * v + 2] = r.z, f.r[4 * v + 3] = r.w;
+        }
+    } else if (col + lane < g.N_out) {
+        const unsigned short* r = reinterpret_cast<const unsigned short*>(g.residual) + (size_t)row0 * g.ldr + col + lane;
+#pragma unroll
+        for (int i = 0; i < 32; ++i, r += g.ldr) f.r[i] = row0 + i < T ? *r : 0;
+    }
+}
+// x (and, gated, u): 32 columns of this thread's row as the MMAs left them; a whole warp calls with its 32 rows; c = the
+// first column within the tile.  Everything in fp32, one rounding at the store.  Rows of out and residual that take 16-byte
+// accesses are read and written by the thread that owns the row.  Others (an odd N, say) would be 2-byte accesses to 32
+// rows at a time, 32 lines each: they go through shared memory, so that a warp reads and writes 32 columns of one row at a
+// time (333 x 2051 with a residual, K = 1003: 21.1 us without that, 12.3 with it).
+template <bool GATED>
+__device__ __forceinline__ void linear_finish32(const GemmArgs& g, int T, int row0, int col, int c, LinearShared& sh, const LinearAhead& f,
+                                                const float (&x)[32], const float (&u)[32]) {
+    const int lane = threadIdx.x & 31, row = row0 + lane;
+    const bool by_vector = linear_by_vector(g, col);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        float4 y[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int e = 8 * v + 4 * h;
+            const float4 b = *reinterpret_cast<const float4*>(sh.bias + c + e);
+            y[h] = make_float4(x[e] + b.x, x[e + 1] + b.y, x[e + 2] + b.z, x[e + 3] + b.w);
+            if (g.act != DCUT_ACT_NONE) y[h] = activate4(g.act, y[h]);
+            if (GATED) {
+                const float4 b2 = *reinterpret_cast<const float4*>(sh.bias + BN / 2 + c + e);
+                y[h].x *= u[e] + b2.x, y[h].y *= u[e + 1] + b2.y, y[h].z *= u[e + 2] + b2.z, y[h].w *= u[e + 3] + b2.w;
+            }
+        }
+        if (!by_vector) {
+            float* s = sh.stage + lane * kStageRow + 8 * v;
+            s[0] = y[0].x, s[1] = y[0].y, s[2] = y[0].z, s[3] = y[0].w, s[4] = y[1].x, s[5] = y[1].y, s[6] = y[1].z, s[7] = y[1].w;
+        } else if (row < T) {
+            if (g.residual) {
+                const uint32_t* r = f.r + 4 * v;
+                y[0].x += bf_lo(r[0]), y[0].y += bf_hi(r[0]), y[0].z += bf_lo(r[1]), y[0].w += bf_hi(r[1]);
+                y[1].x += bf_lo(r[2]), y[1].y += bf_hi(r[2]), y[1].z += bf_lo(r[3]), y[1].w += bf_hi(r[3]);
+            }
+            *reinterpret_cast<uint4*>(g.out + (size_t)row * g.ldo + col + 8 * v) =
+                make_uint4(pack_bf16(y[0].x, y[0].y), pack_bf16(y[0].z, y[0].w), pack_bf16(y[1].x, y[1].y), pack_bf16(y[1].z, y[1].w));
+        }
+    }
+    if (by_vector) return;
+    __syncwarp();
+    if (col + lane < g.N_out) {
+        __nv_bfloat16* o = g.out + (size_t)row0 * g.ldo + col + lane;
+#pragma unroll
+        for (int i = 0; i < 32; ++i, o += g.ldo)
+            if (row0 + i < T) *o = __float2bfloat16_rn(sh.stage[i * kStageRow + lane] + (g.residual ? bf_lo(f.r[i]) : 0.0f));
+    }
+    __syncwarp();                                                      // the next step writes the stage again
 }
 
 // Epilogue of one 128 x bn accumulator (this thread: tensor-memory lane = output row `row`), for every mode.  Columns
 // past N_out (a ragged last tile of a narrow width) were computed on zero weight rows and are not stored.
 template <int MODE>
-__device__ __forceinline__ void gemm_epilogue(const GemmArgs& g, int T, int row, int n_tile, uint32_t t_row, int bn) {
+__device__ __forceinline__ void gemm_epilogue(const GemmArgs& g, int T, int row, int n_tile, uint32_t t_row, int bn, LinearShared& sh) {
     if (MODE == kLinear || MODE == kLinearGated) {
-        const int width = MODE == kLinearGated ? bn >> 1 : bn, col0 = n_tile * width;
+        const int width = MODE == kLinearGated ? bn >> 1 : bn, col0 = n_tile * width, row0 = row - (threadIdx.x & 31);
+        if (row0 >= T) return;                                          // (the whole warp: none of its rows exists)
+        LinearAhead ahead;
+        linear_fetch(g, T, row0, col0, ahead);
 #pragma unroll 1
-        for (int c = 0; c < width; c += 32) {
+        for (int c = 0; c < width && col0 + c < g.N_out; c += 32) {
             uint32_t av[32], uv[32];
             tc_ld32(t_row + c, av);
             if (MODE == kLinearGated) tc_ld32(t_row + width + c, uv);
             tc_wait_ld();
-            if (row < T) {
+            float x[32], u[32];
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    if (col0 + c + e >= g.N_out) break;
-                    float x[8], u[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        x[j] = __uint_as_float(av[e + j]);
-                        u[j] = MODE == kLinearGated ? __uint_as_float(uv[e + j]) : 0.0f;
-                    }
-                    linear_finish8<MODE == kLinearGated>(g, row, col0 + c + e, x, u);
-                }
+            for (int j = 0; j < 32; ++j) {
+                x[j] = __uint_as_float(av[j]);
+                u[j] = MODE == kLinearGated ? __uint_as_float(uv[j]) : 0.0f;
             }
+            linear_finish32<MODE == kLinearGated>(g, T, row0, col0 + c, c, sh, ahead, x, u);
+            if (c + 32 < width) linear_fetch(g, T, row0, col0 + c + 32, ahead);
         }
     } else if (MODE == kSwiGLU) {
         const int half = bn >> 1, col0 = n_tile * half;
@@ -476,6 +529,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
     unsigned long long* bars2 = bars + 2 * kMaxStages + 4;                  // the pair mode's set
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars2 + 2 * kG2Stages + 4);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    LinearShared& sh = reinterpret_cast<LinearShared*>(smem + kGemmSmem - 1024)[warp & 3];   // (linear modes only) behind the barriers
     const int n_kb = g.K / BK;
 
     if (threadIdx.x == 0) {
@@ -496,6 +550,13 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
+    if (threadIdx.x == 32) {                     // the tensor maps that the largest packed length would use
+        const int m = g.plan_by_m[kPlanRows - 1];
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&a_maps.full)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&a_maps.small)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(pick_map(b_maps, m & 7))) : "memory");
+        if (is_gated(MODE)) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(pick_map(b2_maps, m & 7))) : "memory");
+    }
     __syncthreads();
     cluster_sync_all();                          // the peer's barriers exist before anything is signalled on them
     // everything above overlaps the previous kernel of the stream; nothing it wrote is read before this wait
@@ -507,11 +568,11 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
         if (blockIdx.x == 0 && threadIdx.x == 0) atomicExch(g.status, DCUT_DEV_BAD_ROWS);
     }
     const int T = T_packed;
-    // rows 64..127 of the A tile are not loaded when no row of them exists: they hold whatever shared memory held, and
-    // the accumulator rows computed from them are never stored (one-SM and split modes; a pair always loads full boxes)
-    const bool a_half = T <= BM / 2;
-    const CUtensorMap* a_map1 = a_half ? &a_maps.half : &a_maps.full;
-    const uint32_t a_bytes = a_half ? kATile / 2 : kATile;
+    // rows 16..127 or 64..127 of the A tile are not loaded when no row of them exists: the MMA reads there whatever shared
+    // memory holds (with small stages, parts of the following ones), and the accumulator rows computed from them are never
+    // stored (one-SM and split modes; a pair always loads full boxes)
+    const CUtensorMap* a_map1 = T <= kSmallRows ? &a_maps.small : T <= BM / 2 ? &a_maps.half : &a_maps.full;
+    const uint32_t a_bytes = T <= kSmallRows ? kSmallRows * BK * 2 : T <= BM / 2 ? kATile / 2 : kATile;
     const int m_blocks = (T + BM - 1) / BM;
     const int plan_all = m_blocks > 0 ? g.plan_by_m[(m_blocks < kPlanRows ? m_blocks : kPlanRows) - 1] : 0;
     const bool split = plan_all >= kPlanSplit;                      // the pair shares one 128-row tile, half of K each
@@ -524,7 +585,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
     // 64-wide tile at T <= 64 moves 8 KB of weights per stage: with four stages too few bytes were in flight per SM to
     // cover the DRAM latency)
     const uint32_t stage_stride = a_bytes + (uint32_t)bn * BK * 2;                         // multiples of 1 KB
-    const int n_stages = min(kMaxStages, (int)((uint32_t)(kGemmStages * kGemmStageBytes) / stage_stride));
+    const int n_stages = min(kMaxStages, 1 + (int)(((uint32_t)(kGemmStages * kGemmStageBytes) - max(stage_stride, (uint32_t)kATile)) / stage_stride));
     if (warp == 1) {   // tensor memory: two 128 x 256 fp32 accumulators (per CTA; allocated for the pair in pair mode)
         if (pairs) {
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "n"(kTmemCols) : "memory");
@@ -602,6 +663,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
             if (!failed && elect_one()) tc_commit(acc_full);    // this CTA's partial sums are complete
             __syncwarp();
         } else if (has_tile) {
+            if (MODE == kLinear) linear_stage_bias<false>(g, n_tile, bn, sh);
             if (!__all_sync(0xffffffffu, mbar_wait(acc_full, 0))) failed = true;   // ... and its operand ring is idle
             tc_fence_after();
         }
@@ -611,10 +673,14 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
         const int quarter = warp & 3, row_in_tile = quarter * 32 + lane;
         const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16);
         const uint32_t stage_local = smem_u32(smem);              // [column / 4][row] vectors of four fp32: 64 KB at most
+        LinearAhead ahead;                                        // (kLinear only)
+        const int row0 = m0 + quarter * 32;
+        const bool rows_here = row0 < T;                          // (a warp without rows has nothing to exchange)
+        if (MODE == kLinear && has_tile && warp >= 2 && rows_here) linear_fetch(g, T, row0, n_tile * bn + own0, ahead);
         tc_fence_before();
         cluster_sync_all();                                       // both accumulators complete, both rings idle
         tc_fence_after();
-        if (has_tile && warp >= 2 && !failed) {
+        if (has_tile && warp >= 2 && rows_here && !failed) {
             asm volatile("fence.proxy.async;" ::: "memory");      // the ring was last written and read through the async proxy
             const uint32_t stage_peer = mapa_rank(stage_local, rank ^ 1);
 #pragma unroll 1
@@ -633,14 +699,31 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
         tc_fence_before();
         cluster_sync_all();                                       // the peer's partial sums have arrived
         tc_fence_after();
-        if (has_tile && warp >= 2 && !failed) {
+        if (has_tile && warp >= 2 && rows_here && !failed) {
             const int row = m0 + row_in_tile, col0 = n_tile * bn;
             __nv_bfloat16* orow = g.out + (size_t)row * g.N_out + col0;
             const __nv_bfloat16* rrow = MODE == kResidual ? g.residual + (size_t)row * g.N_out + col0 : nullptr;
 #pragma unroll 1
             for (int c = own0; c < own1; c += 32) {
+                if (MODE == kLinear && col0 + c >= g.N_out) break;
                 uint32_t av[32];
                 tc_ld32(t_row + c, av);
+                if (MODE == kLinear) {
+                    tc_wait_ld();
+                    float x[32];
+#pragma unroll
+                    for (int v = 0; v < 8; ++v) {
+                        float add[4];
+                        const uint32_t src = stage_local + (uint32_t)((((c - own0) >> 2) + v) * BM + row_in_tile) * 16;
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(add[0]), "=f"(add[1]), "=f"(add[2]), "=f"(add[3]) : "r"(src));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)   // (rank 0's half of K) + (rank 1's)
+                            x[4 * v + j] = rank ? add[j] + __uint_as_float(av[4 * v + j]) : __uint_as_float(av[4 * v + j]) + add[j];
+                    }
+                    linear_finish32<false>(g, T, row0, col0 + c, c, sh, ahead, x, x);
+                    if (c + 32 < own1) linear_fetch(g, T, row0, col0 + c + 32, ahead);
+                    continue;
+                }
                 tc_wait_ld();
                 if (row < T) {
 #pragma unroll
@@ -652,13 +735,6 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                             const uint32_t src = stage_local + (uint32_t)((((c - own0 + e) >> 2) + v) * BM + row_in_tile) * 16;
                             asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
                                          : "=f"(add[4 * v]), "=f"(add[4 * v + 1]), "=f"(add[4 * v + 2]), "=f"(add[4 * v + 3]) : "r"(src));
-                        }
-                        if (MODE == kLinear) {
-                            float x[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) x[j] = rank ? add[j] + __uint_as_float(av[e + j]) : __uint_as_float(av[e + j]) + add[j];
-                            linear_finish8<false>(g, row, col0 + c + e, x, x);
-                            continue;
                         }
                         uint4 res = make_uint4(0, 0, 0, 0);
                         if (MODE == kResidual) res = *reinterpret_cast<const uint4*>(rrow + c + e);
@@ -756,13 +832,14 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                 const int n_tile = w / m_tiles, m0 = (w - n_tile * m_tiles) * BM;
                 const int acc = it & 1;
                 const int row = m0 + quarter * 32 + lane;
-                if (!mbar_wait(acc_full + 8 * acc, (it >> 1) & 1)) {
+                if (MODE == kLinear || MODE == kLinearGated) linear_stage_bias<MODE == kLinearGated>(g, n_tile, bn, sh);
+                if (!__all_sync(0xffffffffu, mbar_wait(acc_full + 8 * acc, (it >> 1) & 1))) {
                     failed = true;
                     break;
                 }
                 tc_fence_after();
                 const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * BN;
-                gemm_epilogue<MODE>(g, T, row, n_tile, t_row, bn);
+                gemm_epilogue<MODE>(g, T, row, n_tile, t_row, bn, sh);
                 // this accumulator may be overwritten once all four epilogue warps have read it
                 tc_fence_before();
                 mbar_arrive(acc_empty + 8 * acc);
@@ -848,13 +925,14 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                 const int n_tile = w / m_tiles, m0 = (w - n_tile * m_tiles) * (2 * BM) + (int)rank * BM;
                 const int acc = it & 1;
                 const int row = m0 + quarter * 32 + lane;
-                if (!mbar_wait(acc_full + 8 * acc, (it >> 1) & 1)) {
+                if (MODE == kLinear || MODE == kLinearGated) linear_stage_bias<MODE == kLinearGated>(g, n_tile, bn, sh);
+                if (!__all_sync(0xffffffffu, mbar_wait(acc_full + 8 * acc, (it >> 1) & 1))) {
                     failed = true;
                     break;
                 }
                 tc_fence_after();
                 const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * BN;
-                gemm_epilogue<MODE>(g, T, row, n_tile, t_row, bn);
+                gemm_epilogue<MODE>(g, T, row, n_tile, t_row, bn, sh);
                 tc_fence_before();
                 mbar_arrive_remote(lead_acc_empty + 8 * acc);
             }
@@ -995,10 +1073,11 @@ dcut_status make_kmajor_map(dcut_ctx* ctx, CUtensorMap* map, const void* base, l
     return DCUT_OK;
 }
 
-dcut_status make_act_maps(dcut_ctx* ctx, AMaps* maps, const void* base, long long rows, long long cols) {
-    dcut_status st = make_kmajor_map(ctx, &maps->full, base, rows, cols, BM);
+dcut_status make_act_maps(dcut_ctx* ctx, AMaps* maps, const void* base, long long rows, long long cols, long long ld = 0) {
+    dcut_status st = make_kmajor_map(ctx, &maps->full, base, rows, cols, BM, ld);
     if (st != DCUT_OK) return st;
-    return make_kmajor_map(ctx, &maps->half, base, rows, cols, BM / 2);
+    if ((st = make_kmajor_map(ctx, &maps->half, base, rows, cols, BM / 2, ld)) != DCUT_OK) return st;
+    return make_kmajor_map(ctx, &maps->small, base, rows, cols, kSmallRows, ld);
 }
 
 // The weight's tensor maps for the tile widths in `mask` (box = half the width in rows)
@@ -1051,6 +1130,7 @@ int plan_gemm(dcut_ctx* ctx, int n_tiles, int T_cap, unsigned bn_mask, GemmArgs&
 
 template <int MODE>
 dcut_status launch_planned_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMaps& b2, int grid, const GemmArgs& ga, cudaStream_t stream) {
+    const size_t smem = MODE == kLinear || MODE == kLinearGated ? kLinearSmem : kGemmSmem;
     if (ctx->ly_gemm_pairs > 0) {
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -1062,13 +1142,13 @@ dcut_status launch_planned_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, c
         cudaLaunchConfig_t lc = {};
         lc.gridDim = dim3(grid);
         lc.blockDim = dim3(kGemmThreads);
-        lc.dynamicSmemBytes = kGemmSmem;
+        lc.dynamicSmemBytes = smem;
         lc.stream = stream;
         lc.attrs = attr;
         lc.numAttrs = 2;
         return dcut_check_cuda(ctx, cudaLaunchKernelEx(&lc, gemm_tcgen05_kernel<MODE>, a, b, b2, ga), "launch gemm_tcgen05_kernel");
     }
-    return dcut_check_cuda(ctx, dcut_launch_pdl(gemm_tcgen05_kernel<MODE>, dim3(grid), dim3(kGemmThreads), kGemmSmem, stream, a, b, b2, ga),
+    return dcut_check_cuda(ctx, dcut_launch_pdl(gemm_tcgen05_kernel<MODE>, dim3(grid), dim3(kGemmThreads), smem, stream, a, b, b2, ga),
                            "launch gemm_tcgen05_kernel");
 }
 
@@ -1092,8 +1172,7 @@ dcut_status launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, int T_cap, G
     AMaps am;
     BMaps bm = {}, b2m = {};
     dcut_status st;
-    if ((st = make_kmajor_map(ctx, &am.full, l->a, T_cap, l->K, BM, l->lda)) != DCUT_OK) return st;
-    if ((st = make_kmajor_map(ctx, &am.half, l->a, T_cap, l->K, BM / 2, l->lda)) != DCUT_OK) return st;
+    if ((st = make_act_maps(ctx, &am, l->a, T_cap, l->K, l->lda)) != DCUT_OK) return st;
     for (int i = 0; i < kNumBn; ++i) {
         if (!((used >> i) & 1)) continue;
         if ((st = make_kmajor_map(ctx, &bm.m[i], l->w, l->N, l->K, bn_of(i) / 2, l->ldw)) != DCUT_OK) return st;
@@ -1122,8 +1201,8 @@ dcut_status dcut_init_layer(dcut_ctx* ctx) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kResidual>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kSwiGLU>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kArgmax>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kLinear>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kLinearGated>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kLinear>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kLinearGated>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
     if (e != cudaSuccess) return dcut_check_cuda(ctx, e, "cudaFuncSetAttribute(gemm)");
     {
         // The GEMM is launched as clusters of two CTAs so that it can run tiles on pairs of SMs where that pays
@@ -1276,7 +1355,7 @@ dcut_status dcut_launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, const i
     g.act = l->act;
     g.T_cap = T_cap;
     auto vec = [](const void* p, long long ld) { return !(reinterpret_cast<uintptr_t>(p) & 15) && ld % 8 == 0; };
-    g.vec = (vec(l->out, l->ldo) ? 1 : 0) | (vec(l->residual, l->ldr) ? 2 : 0) | (vec(l->bias, 0) && vec(l->bias2, 0) ? 4 : 0);
+    g.vec = vec(l->out, l->ldo) && (!l->residual || vec(l->residual, l->ldr));
     g.status = ctx->d_status;
     return l->w2 ? launch_linear<kLinearGated>(ctx, l, T_cap, g, stream) : launch_linear<kLinear>(ctx, l, T_cap, g, stream);
 }
