@@ -163,6 +163,18 @@ __device__ __forceinline__ uint32_t tile_off(int r, int c16) {
     return (uint32_t)(((c16 >> 3) << 11) + (r << 7) + (((c16 & 7) ^ (r & 7)) << 4));
 }
 
+// Keys behind the last one that an item's rows see (a request's last page ends inside its tile) have weight 0, but 0 x NaN is
+// NaN, and what an unwritten cache slot holds is anything: the warp clears those rows of the V tile it is about to use,
+// `first` .. 15.  Others that share the tile clear the same rows for themselves.  The fence orders the stores before the
+// MMAs and the loads into this stage that follow (async proxy).
+template <int DH>
+__device__ __forceinline__ void clear_v_rows(uint32_t v_tile, int first) {
+    for (int i = max(first, 0) * (DH / 8) + (threadIdx.x & 31); i < kPage * (DH / 8); i += 32)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v_tile + tile_off(i / (DH / 8), i % (DH / 8))), "r"(0) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+
 // the same for a K page of the tcgen05 phase, which one 4-D TMA box delivers as [8-row group][half][8 rows][64 columns]
 __device__ __forceinline__ uint32_t tile_off_k4(int r, int c16) {
     return (uint32_t)(((r >> 3) << 11) + ((c16 >> 3) << 10) + ((r & 7) << 7) + (((c16 & 7) ^ (r & 7)) << 4));
@@ -632,6 +644,7 @@ __device__ __forceinline__ void mma_phase(const CUtensorMap& k_map, const CUtens
             const int R_lo = mt * 16 + (lane >> 2), R_hi = R_lo + 8;
             const int jmax_lo = ctx_len + (row0 + min(R_lo, M - 1)) / group;
             const int jmax_hi = ctx_len + (row0 + min(R_hi, M - 1)) / group;
+            const int jlast = ctx_len + (row0 + M - 1) / group;
             // per-lane ldmatrix row/chunk selectors
             const int kmat = lane >> 3;
             const int k_tok = ((kmat >> 1) << 3) + (lane & 7);
@@ -653,6 +666,8 @@ __device__ __forceinline__ void mma_phase(const CUtensorMap& k_map, const CUtens
                 }
                 const uint32_t k_base = smem_u32(ring + stage * L::kStageBytes);
                 const uint32_t v_base = k_base + L::kPageBytes;
+                const int visible = jlast + 1 - (item.page_begin + p) * kPage;   // rows of this page that some row of the item sees
+                if (visible < kPage) clear_v_rows<DH>(v_base, visible);
 
                 float s[2][4];
 #pragma unroll
@@ -1004,6 +1019,7 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
             if (!q_staged) store_q(item);
             q_staged = false;
             const int jmax = ctx_len + (row0 + min(R, M - 1)) / group;  // last visible cache position
+            const int jlast = ctx_len + (row0 + item.pad[2] - 1) / group;  // the last that any row of the item sees
             const bool live = ((quarter * 32 + 64) & 127) < M;           // (warp-uniform) some of this warp's rows exist
             float m_run = -INFINITY, l_run = 0.0f;
             for (int g = team; g < n_groups; g += 2) {
@@ -1019,6 +1035,15 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
                     continue;
                 }
                 const uint32_t t_s = t_lane + kTcColS + 64 * b;
+                const int last_page = item.page_begin + min(4 * g + 4, n_pages) - 1;       // of this group
+                if ((last_page + 1) * kPage > jlast + 1) {
+                    const int gs = gc % kTcGroupStages;
+                    if (!__all_sync(0xffffffffu, mbar_wait(full_bar + 8 * gs, (gc / kTcGroupStages) & 1, &c->abort))) failed = true;
+                    if (failed) break;
+                    const uint32_t v_grp = smem_u32(ring + gs * kTcGroupBytes) + 4 * kTcPageBytes;
+                    for (int pg = item.page_begin + 4 * g; pg <= last_page; ++pg)
+                        if ((pg + 1) * kPage > jlast + 1) clear_v_rows<128>(v_grp + (pg - item.page_begin - 4 * g) * kTcPageBytes, jlast + 1 - pg * kPage);
+                }
                 uint32_t sr[64];
                 tc_fence_after();
                 tc_ld32(t_s, sr);
@@ -1201,6 +1226,7 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
             const int n_pages = item.page_end - item.page_begin;
             const int n_groups = (n_pages + 3) >> 2;
             const bool has_tail = M > 0;
+            const int jlast = ctx_len + (row0 + M - 1) / group;          // the last position that any row of the item sees
             uint32_t qf[8][4];
             float o[16][4];
             float m_run[2] = {-INFINITY, -INFINITY};
@@ -1438,6 +1464,12 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
                 if (!__all_sync(0xffffffffu, mbar_wait(full_bar + 8 * gs, (gc / kTcGroupStages) & 1, &c->abort))) {
                     failed = true;
                     break;
+                }
+                if (has_tail && (item.page_begin + min(4 * g + 4, n_pages)) * kPage > jlast + 1) {
+                    for (int j = 0; j < min(4, n_pages - 4 * g); ++j) {
+                        const int visible = jlast + 1 - (item.page_begin + 4 * g + j) * kPage;
+                        if (visible < kPage) clear_v_rows<128>(smem_u32(ring + gs * kTcGroupBytes) + (4 + j) * kTcPageBytes, visible);
+                    }
                 }
                 if (swapped) {
                     const int np = min(4, n_pages - 4 * g);

@@ -309,3 +309,42 @@ def test_two_contexts_on_two_streams():
         assert ctxs[i].poll_device_status() == 0
         assert all(torch.equal(o, outs[i][0]) for o in outs[i])
         check(cases[i], outs[i][0], None)
+
+
+def poison_own_slots(c, k_value, v_value):
+    """What lies behind a request's last position in its own pages."""
+    group = np.repeat(np.arange(c["G"]), np.diff(c["cu_group"]))
+    for r in range(c["B"]):
+        end = int(c["ctx"][r] - c["plens"][group[r]] + c["counts"][r])
+        if end % 16:
+            page = int(c["table"][r, end // 16])
+            c["kc"][page, :, end % 16:] = k_value
+            c["vc"][page, :, end % 16:] = v_value
+
+
+@pytest.mark.parametrize("value", [NAN, float("inf"), -float("inf"), 3.3e38])
+@pytest.mark.parametrize("hq,hkv,d,deep", [(8, 8, 128, 1), (8, 2, 128, 17), (6, 2, 64, 9), (32, 4, 128, 17), (32, 2, 128, 9), (18, 2, 128, 16)])
+def test_unwritten_slots_behind_a_request_hold_anything(hq, hkv, d, deep, value):
+    """Warp-level tiles, tensor-memory tiles, their tails of up to 8 and 16 rows; long and short contexts."""
+    rng = np.random.default_rng(hq + deep)
+    counts = rng.integers(1, deep + 1, 20)
+    counts[:3] = deep
+    c = make_case(21, counts, np.concatenate([rng.integers(0, 100, 17), [1000, 2203, 4007]]), [11, 9], [70, 0], hq, hkv, d)
+    ctx = make_ctx(c)
+    clean, clean_lse = run(c, ctx)
+    poison_own_slots(c, value, value)
+    out, lse = run(c, ctx)
+    assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+    check(c, out, lse)
+
+
+@pytest.mark.parametrize("hq,hkv,d,deep", [(8, 8, 128, 1), (8, 2, 64, 17), (32, 4, 128, 17), (32, 2, 128, 9)])
+def test_verify_attn_with_unwritten_slots(hq, hkv, d, deep):
+    rng = np.random.default_rng(hq + deep)
+    counts = rng.integers(1, deep + 1, 12)
+    counts[0] = deep
+    c = make_case(22, counts, rng.integers(0, 3000, 12), [12], [0], hq, hkv, d)
+    poison_own_slots(c, NAN, NAN)
+    ctx = make_ctx(c)
+    out = ctx.verify_attn(c["q"], c["kc"], c["vc"], _i32(c["table"]), _i32(c["ctx"]), _i32(c["cu"]), c["cap"])
+    check(c, out, None)
