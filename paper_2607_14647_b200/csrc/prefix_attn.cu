@@ -5,7 +5,7 @@
 // The softmax is split at P.  Each part gives its normalised output and its log-sum-exp, and two such pairs merge into
 // one (weights 2^(lse - max)), so the shared keys are read once for all rows of a group instead of once per request:
 //
-//   prefix_plan_kernel     one CTA: the partition of the shared part (prefix_plan.cuh) and, for the own parts, the work
+//   prefix_plan_kernel     two CTAs: the partition of the shared part (prefix_plan.cuh) and, for the own parts, the work
 //                          list of dcut_verify_attn on own lengths L - P
 //   attn_item_kernel, attn_combine_kernel   (verify_attn.cu) the own parts: bound by HBM; output kept in fp32
 //   prefix_attn_kernel     the shared part on the tensor cores, its epilogue merging the own part's result and writing out
@@ -765,20 +765,28 @@ struct PrefixPlanArgs {
     int n_groups, prefix_table_stride;
     int group_size, max_rows, T_cap;      // max_rows: tokens of a request
     Group* groups;                        // [n_groups + 1]
-    long long* cost;                      // [n_groups + 1]
     Seg* segs;                            // [n_seg + 1]
     Cut* cuts;                            // [n_seg]
     int n_seg;
 };
 
-// One CTA.  A batch that is not what the call's contract says (cu_q, cu_group, lengths) is reported and left alone: its
+// The own parts' scan takes 2 B + 1 of the long longs; the partition G + 1 costs, a gap for alignment and, as far as that
+// fits (every B up to 8192 has to), G groups of two.
+constexpr int kSmemGroups = 4096;
+__host__ __device__ inline int plan_longs(int B) { return B <= kSmemGroups ? 3 * (B + 1) : 2 * (B + 1); }
+size_t plan_smem(int B) { return sizeof(long long) * plan_longs(B) + sizeof(int) * (2 * (size_t)B + 1); }
+
+// Two CTAs, which check the batch alike: the first makes the own parts' work list, the second the shared part's partition
+// (one after the other in one CTA they took 12 us, chains of dependent loads and scans both).  A batch that is not what the call's contract says (cu_q, cu_group, lengths) is reported and left alone: its
 // partition is empty, so nothing behind the arrays' ends is read or written.
 __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlanArgs p, dcut_plan::PlanArgs a) {
-    extern __shared__ long long prefix_s[];                   // [2 B + 1], then cu_q [B + 1] and own lengths [B]
+    extern __shared__ long long prefix_s[];                   // cu_q [B + 1] and own lengths [B] lie behind plan_longs(B) of these
     __shared__ long long ws64[33], ws64b[33];
     __shared__ int ws32[33], ws32b[33];
     const int tid = threadIdx.x, nthr = blockDim.x, B = a.B, G = p.n_groups;
-    int* cu_s = reinterpret_cast<int*>(prefix_s + 2 * B + 1);
+    __shared__ Seg segs_s[kMaxSegs + 1];
+    int* cu_s = reinterpret_cast<int*>(prefix_s + plan_longs(B));
+    const bool own_part = blockIdx.x == 0;
     int* own_s = cu_s + B + 1;
     dcut_pdl_wait();
     dcut_pdl_launch_dependents();
@@ -808,23 +816,32 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlanArgs p, dcu
         sound = __syncthreads_and(fits);
     }
     if (!packed || !sound) {
-        if (tid == 0) atomicExch(a.status, packed ? DCUT_DEV_BAD_GROUPS : DCUT_DEV_BAD_CU_Q);
-        for (int s = tid; s <= p.n_seg; s += nthr) {
-            p.segs[s] = Seg{G, 0, 0, 0};
-            if (s < p.n_seg) p.cuts[s] = Cut{0, 0, 0, 0};
+        if (!own_part) {
+            for (int s = tid; s <= p.n_seg; s += nthr) {
+                p.segs[s] = Seg{G, 0, 0, 0};
+                if (s < p.n_seg) p.cuts[s] = Cut{0, 0, 0, 0};
+            }
+            return;
         }
+        if (tid == 0) atomicExch(a.status, packed ? DCUT_DEV_BAD_GROUPS : DCUT_DEV_BAD_CU_Q);
         a.B = 0;
+    }
+    if (own_part) {
+        // dcut_verify_attn's work list on the own lengths
         a.cu_q = cu_s;
         a.ctx_lens = own_s;
         dcut_plan::attn_plan_body(a, prefix_s);
         return;
     }
+    long long* cost = prefix_s;                               // [G + 1]
+    Group* groups = B <= kSmemGroups ? reinterpret_cast<Group*>(prefix_s + ((B + 2) & ~1)) : p.groups;   // [G], 16-byte aligned
     // the groups and the cost of the stream before each
     const int per = (G + nthr - 1) / nthr, g0 = tid * per;
     long long mine = 0;
     for (int g = g0; g < g0 + per && g < G; ++g) {
         const int q0 = cu_s[p.cu_group[g]];
         const Group gr = {q0, cu_s[p.cu_group[g + 1]] - q0, p.prefix_lens[g], 0};
+        groups[g] = gr;
         p.groups[g] = gr;
         mine += a.n_kv_heads * head_cost(gr, p.group_size);
     }
@@ -832,54 +849,62 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlanArgs p, dcu
     dcut_plan::plan_block_exclusive_scan4(dcut_plan::PlanScan4{0, 0, mine, 0}, ws32, ws32b, ws64, ws64b, o, t);
     long long before = o.c0;
     for (int g = g0; g < g0 + per && g < G; ++g) {
-        p.cost[g] = before;
-        before += a.n_kv_heads * head_cost(p.groups[g], p.group_size);
+        cost[g] = before;
+        before += a.n_kv_heads * head_cost(groups[g], p.group_size);
     }
-    if (tid == 0) p.cost[G] = t.c0;
+    if (tid == 0) cost[G] = t.c0;
     __syncthreads();
-    for (int s = tid; s <= p.n_seg; s += nthr) p.segs[s] = boundary(s, p.n_seg, p.groups, p.cost, G, p.group_size, a.n_kv_heads);
+    for (int s = tid; s <= p.n_seg; s += nthr) p.segs[s] = segs_s[s] = boundary(s, p.n_seg, groups, cost, G, p.group_size, a.n_kv_heads);
     __syncthreads();
-    for (int b = tid; b < p.n_seg; b += nthr) p.cuts[b] = cut_at(b, p.n_seg, p.segs, p.groups, G, p.group_size);
-    // the own parts: dcut_verify_attn's work list on the own lengths
-    a.cu_q = cu_s;
-    a.ctx_lens = own_s;
-    dcut_plan::attn_plan_body(a, prefix_s);
+    for (int b = tid; b < p.n_seg; b += nthr) p.cuts[b] = cut_at(b, p.n_seg, segs_s, groups, G, p.group_size);
 }
 
 // ------------------------------------------------------------------------------------------------ merge of cut items
 
-// grid: x: boundary b = blockIdx.x + 1; y: 32 rows of the unit's 256; a warp per row
+// grid: x: boundary b = blockIdx.x + 1; y: 16 of the unit's 256 rows; 16 threads per row.  One prefix in a small batch is a
+// single item per kv head, cut into a segment for every SM: the pieces of 8 heads are then all there is to merge, and with
+// one or two CTAs per boundary 8 or 16 SMs read everything (15 us for 16 single tokens of 32q/8kv heads).
+constexpr int kCombineThreads = 256, kCombineY = kSlotRows / (kCombineThreads / 16);
 template <int DH>
-__global__ void __launch_bounds__(1024) prefix_combine_kernel(PrefixArgs a, const Cut* cuts) {
+__global__ void __launch_bounds__(kCombineThreads) prefix_combine_kernel(PrefixArgs a, const Cut* cuts) {
     dcut_pdl_wait();
     dcut_pdl_launch_dependents();
-    constexpr int kPer = DH / 32;
-    const int b = blockIdx.x + 1, lane = threadIdx.x & 31, R = blockIdx.y * 32 + (threadIdx.x >> 5);
+    constexpr int kVec = DH / 64;                                        // float4 per thread
+    const int b = blockIdx.x + 1, c0 = (threadIdx.x & 15) * (DH / 16);
     const Cut cut = cuts[b];
+    if (cut.pieces == 0) return;
     const int gs = a.group_size, tpt = tile_tokens(gs);
+    const int R = blockIdx.y * (kCombineThreads / 16) + (threadIdx.x >> 4);
     const int r = R & (kTileRows - 1), tok = (R / kTileRows) * tpt + r / gs;
-    if (cut.pieces == 0 || r / gs >= tpt || tok >= cut.tokens) return;
-    const int orow = (cut.q0 + tok) * a.n_q_heads + cut.kv_head * gs + r % gs;
-    const float own = a.own_lse[orow];
+    if (r / gs >= tpt || tok >= cut.tokens) return;
+    const size_t orow = (size_t)(cut.q0 + tok) * a.n_q_heads + cut.kv_head * gs + r % gs;
     auto prow = [&](int i) { return (size_t)(i == 0 ? 2 * (b - 1) + 1 : 2 * (b + i - 1)) * kSlotRows + R; };
-    float top = own;
-    for (int i = 0; i < cut.pieces; ++i) top = fmaxf(top, a.part_lse[prow(i)]);
-    float acc[kPer], sum = 0.0f;
-    const float w_own = top == -INFINITY ? 0.0f : exp2f((own - top) * kLog2e);
+    const float own = a.own_lse[orow];
+    float4 acc[kVec];
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) acc[e] = w_own * a.own_o[(size_t)orow * DH + lane * kPer + e];
-    sum = w_own;
+    for (int v = 0; v < kVec; ++v) acc[v] = *reinterpret_cast<const float4*>(a.own_o + orow * DH + c0 + 4 * v);
+    float top = own;
+#pragma unroll 4
+    for (int i = 0; i < cut.pieces; ++i) top = fmaxf(top, a.part_lse[prow(i)]);
+    float sum = top == -INFINITY ? 0.0f : exp2f((own - top) * kLog2e);
+#pragma unroll
+    for (int v = 0; v < kVec; ++v) acc[v].x *= sum, acc[v].y *= sum, acc[v].z *= sum, acc[v].w *= sum;
+#pragma unroll 4
     for (int i = 0; i < cut.pieces; ++i) {
         const size_t pr = prow(i);
         const float l = a.part_lse[pr], wgt = l == -INFINITY ? 0.0f : exp2f((l - top) * kLog2e);
         sum += wgt;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] += wgt * a.part_o[pr * DH + lane * kPer + e];
+        for (int v = 0; v < kVec; ++v) {
+            const float4 x = *reinterpret_cast<const float4*>(a.part_o + pr * DH + c0 + 4 * v);
+            acc[v].x += wgt * x.x, acc[v].y += wgt * x.y, acc[v].z += wgt * x.z, acc[v].w += wgt * x.w;
+        }
     }
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
-    for (int e = 0; e < kPer; e += 2) *reinterpret_cast<uint32_t*>(a.out + (size_t)orow * DH + lane * kPer + e) = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
-    if (a.lse && lane == 0) a.lse[orow] = sum > 0.0f ? top + logf(sum) : -INFINITY;
+    for (int v = 0; v < kVec; ++v)
+        *reinterpret_cast<uint2*>(a.out + orow * DH + c0 + 4 * v) = make_uint2(pack_bf16(acc[v].x * inv, acc[v].y * inv), pack_bf16(acc[v].z * inv, acc[v].w * inv));
+    if (a.lse && c0 == 0) a.lse[orow] = sum > 0.0f ? top + logf(sum) : -INFINITY;
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -908,17 +933,15 @@ dcut_status launch_prefix(dcut_ctx* ctx, const CUtensorMap& qm, const CUtensorMa
     dcut_status st = dcut_check_cuda(ctx, dcut_launch_pdl(prefix_attn_kernel<DH>, dim3(ctx->sm_count), dim3(kThreads), Smem<DH>::kTotal, stream,
                                                           qm, km, vm, a), "launch prefix_attn_kernel");
     if (st != DCUT_OK || ctx->sm_count < 2) return st;
-    return dcut_check_cuda(ctx, dcut_launch_pdl(prefix_combine_kernel<DH>, dim3(ctx->sm_count - 1, kSlotRows / 32), dim3(1024), 0, stream, a, cuts),
+    return dcut_check_cuda(ctx, dcut_launch_pdl(prefix_combine_kernel<DH>, dim3(ctx->sm_count - 1, kCombineY), dim3(kCombineThreads), 0, stream, a, cuts),
                            "launch prefix_combine_kernel");
 }
 
-size_t plan_smem(int B) { return sizeof(long long) * (2 * (size_t)B + 1) + sizeof(int) * (2 * (size_t)B + 1); }
 
 // the context's scratch for these calls, one allocation
 struct Scratch {
     float *own_o, *own_lse, *part_o, *part_lse;
     Group* groups;
-    long long* cost;
     Seg* segs;
     Cut* cuts;
 };
@@ -935,7 +958,6 @@ size_t carve(const dcut_ctx* c, unsigned char* base, Scratch* s) {
     s->part_o = reinterpret_cast<float*>(take(slots * c->lim.head_dim * sizeof(float)));
     s->part_lse = reinterpret_cast<float*>(take(slots * sizeof(float)));
     s->groups = reinterpret_cast<Group*>(take(sizeof(Group) * ((size_t)c->lim.max_B + 1)));
-    s->cost = reinterpret_cast<long long*>(take(sizeof(long long) * ((size_t)c->lim.max_B + 1)));
     s->segs = reinterpret_cast<Seg*>(take(sizeof(Seg) * ((size_t)c->sm_count + 1)));
     s->cuts = reinterpret_cast<Cut*>(take(sizeof(Cut) * ((size_t)c->sm_count + 1)));
     return off;
@@ -945,6 +967,7 @@ size_t carve(const dcut_ctx* c, unsigned char* base, Scratch* s) {
 
 dcut_status dcut_enable_prefix(dcut_ctx* ctx, int max_groups) {
     if (max_groups > ctx->prefix_max_groups) ctx->prefix_max_groups = max_groups;
+    if (ctx->sm_count > kMaxSegs) return dcut_fail(ctx, DCUT_ECAPACITY, "%d SMs: the partition is made for %d", ctx->sm_count, kMaxSegs);
     if (ctx->prefix_scratch) return DCUT_OK;   // (it has room for max_B groups: captured graphs keep their pointers)
     ctx->prefix_max_groups = 0;
     cudaError_t e = cudaFuncSetAttribute(prefix_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<128>::kTotal);
@@ -979,14 +1002,13 @@ dcut_status dcut_launch_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_
     pp.max_rows = l.max_gamma + 1;
     pp.T_cap = T_cap;
     pp.groups = s.groups;
-    pp.cost = s.cost;
     pp.segs = s.segs;
     pp.cuts = s.cuts;
     pp.n_seg = ctx->sm_count;
     dcut_plan::PlanArgs pa;
     dcut_fill_plan_args(ctx, ctx_lens, cu_q, B, &pa);
     ctx->plan_cu_q = nullptr;                  // the context's work list now belongs to this call's own parts
-    if ((st = dcut_check_cuda(ctx, dcut_launch_pdl(prefix_plan_kernel, dim3(1), dim3(B <= 256 ? 256 : 1024), plan_smem(B), stream, pp, pa),
+    if ((st = dcut_check_cuda(ctx, dcut_launch_pdl(prefix_plan_kernel, dim3(2), dim3(B <= 256 ? 256 : 1024), plan_smem(B), stream, pp, pa),
                               "launch prefix_plan_kernel")) != DCUT_OK) return st;
     if ((st = dcut_launch_verify_attn(ctx, q, k_cache, v_cache, num_pages, block_table, block_table_stride, ctx_lens, cu_q, B, T_cap, scale,
                                       out, s.own_lse, 1, s.own_o, stream)) != DCUT_OK) return st;
