@@ -161,10 +161,11 @@ def _heads(t: Optional[torch.Tensor], n_heads: int, head_dim: int):
     """(pointer, token stride, head stride) of a bf16 [tokens, heads, head_dim] view whose last dimension is dense."""
     if t is None:
         return None, 0, 0
+    shape, strides = t.shape, t.stride()
     assert t.is_cuda and t.dtype == torch.bfloat16, "expected a CUDA bf16 tensor"
-    assert t.dim() == 3 and t.shape[1] == n_heads and t.shape[2] == head_dim and t.stride(2) == 1, \
-        f"expected [tokens, {n_heads}, {head_dim}] with dense heads, got {tuple(t.shape)} with strides {t.stride()}"
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    assert len(shape) == 3 and shape[1] == n_heads and shape[2] == head_dim and strides[2] == 1, \
+        f"expected [tokens, {n_heads}, {head_dim}] with dense heads, got {tuple(shape)} with strides {strides}"
+    return t.data_ptr(), strides[0], strides[1]
 
 
 def _rows(t: Optional[torch.Tensor]):
@@ -193,7 +194,7 @@ class PrefixGroups:
 
 
 def _stream() -> int:
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def budget_from_ratio(B: int, gamma: int, num: int, den: int) -> int:
@@ -304,6 +305,7 @@ class Context:
         self.device = torch.cuda.current_device() if device is None else device
         self.limits = Limits(max_B, max_gamma, n_q_heads, n_kv_heads, head_dim, page_size, max_pages_per_req,
                              vocab, hidden, intermediate)
+        self._shape = (n_q_heads, n_kv_heads, head_dim)
         self._h = _vp(None)
         st = _lib.dcut_create(C.byref(self._h), C.byref(self.limits), self.device)
         if st != OK:
@@ -526,14 +528,12 @@ class Context:
                     groups: Optional[PrefixGroups] = None, q_out=None):
         """dcut_rope_append: rotates q and k ([tokens, heads, head_dim] views of any token and head stride) and appends k, v
         to the paged cache.  `inv_freq`: fp64 [rotary_dim / 2] (None: no rotation).  Returns q_out [T_cap, Hq, Dh]."""
-        l = self.limits
-        for t in (q, k, v):
-            assert t is None or t.shape[0] >= T_cap, "q, k and v need T_cap rows"
+        hq, hkv, d = self._shape
+        assert (q is None or q.shape[0] >= T_cap) and k.shape[0] >= T_cap and v.shape[0] >= T_cap, "q, k and v need T_cap rows"
         assert tok_req.shape[0] >= T_cap and tok_pos.shape[0] >= T_cap
         if q is not None and q_out is None:
-            q_out = torch.empty((T_cap, l.n_q_heads, l.head_dim), dtype=torch.bfloat16, device=k.device)
-        (qp, qt, qh), (kp, kt, kh), (vp, vt, vh) = (_heads(t, n, l.head_dim) for t, n in
-                                                    ((q, l.n_q_heads), (k, l.n_kv_heads), (v, l.n_kv_heads)))
+            q_out = torch.empty((T_cap, hq, d), dtype=torch.bfloat16, device=k.device)
+        (qp, qt, qh), (kp, kt, kh), (vp, vt, vh) = _heads(q, hq, d), _heads(k, hkv, d), _heads(v, hkv, d)
         x = Qkv(qp, kp, vp, qt, qh, kt, kh, vt, vh)
         r = Rope(_ptr(inv_freq, torch.float64), 2 * inv_freq.shape[0] if inv_freq is not None else 0, int(interleaved),
                  _ptr(q_gain, torch.bfloat16), _ptr(k_gain, torch.bfloat16), rms_eps)
