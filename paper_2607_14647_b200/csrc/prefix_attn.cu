@@ -587,6 +587,29 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
         // ---------------------------------------------------------------- epilogue
         const bool has = it.blocks > 0, whole = is_whole(it);
         float m_o = -INFINITY, l_o = 0.0f;                        // the other team's part of a single's row
+        // 16 columns of the warp's 32 rows at a time go through shared memory, so that global memory sees 64 bytes of a row
+        // at once; the own part is fetched a chunk ahead, the first while the last products run
+        const int c0 = it.dual ? 0 : team * (DH / 2), c1 = it.dual ? DH : c0 + DH / 2;
+        const int v = lane & 3, rsub = lane >> 2;                 // this lane's vector of four columns, its row of eight
+        const int orow = valid ? (it.q0 + tok) * a.n_q_heads + it.h * gs + row_head : 0;
+        int row[4];
+        bool row_ok[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 8 * i + rsub;
+            row[i] = __shfl_sync(0xffffffffu, orow, r);
+            row_ok[i] = __shfl_sync(0xffffffffu, (int)valid, r);
+        }
+        float4 own[4];
+        auto fetch = [&](float4 (&o)[4], int cc) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (whole && row_ok[i] && cc < c1) o[i] = *reinterpret_cast<const float4*>(a.own_o + (size_t)row[i] * DH + cc + 4 * v);
+            }
+        };
+        const float ls = whole && valid ? a.own_lse[orow] * kLog2e : 0.0f;
+        if (live) fetch(own, c0);
         if (has) {
             failed = !warp_wait(o_full, n_items & 1);
             if (!it.dual && !failed) failed = !warp_wait(smem_u32(c->o_full) + 8 * (team ^ 1), n_items & 1);
@@ -602,14 +625,12 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
             if (failed) break;
             tc_fence_after();
         }
-        const int orow = valid ? (it.q0 + tok) * a.n_q_heads + it.h * gs + row_head : 0;
         const float m_all = fmaxf(m_run, m_o);
         const float w_s = m_run == -INFINITY ? 0.0f : fast_exp2((m_run - m_all) * cs), w_o = m_o == -INFINITY ? 0.0f : fast_exp2((m_o - m_all) * cs);
         const float l_all = l_run * w_s + l_o * w_o;
         const float lp = l_all > 0.0f ? m_all * cs + log2f(l_all) : -INFINITY;             // in powers of two
         float f_s = l_all > 0.0f ? w_s / l_all : 0.0f, f_o = l_all > 0.0f ? w_o / l_all : 0.0f, f_own = 0.0f;
         if (whole) {
-            const float ls = valid ? a.own_lse[orow] * kLog2e : 0.0f;
             const float top = fmaxf(lp, ls), wp = top == -INFINITY ? 0.0f : exp2f(lp - top), wo = top == -INFINITY ? 0.0f : exp2f(ls - top);
             const float inv = wp + wo > 0.0f ? 1.0f / (wp + wo) : 0.0f;
             f_s *= wp * inv;
@@ -619,28 +640,10 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
         }
         const size_t prow0 = whole ? 0 : (size_t)slot_of(it, blockIdx.x) * kSlotRows + tile * kTileRows;
         if (!whole && valid && (it.dual || team == 0)) a.part_lse[prow0 + R] = lp * kLn2;
-        const int c0 = it.dual ? 0 : team * (DH / 2), c1 = it.dual ? DH : c0 + DH / 2;
-        const int v = lane & 3, rsub = lane >> 2;                 // this lane's vector of four columns, its row of eight
-        // 16 columns of the warp's 32 rows at a time go through shared memory, so that global memory sees 64 bytes of a row
-        // at once; the own part's columns are fetched two chunks ahead
-        int row[4];
-        bool row_ok[4];
         float f_row[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = 8 * i + rsub;
-            row[i] = __shfl_sync(0xffffffffu, orow, r);
-            row_ok[i] = __shfl_sync(0xffffffffu, (int)valid, r);
-            f_row[i] = __shfl_sync(0xffffffffu, f_own, r);
-        }
-        auto fetch = [&](float4 (&own)[4], int cc) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                own[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (whole && row_ok[i] && cc < c1) own[i] = *reinterpret_cast<const float4*>(a.own_o + (size_t)row[i] * DH + cc + 4 * v);
-            }
-        };
-        auto chunk = [&](const float4 (&own)[4], int cc) {
+        for (int i = 0; i < 4; ++i) f_row[i] = __shfl_sync(0xffffffffu, f_own, 8 * i + rsub);
+        auto chunk = [&](const float4 (&o)[4], int cc) {
             if (has) {
                 uint32_t os[16], oo[16];
                 tc_ld16(t_o + cc, os);
@@ -665,8 +668,8 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
                 if (!row_ok[i]) continue;
                 if (whole) {
                     *reinterpret_cast<uint2*>(a.out + (size_t)row[i] * DH + cc + 4 * v) =
-                        make_uint2(pack_bf16(fmaf(own[i].x, f_row[i], y.x), fmaf(own[i].y, f_row[i], y.y)),
-                                   pack_bf16(fmaf(own[i].z, f_row[i], y.z), fmaf(own[i].w, f_row[i], y.w)));
+                        make_uint2(pack_bf16(fmaf(o[i].x, f_row[i], y.x), fmaf(o[i].y, f_row[i], y.y)),
+                                   pack_bf16(fmaf(o[i].z, f_row[i], y.z), fmaf(o[i].w, f_row[i], y.w)));
                 } else {
                     *reinterpret_cast<float4*>(a.part_o + (prow0 + quarter * 32 + r) * DH + cc + 4 * v) = y;
                 }
@@ -674,15 +677,10 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
             __syncwarp();
         };
         if (live) {
-            float4 own0[4], own1[4];
-            fetch(own0, c0);
-            fetch(own1, c0 + 16);
 #pragma unroll 1
-            for (int cc = c0; cc < c1; cc += 32) {                // (32 divides a team's share of the columns)
-                chunk(own0, cc);
-                fetch(own0, cc + 32);
-                chunk(own1, cc + 16);
-                fetch(own1, cc + 48);
+            for (int cc = c0; cc < c1; cc += 16) {
+                chunk(own, cc);
+                fetch(own, cc + 16);
             }
         }
         if (has) {
