@@ -14,9 +14,14 @@
 //                         are staged by TMA as 128-byte-swizzled K-major tiles (BK = 64); one elected lane issues the
 //                         MMAs and releases stages with tcgen05.commit; two accumulators in tensor memory let the four
 //                         epilogue warps (tcgen05.ld) work on one tile while the next is being multiplied.
-//                         Epilogues: plain bf16, + residual, bias / activation / gate / residual (dcut_linear), SwiGLU (the B tile is 128 gate rows and the 128 matching
+//                         Epilogues: plain bf16, + residual, SwiGLU (the B tile is 128 gate rows and the 128 matching
 //                         up rows, so silu(g) * u is formed in registers and the [T, 2I] intermediate never exists),
-//                         or row argmax (the LM head fused with acceptance: the logits are never stored).
+//                         row argmax (the LM head fused with acceptance: the logits are never stored), or dcut_linear's:
+//                         bias, activation, gate and residual in fp32 for any N, K and row strides (the tensor maps' zero
+//                         fill completes the last tile and the last k-block).  Measured: 7 rows, K = 4096, N = 6144 with
+//                         bias 15 us (50 MB of weights: 8 us at the copy rate, the rest is fixed: launch, first loads, the
+//                         pair's exchange); 1088 rows to N = 12288 with gelu_tanh 110 us (its products alone 88; operands
+//                         from L2 bound them: 92 bytes per clock and SM at the full MMA rate, about 60 to be had).
 // M is ragged and known only on the device (T = cu_q[B]): grids are sized for T_cap, CTAs without work fall through,
 // rows past T are computed on whatever the buffers hold and never stored.  Every kernel is launched with programmatic
 // dependent launch and waits for its predecessor before touching global memory.
@@ -55,12 +60,11 @@ __host__ __device__ constexpr int bn_of(int i) { return BN - 32 * i; }
 struct BMaps {
     CUtensorMap m[kNumBn];
 };
-// The activations' tensor map with the full 128-row box, a 64-row box and a 16-row box: with at most 64 (16) packed rows
-// the rest of a tile would only be fetched to be ignored (at T = 64 the A tiles were more than half of what the SMs took in).
+// The activations' tensor map with the full 128-row box and with a 64-row box: with at most 64 packed rows a tile's
+// lower half would only be fetched to be ignored (at T = 64 the A tiles were more than half of what the SMs took in).
 struct AMaps {
-    CUtensorMap full, half, small;
+    CUtensorMap full, half;
 };
-constexpr int kSmallRows = 16;
 constexpr unsigned kBnMaskAll = (1u << kNumBn) - 1;
 constexpr int kPlanRows = 72;
 constexpr int kSplitCost = 50;             // gemm_plan: what the exchange of partial sums between the two SMs costs
@@ -553,7 +557,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
     if (threadIdx.x == 32) {                     // the tensor maps that the largest packed length would use
         const int m = g.plan_by_m[kPlanRows - 1];
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&a_maps.full)) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&a_maps.small)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&a_maps.half)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(pick_map(b_maps, m & 7))) : "memory");
         if (is_gated(MODE)) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(pick_map(b2_maps, m & 7))) : "memory");
     }
@@ -568,11 +572,11 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
         if (blockIdx.x == 0 && threadIdx.x == 0) atomicExch(g.status, DCUT_DEV_BAD_ROWS);
     }
     const int T = T_packed;
-    // rows 16..127 or 64..127 of the A tile are not loaded when no row of them exists: the MMA reads there whatever shared
-    // memory holds (with small stages, parts of the following ones), and the accumulator rows computed from them are never
-    // stored (one-SM and split modes; a pair always loads full boxes)
-    const CUtensorMap* a_map1 = T <= kSmallRows ? &a_maps.small : T <= BM / 2 ? &a_maps.half : &a_maps.full;
-    const uint32_t a_bytes = T <= kSmallRows ? kSmallRows * BK * 2 : T <= BM / 2 ? kATile / 2 : kATile;
+    // rows 64..127 of the A tile are not loaded when no row of them exists: they hold whatever shared memory held, and
+    // the accumulator rows computed from them are never stored (one-SM and split modes; a pair always loads full boxes)
+    const bool a_half = T <= BM / 2;
+    const CUtensorMap* a_map1 = a_half ? &a_maps.half : &a_maps.full;
+    const uint32_t a_bytes = a_half ? kATile / 2 : kATile;
     const int m_blocks = (T + BM - 1) / BM;
     const int plan_all = m_blocks > 0 ? g.plan_by_m[(m_blocks < kPlanRows ? m_blocks : kPlanRows) - 1] : 0;
     const bool split = plan_all >= kPlanSplit;                      // the pair shares one 128-row tile, half of K each
@@ -585,7 +589,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
     // 64-wide tile at T <= 64 moves 8 KB of weights per stage: with four stages too few bytes were in flight per SM to
     // cover the DRAM latency)
     const uint32_t stage_stride = a_bytes + (uint32_t)bn * BK * 2;                         // multiples of 1 KB
-    const int n_stages = min(kMaxStages, 1 + (int)(((uint32_t)(kGemmStages * kGemmStageBytes) - max(stage_stride, (uint32_t)kATile)) / stage_stride));
+    const int n_stages = min(kMaxStages, (int)((uint32_t)(kGemmStages * kGemmStageBytes) / stage_stride));
     if (warp == 1) {   // tensor memory: two 128 x 256 fp32 accumulators (per CTA; allocated for the pair in pair mode)
         if (pairs) {
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "n"(kTmemCols) : "memory");
@@ -1076,8 +1080,7 @@ dcut_status make_kmajor_map(dcut_ctx* ctx, CUtensorMap* map, const void* base, l
 dcut_status make_act_maps(dcut_ctx* ctx, AMaps* maps, const void* base, long long rows, long long cols, long long ld = 0) {
     dcut_status st = make_kmajor_map(ctx, &maps->full, base, rows, cols, BM, ld);
     if (st != DCUT_OK) return st;
-    if ((st = make_kmajor_map(ctx, &maps->half, base, rows, cols, BM / 2, ld)) != DCUT_OK) return st;
-    return make_kmajor_map(ctx, &maps->small, base, rows, cols, kSmallRows, ld);
+    return make_kmajor_map(ctx, &maps->half, base, rows, cols, BM / 2, ld);
 }
 
 // The weight's tensor maps for the tile widths in `mask` (box = half the width in rows)
