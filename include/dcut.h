@@ -136,7 +136,7 @@ dcut_status dcut_select(dcut_ctx* ctx, const float* conf, int B, int gamma, cons
  * For request i, packed token t = 0..d_i (d_i = cu_q[i+1]-cu_q[i]-1), query head h:
  *   out = softmax_j( q . k_j * scale ) v_j  over cache positions j = 0 .. L_i + t,
  * reading kv head h / (n_q_heads / n_kv_heads).  The K/V of the 1 + d_i new tokens must already
- * be in the cache at positions L_i .. L_i + d_i.  bf16 in, fp32 accumulate, bf16 out.
+ * be in the cache at positions L_i .. L_i + d_i; slots behind them may hold anything.  bf16 in, fp32 accumulate, bf16 out.
  * DEVICE in:  q bf16 [T, n_q_heads, head_dim]; k_cache, v_cache (layout above, num_pages pages);
  *             block_table i32 [B, block_table_stride]; ctx_lens i32 [B] (= L_i); cu_q i32 [B+1].
  * DEVICE out: out bf16 [T, n_q_heads, head_dim]; lse fp32 [T, n_q_heads] (natural log of the
@@ -475,7 +475,7 @@ dcut_status dcut_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_cache, 
  * DEVICE: a [T_cap rows readable, K] with lda elements from row to row, w and w2 [N, K] with ldw; both strides multiples of 8
  * and >= K, bases 16-byte aligned.  bias, bias2 [N] or NULL; residual [T, N] with ldr or NULL; out [T, N] with ldo (>= N; any
  * alignment: 16-byte aligned rows are stored in vectors).  out may be the residual itself (same stride); it must not
- * overlap a or the weights.  The struct is HOST memory, read during the call.  Needs a context with attention shapes;
+ * overlap the inputs in any other way.  The struct is HOST memory, read during the call.  Needs a context with attention shapes;
  * N, K and T_cap are not bound by dcut_limits.
  */
 typedef enum { DCUT_ACT_NONE = 0, DCUT_ACT_RELU = 1, DCUT_ACT_GELU = 2, DCUT_ACT_GELU_TANH = 3, DCUT_ACT_SILU = 4 } dcut_act;
