@@ -326,7 +326,7 @@ dcut_status dcut_verify_attn(dcut_ctx* c, const void* q, const void* k_cache, co
         return dcut_fail(c, DCUT_ECAPACITY, "cache has too many token rows for 32-bit tile coordinates");
     if (!(scale > 0.0f) || isinf(scale)) return dcut_fail(c, DCUT_EINVAL, "scale must be positive and finite");
     return dcut_launch_verify_attn(c, q, k_cache, v_cache, num_pages, block_table, block_table_stride, ctx_lens, cu_q, B,
-                                   T_cap, scale, out, lse, 0, nullptr, static_cast<cudaStream_t>(stream));
+                                   T_cap, scale, out, lse, 0, nullptr, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 dcut_status dcut_accept(dcut_ctx* c, const void* logits, int V, const int* draft_ids, const int* cu_q, int B, int gamma,

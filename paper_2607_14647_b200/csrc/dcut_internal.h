@@ -206,10 +206,11 @@ dcut_status dcut_launch_accept_rs(dcut_ctx* ctx, const void* target_logits, cons
                                   const int* draft_ids, const int* cu_q, int B, int gamma, int T_cap,
                                   const float* u_accept, const float* u_sample, int* accept_len, int* bonus,
                                   int* out_tokens, int* n_accepted_total, float* prob, cudaStream_t stream);
+namespace dcut_plan { struct PlanArgs; }
 dcut_status dcut_launch_verify_attn(dcut_ctx* ctx, const void* q, const void* k_cache, const void* v_cache,
                                     long long num_pages, const int* block_table, int block_table_stride,
                                     const int* ctx_lens, const int* cu_q, int B, int T_cap, float scale,
-                                    void* out, float* lse, int reuse_plan, float* out_f32, cudaStream_t stream);
+                                    void* out, float* lse, int reuse_plan, const dcut_plan::PlanArgs* list, float* out_f32, cudaStream_t stream);
 // tensor maps of the paged cache: whole (page, kv head) tiles, and the K tiles of the tcgen05 paths (head_dim 128)
 struct CUtensorMap_st;
 dcut_status dcut_make_cache_map(dcut_ctx* ctx, CUtensorMap_st* map, const void* base, long long num_pages);

@@ -787,7 +787,7 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlanArgs p, dcu
     __shared__ long long ws64[33], ws64b[33];
     __shared__ int ws32[33], ws32b[33];
     const int tid = threadIdx.x, nthr = blockDim.x, B = a.B, G = p.n_groups;
-    __shared__ Seg segs_s[kMaxSegs + 1];
+    __shared__ Seg segs_s[kMaxSegs + 1];                      // (dcut_create bounds the SMs)
     int* cu_s = reinterpret_cast<int*>(prefix_s + plan_longs(B));
     const bool own_part = blockIdx.x == 0;
     int* own_s = cu_s + B + 1;
@@ -947,6 +947,10 @@ struct Scratch {
     Group* groups;
     Seg* segs;
     Cut* cuts;
+    AttnEntry* entries;           // the own parts' work list
+    AttnSeg* own_segs;
+    AttnCut* own_cuts;
+    int* plan;
 };
 size_t carve(const dcut_ctx* c, unsigned char* base, Scratch* s) {
     size_t off = 0;
@@ -963,6 +967,10 @@ size_t carve(const dcut_ctx* c, unsigned char* base, Scratch* s) {
     s->groups = reinterpret_cast<Group*>(take(sizeof(Group) * ((size_t)c->lim.max_B + 1)));
     s->segs = reinterpret_cast<Seg*>(take(sizeof(Seg) * ((size_t)c->sm_count + 1)));
     s->cuts = reinterpret_cast<Cut*>(take(sizeof(Cut) * ((size_t)c->sm_count + 1)));
+    s->entries = reinterpret_cast<AttnEntry*>(take(sizeof(AttnEntry) * (size_t)c->max_entries));
+    s->own_segs = reinterpret_cast<AttnSeg*>(take(sizeof(AttnSeg) * ((size_t)c->sm_count + 1)));
+    s->own_cuts = reinterpret_cast<AttnCut*>(take(sizeof(AttnCut) * ((size_t)c->sm_count + 1)));
+    s->plan = reinterpret_cast<int*>(take(sizeof(int) * 16));
     return off;
 }
 
@@ -970,7 +978,6 @@ size_t carve(const dcut_ctx* c, unsigned char* base, Scratch* s) {
 
 dcut_status dcut_enable_prefix(dcut_ctx* ctx, int max_groups) {
     if (max_groups > ctx->prefix_max_groups) ctx->prefix_max_groups = max_groups;
-    if (ctx->sm_count > kMaxSegs) return dcut_fail(ctx, DCUT_ECAPACITY, "%d SMs: the partition is made for %d", ctx->sm_count, kMaxSegs);
     if (ctx->prefix_scratch) return DCUT_OK;   // (it has room for max_B groups: captured graphs keep their pointers)
     ctx->prefix_max_groups = 0;
     cudaError_t e = cudaFuncSetAttribute(prefix_attn_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<128>::kTotal);
@@ -1010,11 +1017,16 @@ dcut_status dcut_launch_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_
     pp.n_seg = ctx->sm_count;
     dcut_plan::PlanArgs pa;
     dcut_fill_plan_args(ctx, ctx_lens, cu_q, B, &pa);
-    ctx->plan_cu_q = nullptr;                  // the context's work list now belongs to this call's own parts
+    // (a list of its own: the context's may be one that a selector has left for dcut_verify_attn, and a replayed graph could
+    // not tell the host that it is gone)
+    pa.entries = s.entries;
+    pa.segs = s.own_segs;
+    pa.cuts = s.own_cuts;
+    pa.plan = s.plan;
     if ((st = dcut_check_cuda(ctx, dcut_launch_pdl(prefix_plan_kernel, dim3(2), dim3(B <= 256 ? 256 : 1024), plan_smem(B), stream, pp, pa),
                               "launch prefix_plan_kernel")) != DCUT_OK) return st;
     if ((st = dcut_launch_verify_attn(ctx, q, k_cache, v_cache, num_pages, block_table, block_table_stride, ctx_lens, cu_q, B, T_cap, scale,
-                                      out, s.own_lse, 1, s.own_o, stream)) != DCUT_OK) return st;
+                                      out, s.own_lse, 0, &pa, s.own_o, stream)) != DCUT_OK) return st;
 
     PrefixArgs a;
     a.prefix_table = groups->prefix_table;

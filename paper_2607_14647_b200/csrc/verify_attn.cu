@@ -1893,7 +1893,7 @@ void dcut_fill_plan_args(dcut_ctx* ctx, const int* ctx_lens, const int* cu_q, in
 dcut_status dcut_launch_verify_attn(dcut_ctx* ctx, const void* q, const void* k_cache, const void* v_cache,
                                     long long num_pages, const int* block_table, int block_table_stride,
                                     const int* ctx_lens, const int* cu_q, int B, int T_cap, float scale,
-                                    void* out, float* lse, int reuse_plan, float* out_f32, cudaStream_t stream) {
+                                    void* out, float* lse, int reuse_plan, const dcut_plan::PlanArgs* list, float* out_f32, cudaStream_t stream) {
     CUtensorMap km, vm, k2m;
     dcut_status st = dcut_make_cache_map(ctx, &km, k_cache, num_pages);
     if (st != DCUT_OK) return st;
@@ -1903,10 +1903,11 @@ dcut_status dcut_launch_verify_attn(dcut_ctx* ctx, const void* q, const void* k_
     if (ctx->lim.head_dim == 128 && (st = dcut_make_k_group_map(ctx, &k2m, k_cache, num_pages)) != DCUT_OK) return st;
 
     PlanArgs pa;
-    dcut_fill_plan_args(ctx, ctx_lens, cu_q, B, &pa);
+    if (list) pa = *list;    // the caller has made the work list, in buffers of its own
+    else dcut_fill_plan_args(ctx, ctx_lens, cu_q, B, &pa);
     // the selector may have left the work list of exactly this batch ready (dcut_enable_plan_in_select)
     if (ctx->plan_in_select && ctx->plan_cu_q == cu_q && ctx->plan_ctx_lens == ctx_lens && ctx->plan_B == B) reuse_plan = 1;
-    if (!reuse_plan) {   // reuse_plan: the previous launch on this stream had the same ctx_lens, cu_q and B (its work list stands)
+    if (!list && !reuse_plan) {   // reuse_plan: the previous launch on this stream had the same ctx_lens, cu_q and B (its work list stands)
         ctx->plan_cu_q = nullptr;   // the list now belongs to this call's batch
         st = dcut_check_cuda(ctx, dcut_launch_pdl(attn_plan_kernel, dim3(1), dim3(B <= 256 ? 256 : kPlanThreads),
                                                   sizeof(long long) * (2 * B + 1) + sizeof(int) * (2 * B + 1), stream, pa),
@@ -1920,9 +1921,9 @@ dcut_status dcut_launch_verify_attn(dcut_ctx* ctx, const void* q, const void* k_
     aa.block_table_stride = block_table_stride;
     aa.ctx_lens = ctx_lens;
     aa.cu_q = cu_q;
-    aa.entries = ctx->d_entries;
-    aa.segs = ctx->d_segs;
-    aa.plan = ctx->d_plan;
+    aa.entries = pa.entries;
+    aa.segs = pa.segs;
+    aa.plan = pa.plan;
     aa.n_q_heads = ctx->lim.n_q_heads;
     aa.n_kv_heads = ctx->lim.n_kv_heads;
     aa.num_pages = num_pages;
@@ -1937,7 +1938,7 @@ dcut_status dcut_launch_verify_attn(dcut_ctx* ctx, const void* q, const void* k_
     aa.status = ctx->d_status;
 
     CombineArgs ca;
-    ca.cuts = ctx->d_cuts;
+    ca.cuts = pa.cuts;
     ca.part_o = ctx->d_part_o;
     ca.part_lse = ctx->d_part_lse;
     ca.n_q_heads = ctx->lim.n_q_heads;

@@ -191,7 +191,7 @@ def test_the_same_bits_every_time_and_between_other_calls():
 
 
 def test_plan_in_select_is_not_used_for_the_own_parts_nor_left_stale():
-    """The list that a selector leaves for dcut_verify_attn is another one: a shared-prefix call in between takes its place."""
+    """The list that a selector leaves for dcut_verify_attn is another one, and outlives a shared-prefix call in between."""
     c = make_case(14, [3, 2, 4, 1], [40, 100, 7, 0], [4], [0], 8, 2, 128)
     ctx = make_ctx(c, max_gamma=3)
     ctx.enable_plan_in_select(True)
@@ -348,3 +348,29 @@ def test_verify_attn_with_unwritten_slots(hq, hkv, d, deep):
     ctx = make_ctx(c)
     out = ctx.verify_attn(c["q"], c["kc"], c["vc"], _i32(c["table"]), _i32(c["ctx"]), _i32(c["cu"]), c["cap"])
     check(c, out, None)
+
+
+def test_a_replayed_call_leaves_the_selector_s_list_alone():
+    """The host cannot see a replay: the list that a selector left has to survive a captured shared-prefix call."""
+    c = make_case(15, [3, 2, 4, 1], [40, 100, 7, 0], [3, 1], [33, 0], 8, 2, 128)
+    ctx = make_ctx(c, max_gamma=3)
+    ctx.enable_plan_in_select(True)
+    ctx.set_cost_dense(np.linspace(1, 1.1, 20).astype(np.float32))
+    conf, z, a = torch.full((4, 3), 0.9, device="cuda"), torch.zeros((4, 3), dtype=torch.int32, device="cuda"), device_args(c)
+    bonus, out = z[:, 0].contiguous(), torch.zeros_like(c["q"])
+    ctx.prefix_attn(c["q"], c["kc"], c["vc"], out=out, **a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.prefix_attn(c["q"], c["kc"], c["vc"], out=out, **a)
+    kc, vc = c["kc"].nan_to_num(), c["vc"].nan_to_num()
+    table = _i32(np.tile(np.arange(c["kc"].shape[0]), (4, 1)))[:, : a["block_table"].shape[1]].contiguous()
+    sel = ctx.select(conf, z, bonus, a["ctx_lens"])
+    T = int(sel.cu_q[-1])
+    q = torch.randn((T, 8, 128), device="cuda").to(torch.bfloat16)
+    want = ctx.verify_attn(q, kc, vc, table, a["ctx_lens"], sel.cu_q, T).clone()
+    sel = ctx.select(conf, z, bonus, a["ctx_lens"])
+    graph.replay()
+    got = ctx.verify_attn(q, kc, vc, table, a["ctx_lens"], sel.cu_q, T)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
