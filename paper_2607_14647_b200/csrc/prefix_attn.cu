@@ -168,6 +168,24 @@ __device__ __forceinline__ float fast_exp2(float x) {     // 2 ulp; -inf -> 0
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ unsigned long long pack_f32x2(float lo, float hi) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack_f32x2(unsigned long long v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ unsigned long long fma_f32x2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ unsigned long long add_f32x2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 __device__ __forceinline__ float fmax3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -515,19 +533,24 @@ __device__ __noinline__ bool softmax_steps(const Steps p, unsigned char* smem_ri
             }
         }
         const float cs = p.cs, mc = (m_run == -INFINITY ? 0.0f : m_run) * cs;
-        float sum4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const unsigned long long cs2 = pack_f32x2(cs, cs), nmc2 = pack_f32x2(-mc, -mc);
+        unsigned long long sum2[2] = {0ull, 0ull};                // four partial sums, two per register pair
         uint32_t pw[kBlock / 2];
 #pragma unroll
         for (int e = 0; e < kBlock / 2; ++e) {
-            const float p0 = fast_exp2(fmaf(__uint_as_float(sr[2 * e]), cs, -mc)), p1 = fast_exp2(fmaf(__uint_as_float(sr[2 * e + 1]), cs, -mc));
-            sum4[(2 * e) & 3] += p0;
-            sum4[(2 * e + 1) & 3] += p1;
+            float x0, x1;
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sr[2 * e]), __uint_as_float(sr[2 * e + 1])), cs2, nmc2), x0, x1);
+            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+            sum2[e & 1] = add_f32x2(sum2[e & 1], pack_f32x2(p0, p1));
             pw[e] = pack_bf16(p0, p1);
         }
         tc_st32(t_s, pw);                                         // P over the first half of S
         // (asked for now, read at the next step's beginning: the answer takes more than 100 cycles)
         s_over = lane == 0 && s + 1 < p.steps && mbar_test(p.s_full + 8 * ((n + 1) & 1), ((n + 1) >> 1) & 1);
-        l_run += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
+        float s0, s1, s2, s3;
+        unpack_f32x2(sum2[0], s0, s1);
+        unpack_f32x2(sum2[1], s2, s3);
+        l_run += (s0 + s1) + (s2 + s3);
         tc_wait_st();
         tc_fence_before();
         warp_arrive(p_bar);
