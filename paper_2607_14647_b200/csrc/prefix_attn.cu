@@ -420,7 +420,15 @@ __device__ __forceinline__ void issue(const PrefixArgs& a, unsigned char* smem, 
             if (more) qk(s + 2 == steps - 1);
         }
         if (!ok) break;
-        if (steps == 0) tc_commit(smem_u32(&c->q_free));                      // (a single's second team may have no block)
+        if (steps == 0) {                                                     // (a single's second team may have no block)
+            tc_commit(smem_u32(&c->q_free));
+            // The softmax warps have seen the item before end: o_full would otherwise run a phase ahead of a warp that still
+            // has to look at it, and a parity wait cannot tell two phases from none.
+            if (n_items > 0 && !wait(smem_u32(&c->o_free), n_items - 1)) {
+                ok = false;
+                break;
+            }
+        }
         tc_commit(o_full);
         const int pos = base + 2 * nblk;
         base = pos % kSlots;

@@ -374,3 +374,24 @@ def test_a_replayed_call_leaves_the_selector_s_list_alone():
     got = ctx.verify_attn(q, kc, vc, table, a["ctx_lens"], sel.cu_q, T)
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("B,size", [(4096, 2), (4097, 1), (6000, 100)])
+def test_thousands_of_requests(B, size):
+    """More requests and groups than the plan keeps in shared memory, and the most that it does."""
+    rng = np.random.default_rng(B)
+    sizes = [size] * (B // size) + ([B % size] if B % size else [])
+    c = make_case(B, rng.integers(1, 3, B), rng.integers(0, 20, B), sizes, rng.integers(0, 40, len(sizes)), 1, 1, 64)
+    check(c, *run(c))
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 128), (2, 2, 64), (9, 1, 128)])
+@pytest.mark.parametrize("longest", [64, 200, 600])
+def test_many_short_items_per_segment(longest, hq, hkv, d):
+    """Several items behind one another in every CTA: with no block, one (the second team has none), a few; cut and whole."""
+    rng = np.random.default_rng(longest + hq)
+    sizes = rng.integers(0, 4, 700)
+    B = int(sizes.sum())
+    plens = rng.integers(0, longest + 1, 700)
+    c = make_case(longest, rng.integers(1, 4, B), rng.integers(0, 40, B), sizes, plens, hq, hkv, d)
+    check(c, *run(c))
