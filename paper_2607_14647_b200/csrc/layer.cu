@@ -49,6 +49,7 @@ constexpr int kWaitLimit = 1 << 22;
 
 enum GemmMode { kPlain = 0, kResidual = 1, kSwiGLU = 2, kArgmax = 3, kLinear = 4, kLinearGated = 5 };
 __host__ __device__ constexpr bool is_gated(int mode) { return mode == kSwiGLU || mode == kLinearGated; }        // two weights share a tile
+__host__ __device__ constexpr bool is_linear(int mode) { return mode == kLinear || mode == kLinearGated; }
 __host__ __device__ constexpr bool may_split_k(int mode) { return mode == kPlain || mode == kResidual || mode == kLinear; }
 
 // Widths of the output tile that the one-SM mode may use: 256, 224, ..., 64 columns.  A narrower tile costs a little
@@ -68,6 +69,11 @@ struct AMaps {
 constexpr unsigned kBnMaskAll = (1u << kNumBn) - 1;
 constexpr int kPlanRows = 72;
 constexpr int kSplitCost = 50;             // gemm_plan: what the exchange of partial sums between the two SMs costs
+// dcut_linear with few k-blocks: one SM per tile only.  gemm_plan is fitted to K of 4096 and more; with up to 512 a tile's cost is
+// its epilogue and the start, which pairs and split K make dearer.  One SM against the plan's choice with them, us, no
+// activation: K = 64, 8 x 6147 6.0 / 8.1, 333 x 6147 9.1 / 12.3; K = 384, 333 x 2048 6.0 / 7.0, 8 x 2048 5.6 / 5.2; K = 640,
+// 8 x 2048 6.5 / 5.7, 700 x 6147 18.2 / 19.0.
+constexpr int kShortK = 512;
 constexpr unsigned kBnMaskSwiGLU = 0x55;   // widths whose halves are whole 32-column epilogue steps: 256, 192, 128, 64
 
 // ------------------------------------------------------------------------------------------------ PTX
@@ -313,7 +319,7 @@ __device__ __forceinline__ void linear_finish32(const GemmArgs& g, int T, int ro
 // past N_out (a ragged last tile of a narrow width) were computed on zero weight rows and are not stored.
 template <int MODE>
 __device__ __forceinline__ void gemm_epilogue(const GemmArgs& g, int T, int row, int n_tile, uint32_t t_row, int bn, LinearShared& sh) {
-    if (MODE == kLinear || MODE == kLinearGated) {
+    if (is_linear(MODE)) {
         const int width = MODE == kLinearGated ? bn >> 1 : bn, col0 = n_tile * width, row0 = row - (threadIdx.x & 31);
         if (row0 >= T) return;                                          // (the whole warp: none of its rows exists)
         LinearAhead ahead;
@@ -567,7 +573,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
     dcut_pdl_wait();
     dcut_pdl_launch_dependents();
     int T_packed = g.cu_q[g.B];
-    if ((MODE == kLinear || MODE == kLinearGated) && T_packed > g.T_cap) {
+    if (is_linear(MODE) && T_packed > g.T_cap) {
         T_packed = g.T_cap;
         if (blockIdx.x == 0 && threadIdx.x == 0) atomicExch(g.status, DCUT_DEV_BAD_ROWS);
     }
@@ -836,7 +842,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                 const int n_tile = w / m_tiles, m0 = (w - n_tile * m_tiles) * BM;
                 const int acc = it & 1;
                 const int row = m0 + quarter * 32 + lane;
-                if (MODE == kLinear || MODE == kLinearGated) linear_stage_bias<MODE == kLinearGated>(g, n_tile, bn, sh);
+                if (is_linear(MODE)) linear_stage_bias<MODE == kLinearGated>(g, n_tile, bn, sh);
                 if (!__all_sync(0xffffffffu, mbar_wait(acc_full + 8 * acc, (it >> 1) & 1))) {
                     failed = true;
                     break;
@@ -929,7 +935,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                 const int n_tile = w / m_tiles, m0 = (w - n_tile * m_tiles) * (2 * BM) + (int)rank * BM;
                 const int acc = it & 1;
                 const int row = m0 + quarter * 32 + lane;
-                if (MODE == kLinear || MODE == kLinearGated) linear_stage_bias<MODE == kLinearGated>(g, n_tile, bn, sh);
+                if (is_linear(MODE)) linear_stage_bias<MODE == kLinearGated>(g, n_tile, bn, sh);
                 if (!__all_sync(0xffffffffu, mbar_wait(acc_full + 8 * acc, (it >> 1) & 1))) {
                     failed = true;
                     break;
@@ -1111,7 +1117,7 @@ int plan_gemm(dcut_ctx* ctx, int n_tiles, int T_cap, unsigned bn_mask, GemmArgs&
         // always launched as clusters of two CTAs (the kernel holds cta_group::2 instructions); the pair mode itself
         // can be switched off
         grid = 2 * (n_work < ctx->ly_gemm_pairs ? n_work : ctx->ly_gemm_pairs);   // room for either mode
-        ga.pairs = ctx->ly_gemm_pair_mode;
+        ga.pairs = ctx->ly_gemm_pair_mode && !(is_linear(MODE) && ga.K <= kShortK);
         ga.force = ctx->ly_gemm_force;
         if (ga.force >= 0 && (ga.force > 22 || (ga.force & 7) == 7 || !((ga.bn_mask >> (ga.force & 7)) & 1) || (ga.force >= 8 && !ga.pairs) ||
                               (ga.force >= 16 && !(may_split_k(MODE) && ga.K >= 2 * BK))))
@@ -1133,7 +1139,7 @@ int plan_gemm(dcut_ctx* ctx, int n_tiles, int T_cap, unsigned bn_mask, GemmArgs&
 
 template <int MODE>
 dcut_status launch_planned_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMaps& b2, int grid, const GemmArgs& ga, cudaStream_t stream) {
-    const size_t smem = MODE == kLinear || MODE == kLinearGated ? kLinearSmem : kGemmSmem;
+    const size_t smem = is_linear(MODE) ? kLinearSmem : kGemmSmem;
     if (ctx->ly_gemm_pairs > 0) {
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeClusterDimension;
