@@ -204,3 +204,14 @@ def test_refusals_through_the_context():
         ctx.linear(c["a"][:, :21].contiguous(), c["w"][:, :21], c["cu"], 4)       # rows 21 elements apart
     with pytest.raises(AssertionError):
         ctx.linear(c["a"].float(), c["w"], c["cu"], 4)
+
+
+@pytest.mark.parametrize("N,ld", [(40, 2000008), (37, 2000003)])
+def test_rows_behind_two_to_the_31_elements(N, ld):
+    T = 1100
+    ctx, c = context(), make(13, T, T, N, 72)
+    out, residual = (torch.empty((T, ld), dtype=torch.bfloat16, device="cuda")[:, :N] for _ in "or")
+    residual.copy_(make(14, T, T, N, 8, residual=True)["residual"])
+    c["residual"] = residual
+    run(ctx, c, "relu", out=out)
+    check(c, out, "relu")

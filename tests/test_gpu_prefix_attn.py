@@ -395,3 +395,20 @@ def test_many_short_items_per_segment(longest, hq, hkv, d):
     plens = rng.integers(0, longest + 1, 700)
     c = make_case(longest, rng.integers(1, 4, B), rng.integers(0, 40, B), sizes, plens, hq, hkv, d)
     check(c, *run(c))
+
+
+def test_pages_behind_two_to_the_31_elements():
+    """The same pages at the end of a cache of more than 2^31 elements give the same bits."""
+    c = make_case(31, [3, 1, 9], [40, 7, 300], [3], [150], 8, 8, 128)
+    ctx = make_ctx(c)
+    want, want_lse = run(c, ctx)
+    pool, shift = c["kc"].shape[0], 2 ** 31 // (8 * 16 * 128) + 5
+    for n in ("kc", "vc"):
+        big = torch.empty((shift + pool, 8, 16, 128), dtype=torch.bfloat16, device="cuda")
+        big[:2] = NAN
+        big[shift:] = c[n]
+        c[n] = big
+    c["table"], c["ptable"] = c["table"] + shift, c["ptable"] + shift
+    c["table"][c["table"] > shift + pool] = 1 << 30
+    out, lse = run(c, ctx)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)

@@ -218,3 +218,28 @@ def test_captured_and_replayed_on_another_stream():
     g.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want) and torch.equal(c["kc"], kc1) and torch.equal(c["vc"], vc1)
+
+
+def test_pages_and_tokens_behind_two_to_the_31_elements():
+    """The last pages of a cache of more than 2^31 elements, from q, k, v whose tokens lie far apart."""
+    ctx = _ctx(4, 8, 8, 128)
+    c = _case(77, [1, 5, 3, 2], [0, 15, 100, 31], 8, 8, 128, 128, layout="dense")
+    want = _call(ctx, c)
+    k_want, v_want = c["kc"].clone(), c["vc"].clone()
+    pool, shift = c["kc"].shape[0], 2 ** 31 // (8 * 16 * 128) + 5
+    c["table"] = c["table"] + shift
+    for n in ("kc", "vc"):
+        big = torch.empty((shift + pool, 8, 16, 128), dtype=torch.bfloat16, device="cuda")
+        big[shift:] = c[n]
+        c[n] = big
+    for n in ("q", "k", "v"):
+        far = torch.empty((c["cap"], 1 << 28), dtype=torch.bfloat16, device="cuda")[:, : 8 * 128].view(c["cap"], 8, 128)
+        far.copy_(c[n])
+        c[n] = far
+    c["kc"][shift:], c["vc"][shift:] = 0, 0
+    got = _call(ctx, c)
+    torch.cuda.synchronize()
+    assert ctx.poll_device_status() == 0 and torch.equal(got, want)
+    req, slot = c["req"][: c["T"]], c["slot"]
+    page, at = c["table"][req, slot // 16], slot % 16
+    assert torch.equal(c["kc"][page, :, at], k_want[page - shift, :, at]) and torch.equal(c["vc"][page, :, at], v_want[page - shift, :, at])
