@@ -25,7 +25,7 @@
 // P is rounded to bf16 (relative 2^-9, as V's type asks of the MMA); everything else stays in fp32 until the one rounding
 // of the output.
 //
-// Measured: 2176 tokens of 32q/8kv heads behind 8192 keys (292 Gflop) 318 us of a call of 402; a pair of tiles takes 1900 to
+// Measured: 2176 tokens of 32q/8kv heads behind 8192 keys (292 Gflop) 318 us of a call of 398; a pair of tiles takes 1900 to
 // 2050 cycles per block, of which the tensor pipe is busy for 1544 (Q K^T with both operands in shared memory runs at half
 // rate at N = 64), the MUFU for 1024; the softmax code alone takes 1300.  Blocks of 128 or 80 keys with one S buffer per
 // tile: 317 and 297-338 us.  Rescaling by a stale maximum 636 (spills), warps taking turns 592.
