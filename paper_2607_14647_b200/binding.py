@@ -157,23 +157,32 @@ def _ptr(t: Optional[torch.Tensor], dtype=None) -> Optional[int]:
     return t.data_ptr()
 
 
-def _heads(t: Optional[torch.Tensor], n_heads: int, head_dim: int):
+def _on(dev: int, t: Optional[torch.Tensor], dtype) -> Optional[int]:
+    """_ptr, for a tensor that has to be on GPU `dev`."""
+    if t is None:
+        return None
+    assert t.get_device() == dev and t.is_contiguous(), f"expected a contiguous tensor on cuda:{dev}"
+    assert t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
+    return t.data_ptr()
+
+
+def _heads(dev: int, t: Optional[torch.Tensor], n_heads: int, head_dim: int):
     """(pointer, token stride, head stride) of a bf16 [tokens, heads, head_dim] view whose last dimension is dense."""
     if t is None:
         return None, 0, 0
     shape, strides = t.shape, t.stride()
-    assert t.is_cuda and t.dtype == torch.bfloat16, "expected a CUDA bf16 tensor"
+    assert t.get_device() == dev and t.dtype == torch.bfloat16, f"expected a bf16 tensor on cuda:{dev}"
     assert len(shape) == 3 and shape[1] == n_heads and shape[2] == head_dim and strides[2] == 1, \
         f"expected [tokens, {n_heads}, {head_dim}] with dense heads, got {tuple(shape)} with strides {strides}"
     return t.data_ptr(), strides[0], strides[1]
 
 
-def _rows(t: Optional[torch.Tensor]):
+def _rows(dev: int, t: Optional[torch.Tensor]):
     """(pointer, row stride) of a bf16 [rows, columns] view whose rows are dense."""
     if t is None:
         return None, 0
     (rows, cols), (ld, step) = t.shape, t.stride()
-    assert t.is_cuda and t.dtype == torch.bfloat16 and (step == 1 or cols == 1), "expected a CUDA bf16 matrix with dense rows"
+    assert t.get_device() == dev and t.dtype == torch.bfloat16 and (step == 1 or cols == 1), f"expected a bf16 matrix with dense rows on cuda:{dev}"
     return t.data_ptr(), ld if rows > 1 else (cols + 7) // 8 * 8                         # (one row: its stride says nothing)
 
 
@@ -189,6 +198,8 @@ class PrefixGroups:
         G = prefix_lens.shape[0]
         assert cu_group.shape == (G + 1,) and prefix_table.shape[0] == G
         self.keep = (cu_group, prefix_lens, prefix_table)
+        self.device = prefix_lens.get_device()
+        assert cu_group.get_device() == self.device and prefix_table.get_device() == self.device
         self.rec = PrefixGroupsRec(G, _ptr(cu_group, torch.int32), _ptr(prefix_lens, torch.int32), _ptr(prefix_table, torch.int32),
                                    prefix_table.shape[1])
 
@@ -328,6 +339,10 @@ class Context:
     def _check(self, st: int):
         if st != OK:
             raise DcutError(st, _lib.dcut_last_error(self._h).decode())
+
+    def _stream(self) -> int:
+        """The current stream of the context's own GPU, whichever GPU is current."""
+        return torch._C._cuda_getCurrentRawStream(self.device)
 
     # -- cost model (host arrays) ------------------------------------------------------------
     def set_cost_dense(self, cost_ms: Sequence[float]):
@@ -528,20 +543,25 @@ class Context:
                     groups: Optional[PrefixGroups] = None, q_out=None):
         """dcut_rope_append: rotates q and k ([tokens, heads, head_dim] views of any token and head stride) and appends k, v
         to the paged cache.  `inv_freq`: fp64 [rotary_dim / 2] (None: no rotation).  Returns q_out [T_cap, Hq, Dh]."""
-        hq, hkv, d = self._shape
+        (hq, hkv, d), dev = self._shape, self.device
         assert (q is None or q.shape[0] >= T_cap) and k.shape[0] >= T_cap and v.shape[0] >= T_cap, "q, k and v need T_cap rows"
-        assert tok_req.shape[0] >= T_cap and tok_pos.shape[0] >= T_cap
+        assert tok_req.shape[0] >= T_cap and tok_pos.shape[0] >= T_cap and k_cache.shape == v_cache.shape
+        assert cu_q is None or cu_q.shape[0] == block_table.shape[0] + 1
+        assert q_out is None or q_out.numel() >= T_cap * hq * d
+        assert groups is None or groups.device == dev
+        assert inv_freq is None or inv_freq.dim() == 1
+        assert (q_gain is None or q_gain.numel() == d) and (k_gain is None or k_gain.numel() == d)
         if q is not None and q_out is None:
             q_out = torch.empty((T_cap, hq, d), dtype=torch.bfloat16, device=k.device)
-        (qp, qt, qh), (kp, kt, kh), (vp, vt, vh) = _heads(q, hq, d), _heads(k, hkv, d), _heads(v, hkv, d)
+        (qp, qt, qh), (kp, kt, kh), (vp, vt, vh) = _heads(dev, q, hq, d), _heads(dev, k, hkv, d), _heads(dev, v, hkv, d)
         x = Qkv(qp, kp, vp, qt, qh, kt, kh, vt, vh)
-        r = Rope(_ptr(inv_freq, torch.float64), 2 * inv_freq.shape[0] if inv_freq is not None else 0, int(interleaved),
-                 _ptr(q_gain, torch.bfloat16), _ptr(k_gain, torch.bfloat16), rms_eps)
-        self._check(_lib.dcut_rope_append(self._h, C.byref(x), C.byref(r), _ptr(q_out, torch.bfloat16), _ptr(k_cache, torch.bfloat16),
-                                          _ptr(v_cache, torch.bfloat16), k_cache.shape[0], _ptr(block_table, torch.int32),
+        r = Rope(_on(dev, inv_freq, torch.float64), 2 * inv_freq.shape[0] if inv_freq is not None else 0, int(interleaved),
+                 _on(dev, q_gain, torch.bfloat16), _on(dev, k_gain, torch.bfloat16), rms_eps)
+        self._check(_lib.dcut_rope_append(self._h, C.byref(x), C.byref(r), _on(dev, q_out, torch.bfloat16), _on(dev, k_cache, torch.bfloat16),
+                                          _on(dev, v_cache, torch.bfloat16), k_cache.shape[0], _on(dev, block_table, torch.int32),
                                           block_table.shape[1], C.byref(groups.rec) if groups is not None else None,
-                                          _ptr(cu_q, torch.int32), block_table.shape[0], _ptr(tok_req, torch.int32),
-                                          _ptr(tok_pos, torch.int32), T_cap, _stream()))
+                                          _on(dev, cu_q, torch.int32), block_table.shape[0], _on(dev, tok_req, torch.int32),
+                                          _on(dev, tok_pos, torch.int32), T_cap, self._stream()))
         return q_out
 
     def enable_prefix_attn(self, max_groups: int):
@@ -551,21 +571,24 @@ class Context:
     def prefix_attn(self, q, k_cache, v_cache, block_table, ctx_lens, cu_q, T_cap: int, groups: PrefixGroups,
                     scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
         """dcut_prefix_attn: verify_attn for requests that share prefixes; `block_table` holds their own pages only."""
-        assert q.shape[0] >= T_cap, "q needs T_cap rows"
+        (hq, hkv, d), dev, B = self._shape, self.device, ctx_lens.shape[0]
+        assert q.shape[0] >= T_cap and q.shape[1:] == (hq, d), f"q must be [T_cap rows, {hq}, {d}]"
+        assert cu_q.shape[0] == B + 1 and block_table.shape[0] == B and k_cache.shape == v_cache.shape and groups.device == dev
         if out is None:
             out = torch.empty_like(q)
+        assert out.numel() >= T_cap * hq * d and (lse is None or lse.numel() >= T_cap * hq)
         if scale is None:
             scale = 1.0 / float(np.sqrt(self.limits.head_dim))
-        self._check(_lib.dcut_prefix_attn(self._h, _ptr(q, torch.bfloat16), _ptr(k_cache, torch.bfloat16), _ptr(v_cache, torch.bfloat16),
-                                          k_cache.shape[0], _ptr(block_table, torch.int32), block_table.shape[1], _ptr(ctx_lens, torch.int32),
-                                          _ptr(cu_q, torch.int32), ctx_lens.shape[0], T_cap, C.byref(groups.rec), float(scale),
-                                          _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), _stream()))
+        self._check(_lib.dcut_prefix_attn(self._h, _on(dev, q, torch.bfloat16), _on(dev, k_cache, torch.bfloat16), _on(dev, v_cache, torch.bfloat16),
+                                          k_cache.shape[0], _on(dev, block_table, torch.int32), block_table.shape[1], _on(dev, ctx_lens, torch.int32),
+                                          _on(dev, cu_q, torch.int32), B, T_cap, C.byref(groups.rec), float(scale),
+                                          _on(dev, out, torch.bfloat16), _on(dev, lse, torch.float32), self._stream()))
         return out
 
     def linear(self, a, w, cu_q, T_cap: int, out=None, bias=None, act: str = "none", w2=None, bias2=None, residual=None):
         """dcut_linear: out = residual + act(a w^T + bias) [* (a w2^T + bias2)] over the packed rows; a, w, residual and out may
         be views with padded rows (a and w: a multiple of 8 elements apart)."""
-        N, K = w.shape
+        (N, K), dev = w.shape, self.device
         assert a.shape[1] == K and a.shape[0] >= T_cap, "a must be [T_cap rows, K]"
         assert bias is None or bias.shape == (N,)
         assert bias2 is None or bias2.shape == (N,)
@@ -573,11 +596,11 @@ class Context:
         if out is None:
             out = torch.empty((T_cap, N), dtype=torch.bfloat16, device=a.device)
         assert out.shape[0] >= T_cap and out.shape[1] == N
-        (ap, lda), (wp, ldw), (w2p, ldw2), (rp, ldr), (op, ldo) = _rows(a), _rows(w), _rows(w2), _rows(residual), _rows(out)
+        (ap, lda), (wp, ldw), (w2p, ldw2), (rp, ldr), (op, ldo) = _rows(dev, a), _rows(dev, w), _rows(dev, w2), _rows(dev, residual), _rows(dev, out)
         assert w2 is None or (w2.shape == w.shape and ldw2 == ldw), "w2 must have the shape and strides of w"
-        l = LinearArgs(ap, lda, wp, w2p, ldw, _ptr(bias, torch.bfloat16), _ptr(bias2, torch.bfloat16), rp, ldr, op, ldo, N, K,
+        l = LinearArgs(ap, lda, wp, w2p, ldw, _on(dev, bias, torch.bfloat16), _on(dev, bias2, torch.bfloat16), rp, ldr, op, ldo, N, K,
                        ACTIVATIONS[act])
-        self._check(_lib.dcut_linear(self._h, C.byref(l), _ptr(cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, _stream()))
+        self._check(_lib.dcut_linear(self._h, C.byref(l), _on(dev, cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, self._stream()))
         return out
 
     def make_model(self, layers: list, embed, g_final, w_lm, k_caches: list, v_caches: list, rms_eps: float = 1e-6,

@@ -215,3 +215,15 @@ def test_rows_behind_two_to_the_31_elements(N, ld):
     c["residual"] = residual
     run(ctx, c, "relu", out=out)
     check(c, out, "relu")
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    ctx, c = context(), make(15, 4, 4, 16, 24)
+    out = run(ctx, c)
+    with pytest.raises(AssertionError):
+        run(ctx, dict(c, bias=c["bias"].cpu()))
+    with pytest.raises(AssertionError):
+        run(ctx, c, out=out.cpu())
+    monkeypatch.setattr(ctx, "device", 1)                      # as if the context lived on the next GPU
+    with pytest.raises(AssertionError):
+        run(ctx, c)
