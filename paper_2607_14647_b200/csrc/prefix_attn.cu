@@ -44,7 +44,11 @@ using namespace dcut_prefix;
 
 constexpr int kThreads = 384;
 constexpr int kTeamThreads = 128;
-constexpr int kSlots = 8;             // ring of K and V blocks, in the order K V K V
+// Ring of K and V blocks, in the order K V K V.  No role waits for a slot's load while the load before it in that slot may
+// still be under way: the wait would return at once (tests/test_prefix_ring.py walks the roles' waits under delayed loads).
+// K: an item's Q arrives after the last Q K^T of the item before.  V: the issuers wait for o_free first; a softmax warp that
+// clears V rows has seen the item before end (both teams' o_full of a single, its own team's of a dual, which reads every V).
+constexpr int kSlots = 8;
 constexpr int kPage = dcut_plan::kPage;
 constexpr int kPagesPerBlock = kBlock / kPage;
 constexpr int kStageBytes = 2048;     // epilogue staging of a warp: 32 rows x 16 fp32
@@ -390,10 +394,14 @@ __device__ __forceinline__ void issue(const PrefixArgs& a, unsigned char* smem, 
         };
         for (int s = 0; ok && s < 2 && s < steps; ++s)
             if ((ok = wait(kv_full + 8 * k_slot, k_phase))) qk(s == steps - 1);
+        // The epilogues of the item before are over.  Before this wait the item has no wait for a V slot, no P V and no o_full:
+        // a parity wait cannot tell two phases from none.  The V of the item before may have been the other team's (a single's
+        // every other block), so its slot may be two phases behind; with o_free all of them have been loaded and read.  O is
+        // overwritten by the first P V, and a warp that still has to look at o_full must not find it a phase ahead (a single's
+        // second team may have no block).
+        if (ok && n_items > 0) ok = wait(smem_u32(&c->o_free), n_items - 1);
         for (int s = 0; ok && s < steps; ++s) {
-            // O += P V; the first of an item overwrites O: the epilogues of the item before must have read it
-            if (!wait2(kv_full + 8 * v_slot, v_phase, p_full + 8 * (n_pv & 1), n_pv >> 1) ||
-                (s == 0 && n_items > 0 && !wait(smem_u32(&c->o_free), n_items - 1))) {
+            if (!wait2(kv_full + 8 * v_slot, v_phase, p_full + 8 * (n_pv & 1), n_pv >> 1)) {
                 ok = false;
                 break;
             }
@@ -420,15 +428,7 @@ __device__ __forceinline__ void issue(const PrefixArgs& a, unsigned char* smem, 
             if (more) qk(s + 2 == steps - 1);
         }
         if (!ok) break;
-        if (steps == 0) {                                                     // (a single's second team may have no block)
-            tc_commit(smem_u32(&c->q_free));
-            // The softmax warps have seen the item before end: o_full would otherwise run a phase ahead of a warp that still
-            // has to look at it, and a parity wait cannot tell two phases from none.
-            if (n_items > 0 && !wait(smem_u32(&c->o_free), n_items - 1)) {
-                ok = false;
-                break;
-            }
-        }
+        if (steps == 0) tc_commit(smem_u32(&c->q_free));
         tc_commit(o_full);
         const int pos = base + 2 * nblk;
         base = pos % kSlots;

@@ -412,3 +412,21 @@ def test_pages_behind_two_to_the_31_elements():
     c["table"][c["table"] > shift + pool] = 1 << 30
     out, lse = run(c, ctx)
     assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 128), (2, 2, 64)])
+def test_odd_singles_before_other_items(hq, hkv, d):
+    """Items of one tile with an odd number of blocks behind one another in a CTA, and before items of two tiles: a slot of
+    the ring changes hands between the teams.  The same bits every time."""
+    rng = np.random.default_rng(hq)
+    sizes = rng.integers(1, 4, 300)
+    sizes[::7] = 70                                    # more than a tile of tokens (64 or 128), at three rows each
+    B = int(sizes.sum())
+    plens = 64 * rng.choice([1, 3, 5, 7], 300) - rng.integers(0, 20, 300)
+    c = make_case(32, rng.integers(1, 4, B), rng.integers(0, 20, B), sizes, plens, hq, hkv, d)
+    ctx = make_ctx(c)
+    out, lse = run(c, ctx)
+    check(c, out, lse)
+    for _ in range(5):
+        again, lse2 = run(c, ctx)
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
