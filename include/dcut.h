@@ -457,7 +457,8 @@ dcut_status dcut_rope_append(dcut_ctx* ctx, const dcut_qkv* qkv, const dcut_rope
  * (max_T * n_q_heads * (head_dim + 1) * 4 bytes) and the pieces of cut work items (512 rows per SM); max_groups <= max_B bounds
  * n_groups (a later call may raise it).  Without it dcut_prefix_attn returns DCUT_ECAPACITY.
  * A cu_q that does not pack B requests of 1 .. max_gamma + 1 rows into T_cap sets device status 7; groups that do not cover
- * the batch, a prefix longer than its table or than a context of its group set status 9; the call then writes nothing.
+ * the batch, a prefix longer than its table or than a context of its group, and a request whose own positions (its rows
+ * among them) need more than block_table_stride pages set status 9; the call then writes nothing.
  */
 dcut_status dcut_enable_prefix_attn(dcut_ctx* ctx, int max_groups);
 dcut_status dcut_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_cache, const void* v_cache, long long num_pages,
@@ -585,8 +586,8 @@ dcut_status dcut_verify_step_host(dcut_ctx* ctx, const dcut_host_step* step, voi
  * 7 = an acceptance call met a cu_q that is not a packing of B requests of 1 .. gamma + 1 rows inside T_cap
  * (rows at or past T_cap were left out: nothing outside the caller's T_cap rows is read or written), 8 =
  * dcut_rope_append met a token whose request or position has no place in the block table (it was left out), 9 =
- * dcut_prefix_attn met groups that do not cover the batch or a prefix that does not fit (nothing was written; 7 there: a
- * cu_q that does not pack the batch), 10 = dcut_linear met a cu_q[B] above T_cap (rows from T_cap on were left out). */
+ * dcut_prefix_attn met groups that do not cover the batch, a prefix or own positions that do not fit (nothing was written;
+ * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear met a cu_q[B] above T_cap (rows from T_cap on were left out). */
 dcut_status dcut_poll_device_status(dcut_ctx* ctx, int* code, void* stream);
 
 #ifdef __cplusplus

@@ -796,7 +796,7 @@ prefix_attn_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_const
 struct PrefixPlanArgs {
     const int* cu_group;
     const int* prefix_lens;
-    int n_groups, prefix_table_stride;
+    int n_groups, prefix_table_stride, block_table_stride;
     int group_size, max_rows, T_cap;      // max_rows: tokens of a request
     Group* groups;                        // [n_groups + 1]
     Seg* segs;                            // [n_seg + 1]
@@ -811,8 +811,9 @@ __host__ __device__ inline int plan_longs(int B) { return B <= kSmemGroups ? 3 *
 size_t plan_smem(int B) { return sizeof(long long) * plan_longs(B) + sizeof(int) * (2 * (size_t)B + 1); }
 
 // Two CTAs, which check the batch alike: the first makes the own parts' work list, the second the shared part's partition
-// (one after the other in one CTA they took 12 us, chains of dependent loads and scans both).  A batch that is not what the call's contract says (cu_q, cu_group, lengths) is reported and left alone: its
-// partition is empty, so nothing behind the arrays' ends is read or written.
+// (one after the other in one CTA they took 12 us, chains of dependent loads and scans both).  A batch that is not what the
+// call's contract says (cu_q, cu_group, prefixes against their table and contexts, own positions against the block table) is
+// reported and left alone: its partition is empty, so nothing behind the arrays' ends is read or written.
 __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlanArgs p, dcut_plan::PlanArgs a) {
     extern __shared__ long long prefix_s[];                   // cu_q [B + 1] and own lengths [B] lie behind plan_longs(B) of these
     __shared__ long long ws64[33], ws64b[33];
@@ -844,8 +845,9 @@ __global__ void __launch_bounds__(1024) prefix_plan_kernel(PrefixPlanArgs p, dcu
                 const int mid = (lo + hi) >> 1;
                 if (p.cu_group[mid] <= i) lo = mid; else hi = mid;
             }
-            own_s[i] -= p.prefix_lens[lo];
-            fits = fits && own_s[i] >= 0;
+            const long long own = (long long)own_s[i] - p.prefix_lens[lo];
+            fits = fits && own >= 0 && own + (cu_s[i + 1] - cu_s[i]) <= (long long)kPage * p.block_table_stride;
+            own_s[i] = (int)own;
         }
         sound = __syncthreads_and(fits);
     }
@@ -1039,6 +1041,7 @@ dcut_status dcut_launch_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_
     pp.prefix_lens = groups->prefix_lens;
     pp.n_groups = groups->n_groups;
     pp.prefix_table_stride = groups->prefix_table_stride;
+    pp.block_table_stride = block_table_stride;
     pp.group_size = l.n_q_heads / l.n_kv_heads;
     pp.max_rows = l.max_gamma + 1;
     pp.T_cap = T_cap;

@@ -430,3 +430,22 @@ def test_odd_singles_before_other_items(hq, hkv, d):
     for _ in range(5):
         again, lse2 = run(c, ctx)
         assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("request_", [0, 1, 2])
+@pytest.mark.parametrize("excess", [1, 16, 100000, None])
+def test_own_positions_behind_the_block_table_are_reported(request_, excess):
+    """The last row's position has to lie in the request's row of the block table; where it just does, nothing is reported."""
+    c = make_case(33, [2, 3, 1], [5, 6, 9], [2, 1], [90, 40], 8, 2, 128)
+    ctx = make_ctx(c, max_gamma=3)
+    plen = c["plens"][0 if request_ < 2 else 1]
+    c["ctx"][request_] = 2 ** 31 - 1 if excess is None else plen + 16 * c["table"].shape[1] - c["counts"][request_] + excess
+    out = torch.full((c["cap"], 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    ctx.prefix_attn(c["q"], c["kc"], c["vc"], out=out, **device_args(c))
+    assert ctx.poll_device_status() == 9 and bool((out == 7).all())
+
+
+def test_own_positions_may_fill_the_block_table():
+    c = make_case(34, [2, 3, 1], [16 * 4 - 2, 16 * 4 - 3, 16 * 4 - 1], [2, 1], [90, 40], 8, 2, 128)
+    c["table"] = np.ascontiguousarray(c["table"][:, :4])
+    check(c, *run(c))
