@@ -344,6 +344,13 @@ class Context:
         """The current stream of the context's own GPU, whichever GPU is current."""
         return torch._C._cuda_getCurrentRawStream(self.device)
 
+    def _same_caches(self, k_cache, v_cache):
+        """The number of pages is read off shape[0], so the rest of the shape has to be the context's."""
+        _, hkv, d = self._shape
+        shape = k_cache.shape
+        assert shape == v_cache.shape and shape[1:] == (hkv, 16, d), \
+            f"caches must be [pages, {hkv}, 16, {d}], got {tuple(shape)} and {tuple(v_cache.shape)}"
+
     # -- cost model (host arrays) ------------------------------------------------------------
     def set_cost_dense(self, cost_ms: Sequence[float]):
         a = np.ascontiguousarray(cost_ms, dtype=np.float32)
@@ -545,7 +552,8 @@ class Context:
         to the paged cache.  `inv_freq`: fp64 [rotary_dim / 2] (None: no rotation).  Returns q_out [T_cap, Hq, Dh]."""
         (hq, hkv, d), dev = self._shape, self.device
         assert (q is None or q.shape[0] >= T_cap) and k.shape[0] >= T_cap and v.shape[0] >= T_cap, "q, k and v need T_cap rows"
-        assert tok_req.shape[0] >= T_cap and tok_pos.shape[0] >= T_cap and k_cache.shape == v_cache.shape
+        assert tok_req.shape[0] >= T_cap and tok_pos.shape[0] >= T_cap
+        self._same_caches(k_cache, v_cache)
         assert cu_q is None or cu_q.shape[0] == block_table.shape[0] + 1
         assert q_out is None or q_out.numel() >= T_cap * hq * d
         assert groups is None or groups.device == dev
@@ -573,7 +581,8 @@ class Context:
         """dcut_prefix_attn: verify_attn for requests that share prefixes; `block_table` holds their own pages only."""
         (hq, hkv, d), dev, B = self._shape, self.device, ctx_lens.shape[0]
         assert q.shape[0] >= T_cap and q.shape[1:] == (hq, d), f"q must be [T_cap rows, {hq}, {d}]"
-        assert cu_q.shape[0] == B + 1 and block_table.shape[0] == B and k_cache.shape == v_cache.shape and groups.device == dev
+        assert cu_q.shape[0] == B + 1 and block_table.shape[0] == B and groups.device == dev
+        self._same_caches(k_cache, v_cache)
         if out is None:
             out = torch.empty_like(q)
         assert out.numel() >= T_cap * hq * d and (lse is None or lse.numel() >= T_cap * hq)
