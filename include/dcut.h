@@ -137,6 +137,8 @@ dcut_status dcut_select(dcut_ctx* ctx, const float* conf, int B, int gamma, cons
  *   out = softmax_j( q . k_j * scale ) v_j  over cache positions j = 0 .. L_i + t,
  * reading kv head h / (n_q_heads / n_kv_heads).  The K/V of the 1 + d_i new tokens must already
  * be in the cache at positions L_i .. L_i + d_i; slots behind them may hold anything.  bf16 in, fp32 accumulate, bf16 out.
+ * A visible key whose score is NaN or +infinity makes the row's out and lse NaN (-infinity: weight 0).  A NaN or an infinity in
+ * V shows in its column in every row that sees it, and may show in the rows of its request before it (0 x NaN is NaN).
  * DEVICE in:  q bf16 [T, n_q_heads, head_dim]; k_cache, v_cache (layout above, num_pages pages);
  *             block_table i32 [B, block_table_stride]; ctx_lens i32 [B] (= L_i); cu_q i32 [B+1].
  * DEVICE out: out bf16 [T, n_q_heads, head_dim]; lse fp32 [T, n_q_heads] (natural log of the

@@ -622,6 +622,7 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
 
         // ---------------------------------------------------------------- epilogue
         const bool has = it.blocks > 0, whole = is_whole(it);
+        const bool other = !it.dual && (nblk + team) >> 1 > 0;    // the other team has blocks of the same rows
         float m_o = -INFINITY, l_o = 0.0f;                        // the other team's part of a single's row
         // 16 columns of the warp's 32 rows at a time go through shared memory, so that global memory sees 64 bytes of a row
         // at once; the own part is fetched a chunk ahead, the first while the last products run
@@ -664,15 +665,17 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
         const float m_all = fmaxf(m_run, m_o);
         const float w_s = m_run == -INFINITY ? 0.0f : fast_exp2((m_run - m_all) * cs), w_o = m_o == -INFINITY ? 0.0f : fast_exp2((m_o - m_all) * cs);
         const float l_all = l_run * w_s + l_o * w_o;
-        const float lp = l_all > 0.0f ? m_all * cs + log2f(l_all) : -INFINITY;             // in powers of two
-        float f_s = l_all > 0.0f ? w_s / l_all : 0.0f, f_o = l_all > 0.0f ? w_o / l_all : 0.0f, f_own = 0.0f;
+        // l_all is 0 without keys and NaN where a key's score is NaN or +inf, and so are all the sums below: maxima pass over a
+        // NaN, weights and sums keep it
+        const float lp = l_all == 0.0f ? -INFINITY : m_all * cs + log2f(l_all);            // in powers of two
+        float f_s = l_all == 0.0f ? 0.0f : w_s / l_all, f_o = l_all == 0.0f ? 0.0f : w_o / l_all, f_own = 0.0f;
         if (whole) {
-            const float top = fmaxf(lp, ls), wp = top == -INFINITY ? 0.0f : exp2f(lp - top), wo = top == -INFINITY ? 0.0f : exp2f(ls - top);
-            const float inv = wp + wo > 0.0f ? 1.0f / (wp + wo) : 0.0f;
+            const float top = fmaxf(lp, ls), wp = lp == -INFINITY ? 0.0f : exp2f(lp - top), wo = ls == -INFINITY ? 0.0f : exp2f(ls - top);
+            const float inv = wp + wo == 0.0f ? 0.0f : 1.0f / (wp + wo);
             f_s *= wp * inv;
             f_o *= wp * inv;
             f_own = wo * inv;
-            if (a.lse && valid && (it.dual || team == 0)) a.lse[orow] = wp + wo > 0.0f ? (top + log2f(wp + wo)) * kLn2 : -INFINITY;
+            if (a.lse && valid && (it.dual || team == 0)) a.lse[orow] = wp + wo == 0.0f ? -INFINITY : (top + log2f(wp + wo)) * kLn2;
         }
         const size_t prow0 = whole ? 0 : (size_t)slot_of(it, blockIdx.x) * kSlotRows + tile * kTileRows;
         if (!whole && valid && (it.dual || team == 0)) a.part_lse[prow0 + R] = lp * kLn2;
@@ -683,13 +686,13 @@ __device__ __forceinline__ void softmax(const PrefixArgs& a, unsigned char* smem
             if (has) {
                 uint32_t os[16], oo[16];
                 tc_ld16(t_o + cc, os);
-                if (!it.dual) tc_ld16(t_oo + cc, oo);
+                if (other) tc_ld16(t_oo + cc, oo);
                 tc_wait_ld();
                 float x[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {                    // an accumulator of weight 0 may hold anything
-                    x[e] = f_s > 0.0f ? __uint_as_float(os[e]) * f_s : 0.0f;
-                    if (!it.dual && f_o > 0.0f) x[e] += __uint_as_float(oo[e]) * f_o;
+                for (int e = 0; e < 16; ++e) {                    // the accumulator of a team without blocks may hold anything
+                    x[e] = steps > 0 ? __uint_as_float(os[e]) * f_s : 0.0f;
+                    if (other) x[e] += __uint_as_float(oo[e]) * f_o;
                 }
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
@@ -922,7 +925,7 @@ __global__ void __launch_bounds__(kCombineThreads) prefix_combine_kernel(PrefixA
     float top = own;
 #pragma unroll 4
     for (int i = 0; i < cut.pieces; ++i) top = fmaxf(top, a.part_lse[prow(i)]);
-    float sum = top == -INFINITY ? 0.0f : exp2f((own - top) * kLog2e);
+    float sum = own == -INFINITY ? 0.0f : exp2f((own - top) * kLog2e);       // (a NaN is no maximum, but its weight is NaN)
 #pragma unroll
     for (int v = 0; v < kVec; ++v) acc[v].x *= sum, acc[v].y *= sum, acc[v].z *= sum, acc[v].w *= sum;
 #pragma unroll 4
@@ -936,11 +939,11 @@ __global__ void __launch_bounds__(kCombineThreads) prefix_combine_kernel(PrefixA
             acc[v].x += wgt * x.x, acc[v].y += wgt * x.y, acc[v].z += wgt * x.z, acc[v].w += wgt * x.w;
         }
     }
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int v = 0; v < kVec; ++v)
         *reinterpret_cast<uint2*>(a.out + orow * DH + c0 + 4 * v) = make_uint2(pack_bf16(acc[v].x * inv, acc[v].y * inv), pack_bf16(acc[v].z * inv, acc[v].w * inv));
-    if (a.lse && c0 == 0) a.lse[orow] = sum > 0.0f ? top + logf(sum) : -INFINITY;
+    if (a.lse && c0 == 0) a.lse[orow] = sum == 0.0f ? -INFINITY : top + logf(sum);
 }
 
 // ------------------------------------------------------------------------------------------------ host

@@ -784,12 +784,12 @@ __device__ __forceinline__ void mma_phase(const CUtensorMap& k_map, const CUtens
                     acc.z += wgt * v.z;
                     acc.w += wgt * v.w;
                 }
-                const float inv = l_all > 0.0f ? 1.0f / l_all : 0.0f;
+                const float inv = l_all == 0.0f ? 0.0f : 1.0f / l_all;
                 acc.x *= inv;
                 acc.y *= inv;
                 acc.z *= inv;
                 acc.w *= inv;
-                const float lse_nat = l_all > 0.0f ? (m_all * a.scale_log2 + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+                const float lse_nat = l_all == 0.0f ? -INFINITY : (m_all * a.scale_log2 + log2f(l_all)) * 0.6931471805599453f;
                 const int t = (row0 + R) / group, hl = (row0 + R) - t * group;
                 const size_t orow = (size_t)(q0 + t) * a.n_q_heads + kvh * group + hl;
                 if (item.n_chunks == 1) {
@@ -1144,9 +1144,11 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
             const float w_s = m_run == -INFINITY ? 0.0f : fast_exp2((m_run - m_all) * cs);
             const float w_o = m_o == -INFINITY ? 0.0f : fast_exp2((m_o - m_all) * cs);
             const float l_all = l_run * w_s + l_o * w_o;
-            const float inv = l_all > 0.0f ? 1.0f / l_all : 0.0f;
-            const float lse_nat = l_all > 0.0f ? (m_all * cs + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+            const float inv = l_all == 0.0f ? 0.0f : 1.0f / l_all;
+            const float lse_nat = l_all == 0.0f ? -INFINITY : (m_all * cs + log2f(l_all)) * 0.6931471805599453f;
             const float f_s = w_s * inv, f_o = w_o * inv;
+            // a team without groups (or without visible keys) has weight 0: its O is not read as a number
+            const bool use_s = w_s > 0.0f || l_all != l_all, use_o = w_o > 0.0f || l_all != l_all;
             const int t = (row0 + R) / group, hl = (row0 + R) - t * group;
             const size_t orow = (size_t)(q0 + t) * a.n_q_heads + kvh * group + hl;
             if (!live) {
@@ -1166,8 +1168,8 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
                 }
                 float v[32];
 #pragma unroll
-                for (int e = 0; e < 32; ++e)   // a team without groups (or without visible keys) has weight 0: its O is not read as a number
-                    v[e] = (w_s > 0.0f ? __uint_as_float(os[e]) * f_s : 0.0f) + (w_o > 0.0f ? __uint_as_float(oo[e]) * f_o : 0.0f);
+                for (int e = 0; e < 32; ++e)
+                    v[e] = (use_s ? __uint_as_float(os[e]) * f_s : 0.0f) + (use_o ? __uint_as_float(oo[e]) * f_o : 0.0f);
                 if (R < M) {
                     if (item.n_chunks == 1 && a.out_f32) {
                         float* po = a.out_f32 + orow * 128 + cc;
@@ -1546,7 +1548,7 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
                     const float w0 = m0 == -INFINITY ? 0.0f : fast_exp2((m0 - m_all) * cs);
                     const float w1 = m1 == -INFINITY ? 0.0f : fast_exp2((m1 - m_all) * cs);
                     const float l_all = l0 * w0 + l1 * w1;
-                    const float inv = l_all > 0.0f ? 1.0f / l_all : 0.0f;
+                    const float inv = l_all == 0.0f ? 0.0f : 1.0f / l_all;
                     const float f0 = w0 * inv, f1 = w1 * inv;
                     const float4 v0 = *reinterpret_cast<const float4*>(t_o + rr * kTcTailStride + c4);
                     const float4 v1 = *reinterpret_cast<const float4*>(t_o + (8 + rr) * kTcTailStride + c4);
@@ -1554,7 +1556,7 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
                     const int R = row0 + rr;
                     const int t = R / group, hl = R - t * group;
                     const size_t orow = (size_t)(q0 + t) * a.n_q_heads + kvh * group + hl;
-                    const float lse_nat = l_all > 0.0f ? (m_all * cs + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+                    const float lse_nat = l_all == 0.0f ? -INFINITY : (m_all * cs + log2f(l_all)) * 0.6931471805599453f;
                     if (item.n_chunks == 1) {
                         if (a.out_f32) *reinterpret_cast<float4*>(a.out_f32 + orow * 128 + c4) = v;
                         else *reinterpret_cast<uint2*>(a.out + orow * 128 + c4) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
@@ -1575,13 +1577,13 @@ __device__ __forceinline__ void tc_phase(const CUtensorMap& k2_map, const CUtens
                     const float w_s = m_run[r] == -INFINITY ? 0.0f : fast_exp2((m_run[r] - m_all) * cs);
                     const float w_o = m_o == -INFINITY ? 0.0f : fast_exp2((m_o - m_all) * cs);
                     const float l_all = l_run[r] * w_s + l_o * w_o;
-                    const float inv = l_all > 0.0f ? 1.0f / l_all : 0.0f;
+                    const float inv = l_all == 0.0f ? 0.0f : 1.0f / l_all;
                     const float f_s = w_s * inv, f_o = w_o * inv;
                     if (rr < M) {
                         const int R = row0 + rr;
                         const int t = R / group, hl = R - t * group;
                         const size_t orow = (size_t)(q0 + t) * a.n_q_heads + kvh * group + hl;
-                        const float lse_nat = l_all > 0.0f ? (m_all * cs + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
+                        const float lse_nat = l_all == 0.0f ? -INFINITY : (m_all * cs + log2f(l_all)) * 0.6931471805599453f;
                         const float* po = t_o + rr * kTcTailStride + c0;
                         if (item.n_chunks == 1) {
 #pragma unroll
@@ -1738,14 +1740,14 @@ __global__ void __launch_bounds__(1024) attn_combine_kernel(CombineArgs a) {
             const float m_all = fmaxf(l0, l1);
             const float w0 = (l0 == -INFINITY) ? 0.0f : __expf(l0 - m_all), w1 = (l1 == -INFINITY) ? 0.0f : __expf(l1 - m_all);
             const float wsum = (0.0f + w0) + w1;
-            const float inv = wsum > 0.0f ? 1.0f / wsum : 0.0f;
+            const float inv = wsum == 0.0f ? 0.0f : 1.0f / wsum;
 #pragma unroll
             for (int e = 0; e < kPer; e += 2) {
                 const float x0 = fmaf(w1, o1[e], fmaf(w0, o0[e], 0.0f)), x1 = fmaf(w1, o1[e + 1], fmaf(w0, o0[e + 1], 0.0f));
                 if (a.out_f32) *reinterpret_cast<float2*>(a.out_f32 + orow * DH + lane * kPer + e) = make_float2(x0 * inv, x1 * inv);
                 else *reinterpret_cast<uint32_t*>(op + e) = pack_bf16(x0 * inv, x1 * inv);
             }
-            if (a.lse && lane == 0) a.lse[orow] = wsum > 0.0f ? m_all + logf(wsum) : -INFINITY;
+            if (a.lse && lane == 0) a.lse[orow] = wsum == 0.0f ? -INFINITY : m_all + logf(wsum);
             continue;
         }
         float m_all = -INFINITY;
@@ -1766,13 +1768,13 @@ __global__ void __launch_bounds__(1024) attn_combine_kernel(CombineArgs a) {
 #pragma unroll
             for (int e = 0; e < kPer; ++e) acc[e] += w * po[e];
         }
-        const float inv = wsum > 0.0f ? 1.0f / wsum : 0.0f;
+        const float inv = wsum == 0.0f ? 0.0f : 1.0f / wsum;
 #pragma unroll
         for (int e = 0; e < kPer; e += 2) {
             if (a.out_f32) *reinterpret_cast<float2*>(a.out_f32 + orow * DH + lane * kPer + e) = make_float2(acc[e] * inv, acc[e + 1] * inv);
             else *reinterpret_cast<uint32_t*>(op + e) = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
         }
-        if (a.lse && lane == 0) a.lse[orow] = wsum > 0.0f ? m_all + logf(wsum) : -INFINITY;
+        if (a.lse && lane == 0) a.lse[orow] = wsum == 0.0f ? -INFINITY : m_all + logf(wsum);
     }
 }
 

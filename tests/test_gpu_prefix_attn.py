@@ -449,3 +449,110 @@ def test_own_positions_may_fill_the_block_table():
     c = make_case(34, [2, 3, 1], [16 * 4 - 2, 16 * 4 - 3, 16 * 4 - 1], [2, 1], [90, 40], 8, 2, 128)
     c["table"] = np.ascontiguousarray(c["table"][:, :4])
     check(c, *run(c))
+
+
+# ------------------------------------------------------------------------------------- scores that are no numbers, where they are seen
+
+def assert_not_numbers_where_the_formula_has_them(c, out, lse, clean, clean_lse):
+    """NaN in exactly the rows (and, for V, columns) that the formula gives it in; what the planted key does not touch keeps its bits.
+    A row to which the planted key is at minus infinity differs from the clean one by that key alone: the clean scores' bound."""
+    d = c["d"]
+    args = (c["table"], c["ctx"], c["cu"], c["cu_group"], c["plens"], c["ptable"], d ** -0.5)
+    q = bf16_values(c["q"])
+    with np.errstate(invalid="ignore"):
+        want, want_lse, A, _ = plain(q, c["kc_plain"], c["vc_plain"], *args)
+    _, _, _, qk = plain(q, c["kc_clean"], c["vc_clean"], *args)
+    T = c["T"]
+    want, want_lse, A, E = want[:T], want_lse[:T], A[:T], d * 2.0 ** -23 * qk[:T]
+    got, got_lse = bf16_values(out)[:T], lse.cpu().numpy().astype(np.float64)[:T]
+    assert np.array_equal(np.isfinite(got), np.isfinite(want)), (np.isfinite(got) != np.isfinite(want)).sum()
+    assert np.array_equal(np.isnan(got_lse), np.isnan(want_lse)), (np.isnan(got_lse) != np.isnan(want_lse)).sum()
+    bad = ~np.isfinite(want)
+    assert bad.any() or not np.isfinite(c["planted"])
+    with np.errstate(invalid="ignore"):
+        lim = 2.0 ** -8 * (np.abs(want) + A) + (2 * E[..., None] + 2.0 ** -15) * A
+        assert (np.abs(got - want) <= lim)[~bad].all()
+        assert (np.abs(got_lse - want_lse) <= E + 2.0 ** -18 + 2.0 ** -21 * np.abs(want_lse))[~np.isnan(want_lse)].all()
+    same = c["untouched"][:T]
+    assert torch.equal(out[:T][same], clean[:T][same]) and torch.equal(lse[:T][same], clean_lse[:T][same])
+    return bad
+
+
+def plant(c, cache, page, slot, value, head=0, element=3):
+    c[cache][int(page), head, int(slot), element] = value
+    c[cache + "_plain"][int(page), head, int(slot), element] = value
+    c["planted"] = value
+
+
+def planted_case(*args, **kw):
+    c = make_case(*args, poison=False, **kw)
+    c["kc_clean"], c["vc_clean"] = c["kc_plain"].copy(), c["vc_plain"].copy()
+    group = np.repeat(np.arange(c["G"]), np.diff(c["cu_group"]))
+    c["group_of_row"], c["req_of_row"] = np.repeat(group, c["counts"]), np.repeat(np.arange(c["B"]), c["counts"])
+    return c
+
+
+# one tile or two per group; one long prefix that is cut over the SMs, or more whole items than SMs
+SHARED = {"cut_single": ([3, 1, 5], [3], [1000], 8, 2), "cut_dual": ([17, 9, 4], [3], [2500], 32, 4), "whole_single": ([2, 1] * 150, [1] * 300, [130] * 300, 8, 2),
+          "whole_dual": ([17, 17] * 60, [2] * 60, [200] * 60, 16, 2), "one_block": ([2], [1], [9], 4, 2)}
+
+
+@pytest.mark.parametrize("value", [NAN, float("inf")])
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("shape", sorted(SHARED))
+def test_a_key_of_a_prefix_that_is_no_number_shows(shape, d, value):
+    counts, sizes, plens, hq, hkv = SHARED[shape]
+    c = planted_case(41, counts, np.arange(len(counts)) % 30, sizes, plens, hq, hkv, d)
+    ctx = make_ctx(c)
+    clean, clean_lse = run(c, ctx)
+    kc = c["kc"].clone()
+    P = plens[0]
+    for j in sorted({0, P // 2, P - 1}):
+        c["kc"].copy_(kc)
+        c["kc_plain"] = c["kc_clean"].copy()
+        plant(c, "kc", c["ptable"][0, j // 16], j % 16, value, head=hkv - 1)
+        c["untouched"] = torch.tensor((c["group_of_row"] > 0)[:, None] | (np.arange(hq) < hq - hq // hkv), device="cuda")
+        out, lse = run(c, ctx)
+        assert_not_numbers_where_the_formula_has_them(c, out, lse, clean, clean_lse)
+
+
+@pytest.mark.parametrize("value", [NAN, float("inf")])
+@pytest.mark.parametrize("shape", sorted(SHARED))
+def test_a_value_of_a_prefix_that_is_no_number_shows_in_its_column(shape, value):
+    counts, sizes, plens, hq, hkv = SHARED[shape]
+    c = planted_case(42, counts, np.arange(len(counts)) % 30, sizes, plens, hq, hkv, 128)
+    ctx = make_ctx(c)
+    clean, clean_lse = run(c, ctx)
+    plant(c, "vc", c["ptable"][0, 0], 5, value)
+    c["untouched"] = torch.tensor((c["group_of_row"] > 0)[:, None] | (np.arange(hq) >= hq // hkv), device="cuda")
+    out, lse = run(c, ctx)
+    bad = assert_not_numbers_where_the_formula_has_them(c, out, lse, clean, clean_lse)
+    assert torch.equal(lse, clean_lse) and bad[..., 3].sum() == bad.sum()
+
+
+@pytest.mark.parametrize("value", [NAN, float("inf")])
+@pytest.mark.parametrize("prefix", [0, 70])
+@pytest.mark.parametrize("hq,hkv,d,deep", [(8, 8, 128, 1), (8, 2, 64, 17), (8, 2, 128, 17), (32, 4, 128, 17), (32, 2, 128, 9), (18, 2, 128, 16)])
+def test_a_key_of_a_request_that_is_no_number_shows(hq, hkv, d, deep, prefix, value):
+    """Own keys: warp-level tiles, tensor-memory tiles and their tails, whole and cut; the last key may be all that a team of
+    softmax warps sees.  dcut_verify_attn, which shares that path, alike."""
+    counts = [deep, deep, 1, max(1, deep - 4)] * 3
+    own = [64 - deep + 1, 0, 64, 127, 200, 1000, 4007, 448, 64, 7, 2203, 128]
+    c = planted_case(43, counts, own, [len(counts)], [prefix], hq, hkv, d)
+    ctx = make_ctx(c)
+    clean, clean_lse = run(c, ctx)
+    for r, back in ((0, 0), (2, 0), (5, 500), (6, 0), (6, 3000), (7, 0), (10, 1)):
+        j = int(own[r] + counts[r] - 1 - back)                          # back 0: the request's last token, which one row sees
+        if j < 0:
+            continue
+        plant(c, "kc", c["table"][r, j // 16], j % 16, value)
+    touched = np.isin(c["req_of_row"], [0, 2, 5, 6, 7, 10])
+    c["untouched"] = torch.tensor(~touched[:, None] | (np.arange(hq) >= hq // hkv), device="cuda")
+    out, lse = run(c, ctx)
+    assert_not_numbers_where_the_formula_has_them(c, out, lse, clean, clean_lse)
+    if prefix == 0:
+        lse2 = torch.empty_like(lse)
+        a = device_args(c)
+        out2 = ctx.verify_attn(c["q"], c["kc"], c["vc"], a["block_table"], a["ctx_lens"], a["cu_q"], c["cap"], lse=lse2)
+        torch.cuda.synchronize()
+        assert_not_numbers_where_the_formula_has_them(c, out2, lse2, out2, lse2)
