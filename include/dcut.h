@@ -425,8 +425,9 @@ typedef struct {
  * DEVICE out: q_out bf16 [T_cap, n_q_heads, head_dim] dense, 16-byte aligned (may be q itself when q is dense; must not
  *   overlap it in any other way); k_cache, v_cache (layout above, 128-byte aligned).
  * T_cap is not bound by dcut_limits: prompts of any length can be appended.  The new tokens' (request, position) pairs
- * must differ from one another.  A token whose request is >= B or whose position has no column in the block table sets
- * device status 8, one whose page is outside [0, num_pages) status 2; nothing is written for such a token.
+ * must differ from one another.  A token whose request is >= B or whose position has no column in the block table, and with
+ * `groups` one whose request not exactly one group covers or whose prefix length is negative, sets device status 8, one whose
+ * page is outside [0, num_pages) status 2; nothing is written for such a token.
  */
 typedef struct {
     const void *q, *k, *v;
@@ -587,7 +588,7 @@ dcut_status dcut_verify_step_host(dcut_ctx* ctx, const dcut_host_step* step, voi
  * kernel gave up, 5 = dcut_commit ran out of room, 6 = dcut_model_verify met a token id outside [0, vocab),
  * 7 = an acceptance call met a cu_q that is not a packing of B requests of 1 .. gamma + 1 rows inside T_cap
  * (rows at or past T_cap were left out: nothing outside the caller's T_cap rows is read or written), 8 =
- * dcut_rope_append met a token whose request or position has no place in the block table (it was left out), 9 =
+ * dcut_rope_append met a token whose request, group or position has no place in the block table (it was left out), 9 =
  * dcut_prefix_attn met groups that do not cover the batch, a prefix or own positions that do not fit (nothing was written;
  * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear met a cu_q[B] above T_cap (rows from T_cap on were left out). */
 dcut_status dcut_poll_device_status(dcut_ctx* ctx, int* code, void* stream);

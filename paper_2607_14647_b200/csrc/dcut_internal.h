@@ -19,7 +19,7 @@
 #define DCUT_DEV_COMMIT_OVERFLOW 5      // dcut_commit: a context or a token stream ran out of room
 #define DCUT_DEV_BAD_TOKEN 6            // dcut_model_verify: a token id outside [0, vocab)
 #define DCUT_DEV_BAD_CU_Q 7             // acceptance: cu_q is not a packing of B requests of 1..gamma+1 rows within T_cap
-#define DCUT_DEV_BAD_APPEND 8           // dcut_rope_append: a token's request or position has no place in the block table
+#define DCUT_DEV_BAD_APPEND 8           // dcut_rope_append: a token's request, group or position has no place in the block table
 #define DCUT_DEV_BAD_ROWS 10            // dcut_linear: cu_q[B] above T_cap
 #define DCUT_DEV_BAD_GROUPS 9           // dcut_prefix_attn: the groups do not cover the batch, a prefix does not fit its table or contexts, or own positions their row of the block table
 

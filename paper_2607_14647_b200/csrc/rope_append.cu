@@ -67,7 +67,7 @@ template <int DH>
 __global__ void __launch_bounds__(kMaxThreads, 2) rope_append_heads_kernel(DcutRopeArgs a) {
     constexpr int kPer = DH / 16;
     __shared__ float cos_s[DH / 2], sin_s[DH / 2];
-    __shared__ int prefix_s;
+    __shared__ int prefix_s, covers_s;
     dcut_pdl_wait();
     dcut_pdl_launch_dependents();
     const int tok = blockIdx.x, tid = threadIdx.x;
@@ -94,17 +94,20 @@ __global__ void __launch_bounds__(kMaxThreads, 2) rope_append_heads_kernel(DcutR
     }
     int prefix = 0;
     if (a.n_groups) {
-        if (tid == 0) prefix_s = 0;
+        if (tid == 0) covers_s = 0;
         __syncthreads();
-        for (int g = tid; g < a.n_groups; g += blockDim.x) {  // the request's group: cu_group is ascending, one g matches
+        for (int g = tid; g < a.n_groups; g += blockDim.x) {  // the request's group: one, where cu_group is as it should be
             const int len = a.prefix_lens[g];
-            if (a.cu_group[g] <= req && req < a.cu_group[g + 1]) prefix_s = len;
+            if (a.cu_group[g] <= req && req < a.cu_group[g + 1]) {
+                atomicAdd(&covers_s, 1);
+                prefix_s = len;
+            }
         }
         __syncthreads();
-        prefix = prefix_s;
+        prefix = covers_s == 1 ? prefix_s : -1;
     }
     const long long slot = (long long)pos - prefix;
-    if (req >= a.B || pos < 0 || slot < 0 || slot / 16 >= a.block_table_stride) {
+    if (req >= a.B || pos < 0 || prefix < 0 || slot < 0 || slot / 16 >= a.block_table_stride) {
         if (tid == 0) atomicExch(a.status, DCUT_DEV_BAD_APPEND);
         return;
     }

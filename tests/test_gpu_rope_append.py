@@ -243,3 +243,24 @@ def test_pages_and_tokens_behind_two_to_the_31_elements():
     req, slot = c["req"][: c["T"]], c["slot"]
     page, at = c["table"][req, slot // 16], slot % 16
     assert torch.equal(c["kc"][page, :, at], k_want[page - shift, :, at]) and torch.equal(c["vc"][page, :, at], v_want[page - shift, :, at])
+
+
+@pytest.mark.parametrize("cu_group,plens,bad_requests", [([0, 2], [32], [2]), ([1, 3], [32], [0]), ([0, 2, 1, 3], [16, 0, 16], [1]), ([0, 1, 3], [16, -16], [1, 2]),
+                                                         ([0, 3, 3], [16, -16], [])])
+def test_requests_that_not_exactly_one_group_covers_are_reported(cu_group, plens, bad_requests):
+    """No group, two of them (borders out of order), a negative prefix length (of an empty group: nothing to report)."""
+    ctx = _ctx(3, 8, 2, 128)
+    c = _case(12, [2, 1, 2], [40, 50, 60], 8, 2, 128, 128, stride=8)
+    rows = [r for r in range(5) if c["req"][r] not in bad_requests]
+    slot = c["slot"] - np.array([next((p for p, lo, hi in zip(plens, cu_group, cu_group[1:]) if lo <= q < hi), 0) for q in c["req"]])
+    c["table"] = np.arange(24).reshape(3, 8)
+    g = torch.Generator("cuda").manual_seed(1)
+    for n in ("kc", "vc"):
+        c[n] = torch.randn((24, 2, 16, 128), generator=g, device="cuda").to(torch.bfloat16)
+    c["plens"], c["cu_group"] = plens, cu_group
+    k0, v0 = bf16_values(c["kc"]), bf16_values(c["vc"])
+    out = torch.full((5, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    _call(ctx, c, q_out=out)
+    assert ctx.poll_device_status() == (8 if bad_requests else 0)
+    assert all(bool((out[r] == 7).all()) for r in range(5) if r not in rows)
+    _check(dict(c, T=len(rows), q=c["q"][rows], k=c["k"][rows], v=c["v"][rows], req=c["req"][rows], pos=c["pos"][rows], slot=slot[rows]), out[rows], k0, v0)
