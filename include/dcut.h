@@ -427,7 +427,7 @@ typedef struct {
  * T_cap is not bound by dcut_limits: prompts of any length can be appended.  The new tokens' (request, position) pairs
  * must differ from one another.  A token whose request is >= B or whose position has no column in the block table, and with
  * `groups` one whose request not exactly one group covers or whose prefix length is negative, sets device status 8, one whose
- * page is outside [0, num_pages) status 2; nothing is written for such a token.
+ * page is outside [0, num_pages) status 2; nothing is written for such a token.  A cu_q[B] above T_cap sets status 10.
  */
 typedef struct {
     const void *q, *k, *v;
@@ -590,7 +590,8 @@ dcut_status dcut_verify_step_host(dcut_ctx* ctx, const dcut_host_step* step, voi
  * (rows at or past T_cap were left out: nothing outside the caller's T_cap rows is read or written), 8 =
  * dcut_rope_append met a token whose request, group or position has no place in the block table (it was left out), 9 =
  * dcut_prefix_attn met groups that do not cover the batch, a prefix or own positions that do not fit (nothing was written;
- * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear met a cu_q[B] above T_cap (rows from T_cap on were left out). */
+ * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear or dcut_rope_append met a cu_q[B] above T_cap
+ * (rows from T_cap on were left out). */
 dcut_status dcut_poll_device_status(dcut_ctx* ctx, int* code, void* stream);
 
 #ifdef __cplusplus

@@ -20,7 +20,7 @@
 #define DCUT_DEV_BAD_TOKEN 6            // dcut_model_verify: a token id outside [0, vocab)
 #define DCUT_DEV_BAD_CU_Q 7             // acceptance: cu_q is not a packing of B requests of 1..gamma+1 rows within T_cap
 #define DCUT_DEV_BAD_APPEND 8           // dcut_rope_append: a token's request, group or position has no place in the block table
-#define DCUT_DEV_BAD_ROWS 10            // dcut_linear: cu_q[B] above T_cap
+#define DCUT_DEV_BAD_ROWS 10            // dcut_linear, dcut_rope_append: cu_q[B] above T_cap
 #define DCUT_DEV_BAD_GROUPS 9           // dcut_prefix_attn: the groups do not cover the batch, a prefix does not fit its table or contexts, or own positions their row of the block table
 
 // One row of the attention work table: a (request, row block of its query tile); it stands for n_kv_heads work items of

@@ -73,6 +73,7 @@ __global__ void __launch_bounds__(kMaxThreads, 2) rope_append_heads_kernel(DcutR
     const int tok = blockIdx.x, tid = threadIdx.x;
     const int req = a.tok_req[tok], pos = a.tok_pos[tok];     // together with cu_q: one trip to memory
     const int T = a.cu_q ? a.cu_q[a.B] : a.T_cap;
+    if (T > a.T_cap && tok == 0 && tid == 0) atomicExch(a.status, DCUT_DEV_BAD_ROWS);
     if (tok >= T || req < 0) return;                          // behind the last token, or padding
     const int Hq = a.q ? a.n_q_heads : 0, Hr = Hq + a.n_kv_heads, units = (Hr + a.n_kv_heads) * kPer;
 

@@ -264,3 +264,13 @@ def test_requests_that_not_exactly_one_group_covers_are_reported(cu_group, plens
     assert ctx.poll_device_status() == (8 if bad_requests else 0)
     assert all(bool((out[r] == 7).all()) for r in range(5) if r not in rows)
     _check(dict(c, T=len(rows), q=c["q"][rows], k=c["k"][rows], v=c["v"][rows], req=c["req"][rows], pos=c["pos"][rows], slot=slot[rows]), out[rows], k0, v0)
+
+
+def test_rows_past_the_capacity_are_reported():
+    ctx = _ctx(3, 8, 2, 128)
+    c = _case(13, [2, 1, 2], [40, 50, 60], 8, 2, 128, 128)
+    c["cu"][-1] = 6
+    k0, v0 = bf16_values(c["kc"]), bf16_values(c["vc"])
+    out = _call(ctx, c)
+    assert ctx.poll_device_status() == 10 and ctx.poll_device_status() == 0
+    _check(c, out, k0, v0)
