@@ -31,12 +31,16 @@
 #include <limits.h>
 #include <math.h>
 #include <stdlib.h>
+#include <string.h>
 
 #include "dcut_internal.h"
+#include "gemm_plan.cuh"
 
 namespace {
 
-constexpr int BM = 128, BN = 256, BK = 64, kGemmStages = 4;
+using namespace dcut_gemm;
+
+constexpr int kGemmStages = 4;
 constexpr int kATile = BM * BK * 2;            // 16 KB
 constexpr int kBTile = BN * BK * 2;            // 32 KB
 constexpr int kGemmStageBytes = kATile + kBTile;
@@ -52,12 +56,6 @@ __host__ __device__ constexpr bool is_gated(int mode) { return mode == kSwiGLU |
 __host__ __device__ constexpr bool is_linear(int mode) { return mode == kLinear || mode == kLinearGated; }
 __host__ __device__ constexpr bool may_split_k(int mode) { return mode == kPlain || mode == kResidual || mode == kLinear; }
 
-// Widths of the output tile that the one-SM mode may use: 256, 224, ..., 64 columns.  A narrower tile costs a little
-// efficiency per flop and buys more tiles, which is what a GEMM with fewer than one wave of 128 x 256 tiles needs
-// (T = 600, N = 4096: 80 tiles for 148 SMs at width 256, 130 at width 160).  One tensor map of the weight per width
-// (box = half the width in rows: a B tile is loaded as two halves, which is also how the SwiGLU tile is put together).
-constexpr int kNumBn = 7;
-__host__ __device__ constexpr int bn_of(int i) { return BN - 32 * i; }
 struct BMaps {
     CUtensorMap m[kNumBn];
 };
@@ -66,16 +64,6 @@ struct BMaps {
 struct AMaps {
     CUtensorMap full, half;
 };
-constexpr unsigned kBnMaskAll = (1u << kNumBn) - 1;
-constexpr int kPlanRows = 72;
-constexpr int kSplitCost = 50;             // gemm_plan: what the exchange of partial sums between the two SMs costs
-// dcut_linear with few k-blocks: one SM per tile only.  gemm_plan is fitted to K of 4096 and more; with up to 512 a tile's cost is
-// its epilogue and the start, which pairs and split K make dearer.  One SM against the plan's choice with them, us, no
-// activation: K = 64, 8 x 6147 6.0 / 8.1, 333 x 6147 9.1 / 12.3; K = 384, 333 x 2048 6.0 / 7.0, 8 x 2048 5.6 / 5.2; K = 640,
-// 8 x 2048 6.5 / 5.7, 700 x 6147 18.2 / 19.0.
-constexpr int kShortK = 512;
-constexpr unsigned kBnMaskSwiGLU = 0x55;   // widths whose halves are whole 32-column epilogue steps: 256, 192, 128, 64
-
 // ------------------------------------------------------------------------------------------------ PTX
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
@@ -167,7 +155,6 @@ struct GemmArgs {
     int B;
     int N_out;         // columns of the output (kSwiGLU: the intermediate size I; otherwise N)
     int K;
-    int n_tiles;       // output tiles along N
     __nv_bfloat16* out;
     const __nv_bfloat16* residual;   // [T, N_out] or null
     unsigned long long* row_key;     // kArgmax: one packed (ordered maximum, ~column) word per row
@@ -177,10 +164,7 @@ struct GemmArgs {
     int T_cap;                       // kLinear*: rows that out has
     int act;                         // kLinear*: dcut_act
     int vec;                         // kLinear*: out and residual take 16-byte accesses at multiples of 8 columns
-    int pairs;                       // launched as clusters of two CTAs: the pair mode may be chosen
-    unsigned bn_mask;                // tile widths whose tensor maps were supplied (bit i: bn_of(i)); bit 0 always
-    int force;                       // experiments: -1 = let gemm_plan choose, 0..6 = that width on one SM, 8..14 = on a pair
-    unsigned char plan_by_m[kPlanRows];   // gemm_plan for 1, 2, ... row blocks of 128 (the last entry serves all larger counts)
+    unsigned char plan_by_m[kPlanRows];   // gemm_plan.cuh: for 1, 2, ... row blocks of 128 (the last entry serves all larger counts)
     int* status;
 };
 
@@ -434,7 +418,7 @@ __device__ __forceinline__ void gemm_epilogue(const GemmArgs& g, int T, int row,
 // Measured against the one-CTA kernel: 74 us against 86 us for the down projection at T = 512-640 (K = 12288), 81 against
 // 90 us for gate/up + SwiGLU at T = 512, but 135 against 92 us for the down projection at T = 1088, where 5 x 16 = 80
 // pair tiles need two waves on 74 pairs (and 1280 padded rows are computed instead of 1152): the mode is therefore
-// chosen per launch (gemm_plan).
+// chosen per launch (gemm_plan.cuh).
 
 constexpr int kG2Stages = 6;
 constexpr int kG2StageBytes = kATile + kBTile / 2;     // 32 KB
@@ -485,48 +469,7 @@ __device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
 //   A pair per 128 x bn tile, half of K each (below): for launches whose tiles all fit one wave of pairs.
 // In the first two the operand ring and its barriers continue across tiles and the accumulator is double-buffered in
 // tensor memory (2 x 256 columns), so the epilogue of one tile overlaps the main loop of the next.
-// The cheapest way to run this launch under a model fitted to measurements on the four projections of an 8B-class
-// layer at 17 packed lengths from 64 to 1088 (every width, every mode): time = waves x (4 bn + 1664) on one SM per
-// tile, waves x (7 bn + 800) on a pair, half a one-SM tile + kSplitCost for a pair splitting K.  (A pair tile moves two
-// thirds of the bytes per flop from L2 and its MMAs are issued at about 0.57 of the one-SM rate per column; the
-// constants stand for what a tile costs whatever its width.)  Over those 68 cases the pick reaches the best measured
-// single choice to within a percent (geometric mean).  Returns the width index, + kPlanPair or + kPlanSplit; the
-// wider tile wins ties.
-// The choice depends on T only through the number of 128-row blocks, so the host tabulates it per launch
-// (GemmArgs::plan_by_m) and the kernel looks it up after reading T.
-constexpr int kPlanPair = 8, kPlanSplit = 16;
-inline int gemm_plan(int m1, int N_out, unsigned bn_mask, bool pairs, bool may_split, int force, bool swiglu, int grid) {
-    if (force >= 0) return force;
-    const int m2 = (m1 + 1) / 2;
-    const int n_pairs = pairs ? grid >> 1 : 0;
-    int best = 0, best_cost = INT_MAX;
-    for (int i = 0; i < kNumBn; ++i) {
-        if (!((bn_mask >> i) & 1)) continue;
-        const int bn = bn_of(i), per = swiglu ? bn >> 1 : bn, n_tiles = (N_out + per - 1) / per;
-        const int cost1 = ((m1 * n_tiles + grid - 1) / grid) * (4 * bn + 1664);
-        if (cost1 < best_cost) {
-            best_cost = cost1;
-            best = i;
-        }
-        if (n_pairs > 0) {
-            const int cost2 = ((m2 * n_tiles + n_pairs - 1) / n_pairs) * (7 * bn + 800);
-            if (cost2 < best_cost) {
-                best_cost = cost2;
-                best = kPlanPair + i;
-            }
-            // both SMs of a pair on one 128-row tile, half of K each (only as a single wave: a tile per pair)
-            if (may_split && m1 * n_tiles <= n_pairs) {
-                const int cost3 = (4 * bn + 1664) / 2 + kSplitCost;
-                if (cost3 < best_cost) {
-                    best_cost = cost3;
-                    best = kPlanSplit + i;
-                }
-            }
-        }
-    }
-    return best;
-}
-
+// Which of them, and how wide a tile: gemm_plan.cuh, by the packed length.
 static_assert(kGemmStages * kGemmStageBytes == kG2Stages * kG2StageBytes, "both modes use the same operand area");
 
 template <int MODE>
@@ -1099,42 +1042,14 @@ dcut_status make_weight_maps(dcut_ctx* ctx, BMaps* maps, const void* w, long lon
     return DCUT_OK;
 }
 
-// Fills in how a launch runs (GemmArgs::plan_by_m and what goes with it); returns its grid
+// Fills in how a launch runs (gemm_plan.cuh); returns its grid
 template <int MODE>
-int plan_gemm(dcut_ctx* ctx, int n_tiles, int T_cap, unsigned bn_mask, GemmArgs& ga) {
-    ga.n_tiles = n_tiles;
-    ga.bn_mask = bn_mask | 1u;
-
-    // work items at the narrowest width that may be chosen (the widest has n_tiles per row block)
-    int narrow = 0;
-    for (int i = 0; i < kNumBn; ++i)
-        if ((ga.bn_mask >> i) & 1) narrow = i;
-    const int n_work = ((T_cap + BM - 1) / BM) * ((n_tiles * BN + bn_of(narrow) - 1) / bn_of(narrow));
-    int grid = n_work < ctx->sm_count ? n_work : ctx->sm_count;   // persistent: at most one CTA per SM
-    ga.pairs = 0;
-    ga.force = ctx->ly_gemm_force >= 0 && ctx->ly_gemm_force < kNumBn && ((ga.bn_mask >> ctx->ly_gemm_force) & 1) ? ctx->ly_gemm_force : -1;
-    if (ctx->ly_gemm_pairs > 0) {
-        // always launched as clusters of two CTAs (the kernel holds cta_group::2 instructions); the pair mode itself
-        // can be switched off
-        grid = 2 * (n_work < ctx->ly_gemm_pairs ? n_work : ctx->ly_gemm_pairs);   // room for either mode
-        ga.pairs = ctx->ly_gemm_pair_mode && !(is_linear(MODE) && ga.K <= kShortK);
-        ga.force = ctx->ly_gemm_force;
-        if (ga.force >= 0 && (ga.force > 22 || (ga.force & 7) == 7 || !((ga.bn_mask >> (ga.force & 7)) & 1) || (ga.force >= 8 && !ga.pairs) ||
-                              (ga.force >= 16 && !(may_split_k(MODE) && ga.K >= 2 * BK))))
-            ga.force = -1;
-        const int m_cap = (T_cap + BM - 1) / BM;   // no launch has more row blocks than that: the rest of the table repeats
-        for (int m = 1; m <= kPlanRows; ++m)
-            ga.plan_by_m[m - 1] = m > m_cap && m > 1 ? ga.plan_by_m[m - 2]
-                                                    : (unsigned char)gemm_plan(m, ga.N_out, ga.bn_mask, ga.pairs != 0,
-                                                                               ga.pairs != 0 && may_split_k(MODE) && ga.K >= 2 * BK,
-                                                                               ga.force, is_gated(MODE), grid);
-        return grid;
-    }
-    for (int m = 1; m <= kPlanRows; ++m)
-        ga.plan_by_m[m - 1] = m > (T_cap + BM - 1) / BM && m > 1
-                                  ? ga.plan_by_m[m - 2]
-                                  : (unsigned char)gemm_plan(m, ga.N_out, ga.bn_mask, false, false, ga.force, is_gated(MODE), grid);
-    return grid;
+int plan_gemm(dcut_ctx* ctx, int T_cap, unsigned bn_mask, GemmArgs& ga) {
+    const Shape shape = {ga.N_out, ga.K, T_cap, is_gated(MODE), may_split_k(MODE), is_linear(MODE)};
+    const Launch l = plan(shape, Device{ctx->sm_count, ctx->ly_gemm_pairs, ctx->ly_gemm_pair_mode != 0, ctx->ly_gemm_force, bn_mask});
+    static_assert(sizeof(ga.plan_by_m) == sizeof(l.by_m), "one table");
+    memcpy(ga.plan_by_m, l.by_m, sizeof(l.by_m));
+    return l.grid;
 }
 
 template <int MODE>
@@ -1162,10 +1077,9 @@ dcut_status launch_planned_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, c
 }
 
 template <int MODE>
-dcut_status launch_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMaps& b2, int n_tiles,
-                        int T_cap, unsigned bn_mask, const GemmArgs& g, cudaStream_t stream) {
+dcut_status launch_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMaps& b2, int T_cap, unsigned bn_mask, const GemmArgs& g, cudaStream_t stream) {
     GemmArgs ga = g;
-    const int grid = plan_gemm<MODE>(ctx, n_tiles, T_cap, bn_mask, ga);
+    const int grid = plan_gemm<MODE>(ctx, T_cap, bn_mask, ga);
     return launch_planned_gemm<MODE>(ctx, a, b, b2, grid, ga, stream);
 }
 
@@ -1174,8 +1088,7 @@ dcut_status launch_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMa
 template <int MODE>
 dcut_status launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, int T_cap, GemmArgs& g, cudaStream_t stream) {
     const unsigned mask = (is_gated(MODE) ? ctx->ly_gemm_bn_mask & kBnMaskSwiGLU : ctx->ly_gemm_bn_mask) | 1u;
-    const int per = is_gated(MODE) ? BN / 2 : BN;
-    const int grid = plan_gemm<MODE>(ctx, (l->N + per - 1) / per, T_cap, mask, g);
+    const int grid = plan_gemm<MODE>(ctx, T_cap, mask, g);
     unsigned used = 0;
     for (int m = 0; m < kPlanRows && m <= (T_cap - 1) / BM; ++m) used |= 1u << (g.plan_by_m[m] & 7);
     AMaps am;
@@ -1319,7 +1232,7 @@ dcut_status dcut_launch_lm_head_argmax(dcut_ctx* ctx, const void* x, const void*
     g.row_key = row_key;
     g.V = V;
     g.status = ctx->d_status;
-    return launch_gemm<kArgmax>(ctx, am, bm, bm, (V + BN - 1) / BN, T_cap, 1u, g, stream);
+    return launch_gemm<kArgmax>(ctx, am, bm, bm, T_cap, 1u, g, stream);
 }
 
 dcut_status dcut_launch_gemm(dcut_ctx* ctx, const void* a, const void* w, const void* w2, int mode, int N, int K,
@@ -1344,9 +1257,9 @@ dcut_status dcut_launch_gemm(dcut_ctx* ctx, const void* a, const void* w, const 
     g.row_key = nullptr;
     g.V = 0;
     g.status = ctx->d_status;
-    if (mode == kSwiGLU) return launch_gemm<kSwiGLU>(ctx, am, bm, b2m, N / (BN / 2), T_cap, mask, g, stream);
-    if (mode == kResidual) return launch_gemm<kResidual>(ctx, am, bm, b2m, N / BN, T_cap, mask, g, stream);
-    return launch_gemm<kPlain>(ctx, am, bm, b2m, N / BN, T_cap, mask, g, stream);
+    if (mode == kSwiGLU) return launch_gemm<kSwiGLU>(ctx, am, bm, b2m, T_cap, mask, g, stream);
+    if (mode == kResidual) return launch_gemm<kResidual>(ctx, am, bm, b2m, T_cap, mask, g, stream);
+    return launch_gemm<kPlain>(ctx, am, bm, b2m, T_cap, mask, g, stream);
 }
 
 dcut_status dcut_launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, const int* cu_q, int B, int T_cap, cudaStream_t stream) {
@@ -1412,7 +1325,7 @@ dcut_status dcut_launch_layer(dcut_ctx* ctx, const dcut_layer_weights* w, const 
                               "launch rmsnorm_kernel")) != DCUT_OK) return st;
     // 2. qkv = n . Wqkv^T
     g.N_out = qkv_w; g.K = H; g.out = ctx->ly_qkv; g.residual = nullptr;
-    if ((st = launch_gemm<kPlain>(ctx, lm->act[0], wm->m[0], wm->m[0], qkv_w / BN, T_cap, wmask[0], g, stream)) != DCUT_OK) return st;
+    if ((st = launch_gemm<kPlain>(ctx, lm->act[0], wm->m[0], wm->m[0], T_cap, wmask[0], g, stream)) != DCUT_OK) return st;
     // 3. RoPE, append the new K/V to the paged cache
     RopeArgs r;
     r.qkv = ctx->ly_qkv; r.cu_q = cu_q; r.tok_req = tok_req; r.tok_pos = tok_pos; r.block_table = block_table;
@@ -1428,10 +1341,10 @@ dcut_status dcut_launch_layer(dcut_ctx* ctx, const dcut_layer_weights* w, const 
     g.N_out = H; g.K = q_w;
     if (part == 1) {
         g.out = static_cast<__nv_bfloat16*>(y); g.residual = nullptr;
-        return launch_gemm<kPlain>(ctx, lm->act[1], wm->m[1], wm->m[1], H / BN, T_cap, wmask[1], g, stream);
+        return launch_gemm<kPlain>(ctx, lm->act[1], wm->m[1], wm->m[1], T_cap, wmask[1], g, stream);
     }
     g.out = ctx->ly_h1; g.residual = static_cast<const __nv_bfloat16*>(x);
-    if ((st = launch_gemm<kResidual>(ctx, lm->act[1], wm->m[1], wm->m[1], H / BN, T_cap, wmask[1], g, stream)) != DCUT_OK) return st;
+    if ((st = launch_gemm<kResidual>(ctx, lm->act[1], wm->m[1], wm->m[1], T_cap, wmask[1], g, stream)) != DCUT_OK) return st;
     }
     // 6. n2 = RMSNorm(h1)   (the MLP half of a tensor-parallel layer starts here, from the caller's h1)
     const __nv_bfloat16* h1 = part == 2 ? static_cast<const __nv_bfloat16*>(x) : ctx->ly_h1;
@@ -1440,15 +1353,15 @@ dcut_status dcut_launch_layer(dcut_ctx* ctx, const dcut_layer_weights* w, const 
                               "launch rmsnorm_kernel")) != DCUT_OK) return st;
     // 7. act = SiLU(n2 . Wg^T) * (n2 . Wu^T)
     g.N_out = I; g.K = H; g.out = ctx->ly_act; g.residual = nullptr;
-    if ((st = launch_gemm<kSwiGLU>(ctx, lm->act[2], wm->m[2], wm->m[3], I / (BN / 2), T_cap, wmask[2], g, stream)) != DCUT_OK) return st;
+    if ((st = launch_gemm<kSwiGLU>(ctx, lm->act[2], wm->m[2], wm->m[3], T_cap, wmask[2], g, stream)) != DCUT_OK) return st;
     // 8. y = h1 + act . Wd^T
     g.N_out = H; g.K = I; g.out = static_cast<__nv_bfloat16*>(y);
     if (part == 2) {
         g.residual = nullptr;
-        return launch_gemm<kPlain>(ctx, lm->act[3], wm->m[4], wm->m[4], H / BN, T_cap, wmask[4], g, stream);
+        return launch_gemm<kPlain>(ctx, lm->act[3], wm->m[4], wm->m[4], T_cap, wmask[4], g, stream);
     }
     g.residual = ctx->ly_h1;
-    return launch_gemm<kResidual>(ctx, lm->act[3], wm->m[4], wm->m[4], H / BN, T_cap, wmask[4], g, stream);
+    return launch_gemm<kResidual>(ctx, lm->act[3], wm->m[4], wm->m[4], T_cap, wmask[4], g, stream);
 }
 
 namespace {

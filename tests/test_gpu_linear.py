@@ -227,3 +227,26 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     monkeypatch.setattr(ctx, "device", 1)                      # as if the context lived on the next GPU
     with pytest.raises(AssertionError):
         run(ctx, c)
+
+
+@pytest.mark.parametrize("T,cap,N,K", [(9700, 9700, 200, 600), (12345, 13000, 64, 1000), (9217, 9300, 33, 640), (100, 20000, 256, 520)])
+def test_very_many_rows_and_few_columns(T, cap, N, K):
+    """More row blocks than the table of plans has entries, where a single wave of pairs would do for that many and no more."""
+    ctx, c = context(), make(16, T, cap, N, K)
+    out = torch.full((cap, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    run(ctx, c, "relu", out=out)
+    assert ctx.poll_device_status() == 0
+    check(c, out, "relu")
+    assert (out[T:] == 7.0).all()
+
+
+def test_very_many_rows_of_the_layer_s_product():
+    from paper_2607_14647_b200 import binding
+    ctx = binding.Context(max_B=8192, max_gamma=1, n_q_heads=8, n_kv_heads=2, head_dim=128, max_pages_per_req=4)
+    T, N, K = 9700, 256, 640
+    c = make(17, T, T, N, K, bias=False, residual=True)
+    a, w, res = (c[n].contiguous() for n in ("a", "w", "residual"))
+    out = torch.full((T, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    ctx.gemm_bf16(a, w, torch.tensor([0, T], dtype=torch.int32, device="cuda"), T, out, mode=1, residual=res)
+    torch.cuda.synchronize()
+    check(c, out)
