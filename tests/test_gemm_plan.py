@@ -61,7 +61,8 @@ def test_few_columns_and_very_many_rows(lib, N, blocks):
 
 @pytest.mark.parametrize("force", [*range(7), *range(8, 15), *range(16, 23)])
 def test_a_forced_plan_is_taken_where_it_can_be(lib, force):
-    for T, N, K, gated in ((9, 331, 584, False), (300, 331, 600, False), (9, 331, 584, True), (300, 331, 600, True), (200, 777, 520, False)):
+    shapes = [(9, 331, 584), (300, 331, 600), (9, 336, 584), (300, 336, 600)]            # test_gpu_linear.py runs these
+    for T, N, K, gated in [(*s, g) for s in shapes for g in (False, True)] + [(200, 777, 520, False)]:
         p = plan(lib, N, K, T, gated, force=force)[0][-(-T // 128) - 1]
         can = (not gated or GATED >> (force & 7) & 1) and not (gated and force >= SPLIT)
         assert (p == force) == bool(can), (T, N, K, gated, p)

@@ -250,3 +250,28 @@ def test_very_many_rows_of_the_layer_s_product():
     ctx.gemm_bf16(a, w, torch.tensor([0, T], dtype=torch.int32, device="cuda"), T, out, mode=1, residual=res)
     torch.cuda.synchronize()
     check(c, out)
+
+
+@pytest.mark.parametrize("gated,plan", [(False, p) for p in (*range(7), *range(8, 15), *range(16, 23))] + [(True, p) for p in (0, 2, 4, 6, 8, 10, 12, 14)])
+def test_every_plan_at_lengths_that_can_take_it(plan, gated, monkeypatch):
+    """K above 512, so that pairs and split K are open (tests/test_gemm_plan.py holds that these launches do take the plan): the
+    half activation box, one and two pair tiles of rows, odd N (2-byte rows and residual); even N (vectors)."""
+    monkeypatch.setenv("DCUT_GEMM_FORCE", str(plan))
+    ctx = context()
+    for T, N, K in ((9, 331, 584), (300, 331, 600), (9, 336, 584), (300, 336, 600)):
+        c = make(plan + T, T, T, N, K, gated, True, True)
+        out = torch.full((T + 3, N), 7.0, dtype=torch.bfloat16, device="cuda")
+        run(ctx, c, "gelu", out=out)
+        assert ctx.poll_device_status() == 0
+        check(c, out, "gelu")
+        assert (out[T:] == 7.0).all()
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_few_k_blocks_whatever_is_forced(gated, monkeypatch):
+    """Up to K = 512 the pair modes are closed: a forced one falls back to the rule."""
+    monkeypatch.setenv("DCUT_GEMM_FORCE", "8")
+    ctx = context()
+    for T, N, K in ((9, 331, 512), (300, 331, 64)):
+        c = make(18 + T, T, T, N, K, gated, True, True)
+        check(c, run(ctx, c, "gelu"), "gelu")
