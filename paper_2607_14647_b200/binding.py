@@ -174,7 +174,7 @@ def _heads(dev: int, t: Optional[torch.Tensor], n_heads: int, head_dim: int):
     assert t.get_device() == dev and t.dtype == torch.bfloat16, f"expected a bf16 tensor on cuda:{dev}"
     assert len(shape) == 3 and shape[1] == n_heads and shape[2] == head_dim and strides[2] == 1, \
         f"expected [tokens, {n_heads}, {head_dim}] with dense heads, got {tuple(shape)} with strides {strides}"
-    return t.data_ptr(), strides[0], strides[1]
+    return t.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1] if n_heads > 1 else 0     # (of a single one the stride says nothing)
 
 
 def _rows(dev: int, t: Optional[torch.Tensor]):

@@ -66,3 +66,16 @@ def test_caches_of_two_sizes_are_refused_and_the_context_s_own_layout_is_taken(c
         call(ctx, caches()[0], caches((7, HKV, 16, D))[1])
     call(ctx, *caches())
     assert len(ctx.calls) == 1 and ctx.calls[0][6 if call is append else 4] == 6          # num_pages
+
+
+def test_strides_of_a_single_token_or_head_say_nothing(ctx):
+    """A single row of a buffer whose rows are no multiple of 8 apart; one key head cut out of a row of them."""
+    row = torch.zeros((1, HQ * D + 3), dtype=BF16)
+    append(ctx, *caches(), q=row[:, : HQ * D].view(1, HQ, D), k=torch.zeros((1, HKV, D), dtype=BF16), v=torch.zeros((1, HKV, D), dtype=BF16), T_cap=1)
+    x = ctx.calls[-1][1]._obj
+    assert (x.q_token_stride, x.q_head_stride, x.k_token_stride, x.k_head_stride) == (0, D, 0, D)
+    ctx._shape = (HQ, 1, D)
+    one = torch.zeros((T, 2 * D), dtype=BF16).as_strided((T, 1, D), (2 * D, 5, 1))
+    append(ctx, *caches((6, 1, 16, D)), k=one, v=torch.zeros((T, 1, D), dtype=BF16))
+    x = ctx.calls[-1][1]._obj
+    assert (x.q_token_stride, x.k_token_stride, x.k_head_stride, x.v_token_stride, x.v_head_stride) == (HQ * D, 2 * D, 0, D, 0)
