@@ -556,3 +556,25 @@ def test_a_key_of_a_request_that_is_no_number_shows(hq, hkv, d, deep, prefix, va
         out2 = ctx.verify_attn(c["q"], c["kc"], c["vc"], a["block_table"], a["ctx_lens"], a["cu_q"], c["cap"], lse=lse2)
         torch.cuda.synchronize()
         assert_not_numbers_where_the_formula_has_them(c, out2, lse2, out2, lse2)
+
+
+@pytest.mark.parametrize("counts,own,sizes,plens,hq,hkv,d", [([1] * 16, list(range(0, 160, 10)), [16], [512], 32, 8, 128), ([17] * 8 + [3] * 4, [30] * 12, [7, 5], [160, 2048], 16, 2, 128),
+                                                           ([5, 9, 1], [0, 40, 700], [3], [1008], 8, 8, 64)])
+def test_agrees_with_verify_attn_where_the_prefix_s_pages_are_joined_to_every_request_s(counts, own, sizes, plens, hq, hkv, d):
+    c = make_case(44, counts, own, sizes, plens, hq, hkv, d)
+    group = np.repeat(np.arange(c["G"]), sizes)
+    joined = np.full((c["B"], max(plens) // 16 + c["table"].shape[1]), -1)
+    for r in range(c["B"]):
+        n = plens[group[r]] // 16
+        joined[r, :n] = c["ptable"][group[r], :n]
+        joined[r, n:n + c["table"].shape[1]] = c["table"][r]
+    ctx = make_ctx(c)
+    out, lse = run(c, ctx)
+    from paper_2607_14647_b200 import binding
+    whole = binding.Context(max_B=c["B"], max_gamma=max(1, max(counts) - 1), n_q_heads=hq, n_kv_heads=hkv, head_dim=d, max_pages_per_req=joined.shape[1])
+    lse2 = torch.empty_like(lse)
+    out2 = whole.verify_attn(c["q"], c["kc"], c["vc"], _i32(joined), _i32(c["ctx"]), _i32(c["cu"]), c["cap"], lse=lse2)
+    torch.cuda.synchronize()
+    assert whole.poll_device_status() == 0
+    check(c, out, lse)
+    check(c, out2, lse2)

@@ -277,12 +277,12 @@ def test_rows_past_the_capacity_are_reported():
 
 
 def test_one_token_from_a_row_of_any_length():
-    """The only row of a buffer whose rows are no multiple of 8 elements apart."""
+    """The first row of a buffer whose rows are no multiple of 8 elements apart."""
     ctx = _ctx(1, 8, 2, 128)
     c = _case(14, [1], [37], 8, 2, 128, 128, layout="dense")
     for n, h in (("q", 8), ("k", 2), ("v", 2)):
-        row = torch.zeros((1, h * 128 + 3), dtype=torch.bfloat16, device="cuda")
-        row[:, : h * 128] = c[n].reshape(1, -1)
-        c[n] = row[:, : h * 128].view(1, h, 128)
+        rows = torch.zeros((2, h * 128 + 3), dtype=torch.bfloat16, device="cuda")
+        rows[:1, : h * 128] = c[n].reshape(1, -1)
+        c[n] = rows[:, : h * 128].view(2, h, 128)[:1]
         assert c[n].stride(0) % 8
     _both(ctx, c)

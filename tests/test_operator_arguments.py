@@ -69,9 +69,10 @@ def test_caches_of_two_sizes_are_refused_and_the_context_s_own_layout_is_taken(c
 
 
 def test_strides_of_a_single_token_or_head_say_nothing(ctx):
-    """A single row of a buffer whose rows are no multiple of 8 apart; one key head cut out of a row of them."""
-    row = torch.zeros((1, HQ * D + 3), dtype=BF16)
-    append(ctx, *caches(), q=row[:, : HQ * D].view(1, HQ, D), k=torch.zeros((1, HKV, D), dtype=BF16), v=torch.zeros((1, HKV, D), dtype=BF16), T_cap=1)
+    """The first row of a buffer whose rows are no multiple of 8 apart; one key head with any stride."""
+    q = torch.zeros((2, HQ * D + 3), dtype=BF16)[:, : HQ * D].view(2, HQ, D)[:1]
+    assert q.stride(0) % 8
+    append(ctx, *caches(), q=q, k=torch.zeros((1, HKV, D), dtype=BF16), v=torch.zeros((1, HKV, D), dtype=BF16), T_cap=1)
     x = ctx.calls[-1][1]._obj
     assert (x.q_token_stride, x.q_head_stride, x.k_token_stride, x.k_head_stride) == (0, D, 0, D)
     ctx._shape = (HQ, 1, D)
