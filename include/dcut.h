@@ -453,6 +453,8 @@ dcut_status dcut_rope_append(dcut_ctx* ctx, const dcut_qkv* qkv, const dcut_rope
  * types and layouts, softmax over all positions j = 0 .. L_i + t) where position j lies as dcut_prefix_groups says.  The
  * shared positions of a group are read once for all its rows, on the tensor cores; ctx_lens[i] = L_i counts the prefix, so
  * L_i >= prefix_lens of the request's group.  Slots behind prefix_lens[g] in the prefix's last page may hold anything.
+ * It takes five launches where dcut_verify_attn takes three: below about 10^5 positions in all (requests x prefix length), with a
+ * prefix of whole pages, dcut_verify_attn on block tables that begin with the shared pages is faster.
  * DEVICE in: q bf16 [T_cap rows readable, n_q_heads, head_dim], the caches, block_table (own pages), ctx_lens, cu_q, the
  *   arrays of `groups` (n_groups <= B; the struct is read during the call only).  DEVICE out: out, lse as dcut_verify_attn;
  *   rows from cu_q[B] on are not touched.

@@ -22,10 +22,10 @@
 // team exponentiates one block, the tensor cores fill its other buffer, and a step has two hand-overs only (S to the
 // softmax, P to the MMAs), each of about 190 cycles between warps.
 // An odd last tile is a single: both teams work on the one tile, taking its key blocks in turn, and merge at the end.
-// P is rounded to bf16 (relative 2^-9, as V's type asks of the MMA); everything else stays in fp32 until the one rounding
-// of the output.
+// P is rounded to bf16 (half a step, 2^-8 of the weight at most, as V's type asks of the MMA); everything else stays in fp32
+// until the one rounding of the output.
 //
-// Measured: 2176 tokens of 32q/8kv heads behind 8192 keys (292 Gflop) 318 us of a call of 398; a pair of tiles takes 1900 to
+// Measured: 2176 tokens of 32q/8kv heads behind 8192 keys (292 Gflop) 318 us of a call of 398 to 407; a pair of tiles takes 1900 to
 // 2050 cycles per block, of which the tensor pipe is busy for 1544 (Q K^T with both operands in shared memory runs at half
 // rate at N = 64), the MUFU for 1024; the softmax code alone takes 1300.  Blocks of 128 or 80 keys with one S buffer per
 // tile: 317 and 297-338 us.  Rescaling by a stale maximum 636 (spills), warps taking turns 592.
@@ -331,8 +331,8 @@ __device__ __forceinline__ void produce(const CUtensorMap& q_map, const CUtensor
 
 // The issuer of one team's products.  One elected lane (not `lane == 0`: the compiler then keeps the operands of
 // tcgen05.mma in uniform registers) runs the whole role.  Each team has an issuer of its own: issuing an MMA lasts as long
-// as the MMA (about 51 cycles for Q K^T of 80 keys, 54-61 for P V of 16), a wait for a barrier about 150 even when its
-// phase is over, and while one issuer waits the other feeds the tensor pipe.
+// as the MMA (73 cycles for Q K^T of 64 keys and 16 of the head's elements, 65 for P V of 16 keys, at head size 128), a wait for
+// a barrier about 150 even when its phase is over, and while one issuer waits the other feeds the tensor pipe.
 template <int DH>
 __device__ __forceinline__ void issue(const PrefixArgs& a, unsigned char* smem, Ctrl* c, Walk w, const int team) {
     using L = Smem<DH>;
@@ -347,10 +347,6 @@ __device__ __forceinline__ void issue(const PrefixArgs& a, unsigned char* smem, 
     int base = 0, base_phase = 0;         // ring slot of the item's first K block, and its phase
     bool ok = true;
     auto wait = [&](uint32_t bar, int parity) { return mbar_wait(bar, parity & 1, &c->abort); };
-    // both phases, asked for together: two answers in the time of one
-    auto wait2 = [&](uint32_t bar0, int parity0, uint32_t bar1, int parity1) {
-        return wait(bar0, parity0) && wait(bar1, parity1);
-    };
     while (ok && next_item(w, a.groups, &it)) {
         if (it.blocks == 0) continue;
         const int nblk = it.b1 - it.b0;
@@ -401,7 +397,7 @@ __device__ __forceinline__ void issue(const PrefixArgs& a, unsigned char* smem, 
         // second team may have no block).
         if (ok && n_items > 0) ok = wait(smem_u32(&c->o_free), n_items - 1);
         for (int s = 0; ok && s < steps; ++s) {
-            if (!wait2(kv_full + 8 * v_slot, v_phase, p_full + 8 * (n_pv & 1), n_pv >> 1)) {
+            if (!wait(kv_full + 8 * v_slot, v_phase) || !wait(p_full + 8 * (n_pv & 1), n_pv >> 1)) {
                 ok = false;
                 break;
             }
@@ -417,7 +413,7 @@ __device__ __forceinline__ void issue(const PrefixArgs& a, unsigned char* smem, 
             }
             tc_commit(pv_done);
             const bool more = s + 2 < steps;
-            if (!(more ? wait2(pv_done, n_pv, kv_full + 8 * k_slot, k_phase) : wait(pv_done, n_pv))) {
+            if (!wait(pv_done, n_pv) || (more && !wait(kv_full + 8 * k_slot, k_phase))) {
                 ok = false;
                 break;
             }

@@ -26,7 +26,7 @@ constexpr int kMaxSegs = 256;
 // Cost of a key block and of an item beyond its blocks; only the ratios matter.  A block of a single lasts as long as one of a
 // dual (both are a chain of hand-overs), and an item costs about six blocks beyond its own: filling the chain, draining
 // it and writing 256 rows.  Measured, (dual, single, item) on 48 requests of 64q/8kv heads in three groups, one of them
-// without a prefix / on 64 requests of 32q/8kv behind 4099 keys: (16, 10, 30) 257 / 166 us, (16, 10, 100) 179 / 170,
+// without a prefix / on 64 requests of 32q/8kv behind 4099 keys (no other batch was tried): (16, 10, 30) 257 / 166 us, (16, 10, 100) 179 / 170,
 // (16, 13, 100) 161 / 158, (16, 16, 60) 185 / 158, (16, 16, 100) 157 / 157, (16, 20, 80) 161 / 159.
 constexpr long long kCostDual = 16, kCostSingle = 16, kCostItem = 100;
 
