@@ -503,6 +503,44 @@ typedef struct {
 dcut_status dcut_linear(dcut_ctx* ctx, const dcut_linear_args* args, const int* cu_q, int B, int T_cap, void* stream);
 
 /*
+ * A target held in 8 bits: dcut_rms_norm writes the 8-bit rows, dcut_linear8 multiplies them.
+ *
+ * dcut_rms_norm: the residual's addition, the RMS norm and the rounding to 8 bits in one pass, for the rows r < cu_q[B]:
+ *   h = x + residual                                        (residual NULL: h = x)
+ *   y = h gain / sqrt(mean(h^2) + rms_eps), normed != 0     (gain NULL: 1; gain_plus_one != 0: 1 + gain), else y = h
+ *   h_out = bf16(h);  out = bf16(y);  scale8[r] = max(max|y_r|, 2^-100) / 448,  out8 = e4m3(y / scale8[r])
+ * in fp32 with one rounding per output (h is normalised before its rounding).  Each of h_out, out and the pair (out8, scale8) may
+ * be NULL, not all of them.  A row with a NaN or an infinity in y gets the scale NaN (and NaN in out8).
+ * normed = 0 quantises rows: the attention's output ahead of the O projection, an MLP's activation, or a weight at load
+ * time (its rows are output channels: dcut_linear8's w_scale).
+ * DEVICE in: x, residual bf16 [T_cap, width], gain bf16 [width].  DEVICE out: h_out, out bf16, out8 e4m3 (1 byte) [T_cap, width], scale8
+ * fp32 [T_cap].  ld*: elements from row to row, >= width; any of them and any alignment of the type serve, but rows that start on
+ * 16 bytes (out8: 8) are moved in vectors.  h_out may be x or the residual, out may be x, each with that one's stride; nothing else may overlap.
+ * cu_q int32 [B+1], or NULL: all T_cap rows (B is not looked at).  width up to 32768; T_cap is not bound by dcut_limits.  A
+ * cu_q[B] above T_cap sets device status 10; rows from cu_q[B] on are not touched.  The struct is HOST memory, read during the call.
+ */
+typedef struct {
+    const void* x;
+    long long ldx;
+    const void* residual;
+    long long ldr;
+    const void* gain;
+    int gain_plus_one;
+    int normed;
+    float rms_eps;             /* > 0 where normed */
+    int width;
+    void* h_out;
+    long long ldh;
+    void* out;
+    long long ldo;
+    void* out8;
+    long long ld8;
+    float* scale8;
+} dcut_norm_args;
+#define DCUT_NORM_MAX_WIDTH 32768
+dcut_status dcut_rms_norm(dcut_ctx* ctx, const dcut_norm_args* args, const int* cu_q, int B, int T_cap, void* stream);
+
+/*
  * dcut_accept without any allocation.  (The paper has no counterpart: this entry point exists for
  * the way the library gets embedded, not for the method.)
  *
@@ -592,8 +630,8 @@ dcut_status dcut_verify_step_host(dcut_ctx* ctx, const dcut_host_step* step, voi
  * (rows at or past T_cap were left out: nothing outside the caller's T_cap rows is read or written), 8 =
  * dcut_rope_append met a token whose request, group or position has no place in the block table (it was left out), 9 =
  * dcut_prefix_attn met groups that do not cover the batch, a prefix or own positions that do not fit (nothing was written;
- * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear or dcut_rope_append met a cu_q[B] above T_cap
- * (rows from T_cap on were left out). */
+ * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear, dcut_rope_append or dcut_rms_norm met a
+ * cu_q[B] above T_cap (rows from T_cap on were left out). */
 dcut_status dcut_poll_device_status(dcut_ctx* ctx, int* code, void* stream);
 
 #ifdef __cplusplus

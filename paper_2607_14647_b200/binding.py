@@ -33,7 +33,7 @@ EXPORTS = ["dcut_create", "dcut_destroy", "dcut_last_error", "dcut_set_cost_dens
            "dcut_enable_plan_in_select", "dcut_cost_grid_create", "dcut_cost_grid_destroy", "dcut_cost_grid_budget",
            "dcut_cost_grid_record", "dcut_cost_grid_get", "dcut_cost_grid_nearest", "dcut_cost_grid_buckets",
            "dcut_set_cost_from_grid", "dcut_layer_attn_part", "dcut_layer_mlp_part", "dcut_residual_add",
-           "dcut_rope_append", "dcut_enable_prefix_attn", "dcut_prefix_attn", "dcut_linear"]
+           "dcut_rope_append", "dcut_enable_prefix_attn", "dcut_prefix_attn", "dcut_linear", "dcut_rms_norm"]
 
 
 class Limits(C.Structure):
@@ -134,6 +134,14 @@ _lib.dcut_enable_prefix_attn.argtypes = [_vp, _i]
 _lib.dcut_prefix_attn.argtypes = [_vp, _vp, _vp, _vp, _ll, _vp, _i, _vp, _vp, _i, _i, C.POINTER(PrefixGroupsRec), _f, _vp, _vp, _vp]
 
 
+class NormArgs(C.Structure):
+    _fields_ = [("x", _vp), ("ldx", _ll), ("residual", _vp), ("ldr", _ll), ("gain", _vp), ("gain_plus_one", _i), ("normed", _i), ("rms_eps", _f),
+                ("width", _i), ("h_out", _vp), ("ldh", _ll), ("out", _vp), ("ldo", _ll), ("out8", _vp), ("ld8", _ll), ("scale8", _vp)]
+
+
+_lib.dcut_rms_norm.argtypes = [_vp, C.POINTER(NormArgs), _vp, _i, _i, _vp]
+
+
 @dataclass
 class PreparedModel:
     rec: "Model"
@@ -177,13 +185,18 @@ def _heads(dev: int, t: Optional[torch.Tensor], n_heads: int, head_dim: int):
     return t.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1] if n_heads > 1 else 0     # (of a single one the stride says nothing)
 
 
-def _rows(dev: int, t: Optional[torch.Tensor]):
-    """(pointer, row stride) of a bf16 [rows, columns] view whose rows are dense."""
+def _rows(dev: int, t: Optional[torch.Tensor], dtype=torch.bfloat16, step16: int = 8):
+    """(pointer, row stride) of a [rows, columns] view whose rows are dense; step16: elements of 16 bytes."""
     if t is None:
         return None, 0
     (rows, cols), (ld, step) = t.shape, t.stride()
-    assert t.get_device() == dev and t.dtype == torch.bfloat16 and (step == 1 or cols == 1), f"expected a bf16 matrix with dense rows on cuda:{dev}"
-    return t.data_ptr(), ld if rows > 1 else (cols + 7) // 8 * 8                         # (one row: its stride says nothing)
+    assert t.get_device() == dev and t.dtype == dtype and (step == 1 or cols == 1), f"expected a matrix of {dtype} with dense rows on cuda:{dev}"
+    return t.data_ptr(), ld if rows > 1 else (cols + step16 - 1) // step16 * step16      # (one row: its stride says nothing)
+
+
+def rows8(rows: int, cols: int, device="cuda") -> torch.Tensor:
+    """Room for e4m3 rows as linear8 reads them: rows start on 16 bytes."""
+    return torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)[:, :cols]
 
 
 def rope_inv_freq(theta: float, rotary_dim: int, device="cuda") -> torch.Tensor:
@@ -611,6 +624,33 @@ class Context:
                        ACTIVATIONS[act])
         self._check(_lib.dcut_linear(self._h, C.byref(l), _on(dev, cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, self._stream()))
         return out
+
+    def rms_norm(self, x, cu_q, T_cap: int, gain=None, rms_eps: float = 1e-6, residual=None, h_out=None, out=None, out8=None, scale8=None,
+                 gain_plus_one: bool = False):
+        """dcut_rms_norm: h = x + residual to `h_out`, its RMS norm to `out` (bf16) and / or to `out8` (e4m3, see rows8) with the rows'
+        scales in `scale8` (fp32); the outputs that are given are written.  Matrices may be views with padded rows; cu_q None: all rows."""
+        self._norm(x, cu_q, T_cap, True, gain, rms_eps, residual, h_out, out, out8, scale8, gain_plus_one)
+
+    def quantize(self, x, cu_q, T_cap: int, residual=None, h_out=None, out=None, out8=None, scale8=None):
+        """dcut_rms_norm without the norm: the rows of x (+ residual) in e4m3 with a scale each.  Returns (out8, scale8)."""
+        if out8 is None:
+            out8 = rows8(T_cap, x.shape[1], x.device)
+        if scale8 is None:
+            scale8 = torch.empty(T_cap, dtype=torch.float32, device=x.device)
+        self._norm(x, cu_q, T_cap, False, None, 0.0, residual, h_out, out, out8, scale8, False)
+        return out8, scale8
+
+    def _norm(self, x, cu_q, T_cap, normed, gain, rms_eps, residual, h_out, out, out8, scale8, gain_plus_one):
+        width, dev = x.shape[1], self.device
+        for t in (x, residual, h_out, out, out8):
+            assert t is None or (t.shape[0] >= T_cap and t.shape[1] == width), f"expected [T_cap rows, {width}], got {tuple(t.shape)}"
+        assert gain is None or gain.shape == (width,)
+        assert scale8 is None or scale8.numel() >= T_cap
+        (xp, ldx), (rp, ldr), (hp, ldh), (op, ldo) = _rows(dev, x), _rows(dev, residual), _rows(dev, h_out), _rows(dev, out)
+        p8, ld8 = _rows(dev, out8, torch.float8_e4m3fn, 16)
+        n = NormArgs(xp, ldx, rp, ldr, _on(dev, gain, torch.bfloat16), int(gain_plus_one), int(normed), rms_eps, width, hp, ldh, op, ldo, p8, ld8,
+                     _on(dev, scale8, torch.float32))
+        self._check(_lib.dcut_rms_norm(self._h, C.byref(n), _on(dev, cu_q, torch.int32), 0 if cu_q is None else cu_q.shape[0] - 1, T_cap, self._stream()))
 
     def make_model(self, layers: list, embed, g_final, w_lm, k_caches: list, v_caches: list, rms_eps: float = 1e-6,
                    rope_theta: float = 1e6) -> "PreparedModel":

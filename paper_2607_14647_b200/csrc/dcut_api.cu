@@ -641,6 +641,28 @@ dcut_status dcut_linear(dcut_ctx* c, const dcut_linear_args* l, const int* cu_q,
     return dcut_launch_linear(c, l, cu_q, B, T_cap, static_cast<cudaStream_t>(stream));
 }
 
+dcut_status dcut_rms_norm(dcut_ctx* c, const dcut_norm_args* n, const int* cu_q, int B, int T_cap, void* stream) {
+    if (!c) return DCUT_EINVAL;
+    if (!n || !n->x || (n->out8 != nullptr) != (n->scale8 != nullptr)) return dcut_fail(c, DCUT_EINVAL, "null pointer argument (out8 and scale8 go together)");
+    if (!n->h_out && !n->out && !n->out8) return dcut_fail(c, DCUT_EINVAL, "no output");
+    if (n->gain && !n->normed) return dcut_fail(c, DCUT_EINVAL, "a gain goes with the norm");
+    if ((cu_q && B < 1) || T_cap < 1 || n->width < 1) return dcut_fail(c, DCUT_EINVAL, "need B, T_cap, width >= 1");
+    if (n->width > DCUT_NORM_MAX_WIDTH) return dcut_fail(c, DCUT_ECAPACITY, "width = %d exceeds %d", n->width, DCUT_NORM_MAX_WIDTH);
+    if (n->normed && (!(n->rms_eps > 0.0f) || isinf(n->rms_eps))) return dcut_fail(c, DCUT_EINVAL, "rms_eps must be > 0 and finite");
+    const void* rows[5] = {n->x, n->residual, n->h_out, n->out, n->out8};
+    const long long ld[5] = {n->ldx, n->ldr, n->ldh, n->ldo, n->ld8};
+    for (int i = 0; i < 5; ++i)
+        if (rows[i] && (ld[i] < n->width || ld[i] > (1ll << 32))) return dcut_fail(c, DCUT_EINVAL, "row strides must be >= width and <= 2^32");
+    const uintptr_t al2 = reinterpret_cast<uintptr_t>(n->x) | reinterpret_cast<uintptr_t>(n->residual) | reinterpret_cast<uintptr_t>(n->gain) |
+                          reinterpret_cast<uintptr_t>(n->h_out) | reinterpret_cast<uintptr_t>(n->out);
+    if ((al2 & 1) || (reinterpret_cast<uintptr_t>(n->scale8) & 3)) return dcut_fail(c, DCUT_EINVAL, "bf16 arguments must be 2-byte aligned, scale8 4-byte");
+    if ((n->h_out && ((n->h_out == n->x && n->ldh != n->ldx) || (n->h_out == n->residual && n->ldh != n->ldr))) || (n->out && n->out == n->x && n->ldo != n->ldx))
+        return dcut_fail(c, DCUT_EINVAL, "an output over an input needs the same stride");
+    if (n->out && (n->out == n->h_out || n->out == n->residual)) return dcut_fail(c, DCUT_EINVAL, "out must not be h_out or the residual");
+    DCUT_ON_DEVICE(c);
+    return dcut_launch_rms_norm(c, n, cu_q, B, T_cap, static_cast<cudaStream_t>(stream));
+}
+
 dcut_status dcut_poll_device_status(dcut_ctx* c, int* code, void* stream) {
     if (!c) return DCUT_EINVAL;
     DeviceGuard guard(c->device);

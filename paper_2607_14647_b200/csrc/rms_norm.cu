@@ -1,0 +1,252 @@
+// dcut_rms_norm: the residual's addition, the RMS norm and the 8-bit rows that dcut_linear8 reads, in one pass over a row.
+//
+//   h = x + residual;   y = (h * gain) * r,  r = 1 / sqrt(mean(h^2) + eps)   (or y = h);   scale = max(max|y|, 2^-100) / 448,
+//   y8 = e4m3(y / scale)
+//
+// Every byte is read once and written once: bound by HBM for thousands of rows, by the launch and one trip to memory for few.
+// A row stays in registers.  max|y| = r * max|h * gain| (rounding is monotone, r > 0), so the sum of squares and the maximum
+// leave through one reduction and the row is finished behind a single barrier.  Sum and statistics are fp32, h is normalised
+// before it is rounded to bf16; each output is rounded once.
+// A sum of squares that overflows (|h| above about 10^18) is formed again from h * 2^-80.  The maximum keeps a NaN.
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include "dcut_internal.h"
+
+namespace {
+
+constexpr int kMaxThreads = 1024;
+constexpr float kE4m3Max = 448.0f;
+constexpr float kLeast = 7.888609052210118e-31f;       // 2^-100: 448 / it and it / 448 are normal numbers
+
+struct NormArgs {
+    const __nv_bfloat16 *x, *residual, *gain;          // residual, gain may be null
+    long long ldx, ldr, ldh, ldo, ld8;
+    __nv_bfloat16 *h_out, *out;                        // may be null
+    unsigned char* out8;                               // may be null (with scale8)
+    float* scale8;
+    const int* cu_q;                                   // or null: T_cap rows
+    int B, T_cap, width, normed;
+    float eps, gain_add;                               // gain_add: 0, or 1 (the factor is 1 + gain)
+    int* status;
+};
+
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ void unpack8(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[2 * j] = bf_lo(w[j]), x[2 * j + 1] = bf_hi(w[j]);
+}
+// the larger magnitude (its sign says nothing); NaN if either is
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// two values to e4m3, round to nearest even, saturating; the first goes to the low byte
+__device__ __forceinline__ uint32_t e4m3x2(float first, float second) {
+    unsigned short r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(second), "f"(first));
+    return r;
+}
+
+// Where slot i of a thread lies: VEC: 8 neighbouring elements, read and written as vectors (the row's last one may be partly
+// used); otherwise element j of the slot is `threads` elements after element j - 1, so that a warp's 2-byte accesses are neighbours.
+template <bool VEC>
+struct Place {
+    int first, step, live;                             // live: elements of the slot that exist
+    __device__ __forceinline__ Place(int slot, int tid, int threads, int width) {
+        if (VEC) {
+            first = (slot * threads + tid) * 8, step = 1;
+            live = min(8, max(0, width - first));
+        } else {
+            first = slot * 8 * threads + tid, step = threads;
+            live = first < width ? min(8, (width - first + threads - 1) / threads) : 0;
+        }
+    }
+    __device__ __forceinline__ uint4 load(const __nv_bfloat16* row) const {
+        if (VEC && live == 8) return *reinterpret_cast<const uint4*>(row + first);
+        uint32_t w[4] = {0, 0, 0, 0};
+        const unsigned short* p = reinterpret_cast<const unsigned short*>(row) + first;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < live) w[j >> 1] |= (uint32_t)p[j * step] << (16 * (j & 1));
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16* row, const float (&v)[8]) const {
+        const uint32_t w[4] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        if (VEC && live == 8) {
+            *reinterpret_cast<uint4*>(row + first) = make_uint4(w[0], w[1], w[2], w[3]);
+            return;
+        }
+        unsigned short* p = reinterpret_cast<unsigned short*>(row) + first;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < live) p[j * step] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+    }
+    __device__ __forceinline__ void store8(unsigned char* row, const float (&v)[8]) const {
+        const uint32_t w[2] = {e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16};
+        if (VEC && live == 8) {
+            *reinterpret_cast<uint2*>(row + first) = make_uint2(w[0], w[1]);
+            return;
+        }
+        unsigned char* p = row + first;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < live) p[j * step] = (unsigned char)(w[j >> 2] >> (8 * (j & 3)));
+    }
+};
+
+struct Stats {
+    float sum, top;
+};
+// Over the threads of a row, in a fixed order: a warp's by shuffles, then (ALONE: a row per CTA) the warps'.
+template <bool ALONE>
+__device__ __forceinline__ Stats over_row(Stats s, Stats* warps) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        s.sum += __shfl_xor_sync(0xffffffffu, s.sum, o);
+        s.top = larger(s.top, __shfl_xor_sync(0xffffffffu, s.top, o));
+    }
+    if (!ALONE) return s;
+    const int lane = threadIdx.x & 31, n_warps = blockDim.x >> 5;
+    if (lane == 0) warps[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = lane < n_warps ? warps[lane] : Stats{0.0f, 0.0f};
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        s.sum += __shfl_xor_sync(0xffffffffu, s.sum, o);
+        s.top = larger(s.top, __shfl_xor_sync(0xffffffffu, s.top, o));
+    }
+    return s;
+}
+
+// V slots per thread; ALONE: the CTA has one row, otherwise every warp its own.
+template <int V, bool VEC, bool ALONE>
+__global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
+    __shared__ Stats warps[2][32];
+    dcut_pdl_wait();
+    dcut_pdl_launch_dependents();
+    const int T = a.cu_q ? a.cu_q[a.B] : a.T_cap;
+    if (T > a.T_cap && blockIdx.x == 0 && threadIdx.x == 0) atomicExch(a.status, DCUT_DEV_BAD_ROWS);
+    const int row = ALONE ? blockIdx.x : blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    const int tid = ALONE ? threadIdx.x : threadIdx.x & 31, threads = ALONE ? blockDim.x : 32;
+    if (row >= min(T, a.T_cap)) return;
+
+    const __nv_bfloat16* x_row = a.x + (size_t)row * a.ldx;
+    const __nv_bfloat16* r_row = a.residual ? a.residual + (size_t)row * a.ldr : nullptr;
+    uint4 xv[V], rv[V], gv[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const Place<VEC> at(i, tid, threads, a.width);
+        xv[i] = at.load(x_row);
+        if (r_row) rv[i] = at.load(r_row);
+        if (a.gain) gv[i] = at.load(a.gain);
+    }
+    float h[V][8];
+    Stats s = {0.0f, 0.0f};
+    auto factor = [&](int i, float (&g)[8]) {
+        if (!a.gain) return;
+        unpack8(gv[i], g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] += a.gain_add;
+    };
+    auto take = [&](int i) {                           // elements that do not exist are zeros
+        float g[8];
+        factor(i, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s.sum = fmaf(h[i][j], h[i][j], s.sum);
+            s.top = larger(s.top, a.gain ? h[i][j] * g[j] : h[i][j]);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        unpack8(xv[i], h[i]);
+        if (r_row) {
+            float r[8];
+            unpack8(rv[i], r);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[i][j] += r[j];
+        }
+        if (a.h_out) Place<VEC>(i, tid, threads, a.width).store(a.h_out + (size_t)row * a.ldh, h[i]);
+        take(i);
+    }
+    s = over_row<ALONE>(s, warps[0]);
+    float r = 1.0f;
+    if (a.normed) {
+        float eps = a.eps;
+        if (!(s.sum < INFINITY) || !(fabsf(s.top) < INFINITY)) {      // (the same answer in every thread of the row)
+            s = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[i][j] *= 0x1p-80f;
+                take(i);
+            }
+            s = over_row<ALONE>(s, warps[1]);
+            eps = eps * 0x1p-80f * 0x1p-80f;
+        }
+        r = 1.0f / sqrtf(s.sum / (float)a.width + eps);
+    }
+    const float top = fabsf(s.top) * r;
+    const float most = top < INFINITY ? fmaxf(top, kLeast) : NAN;     // a row with a value that is no number has no scale
+    const float inv = kE4m3Max / most;
+    if (a.out8 && tid == 0) a.scale8[row] = most / kE4m3Max;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const Place<VEC> at(i, tid, threads, a.width);
+        float g[8], y[8];
+        factor(i, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = a.gain ? h[i][j] * g[j] * r : h[i][j] * r;
+        if (a.out) at.store(a.out + (size_t)row * a.ldo, y);
+        if (a.out8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] *= inv;
+            at.store8(a.out8 + (size_t)row * a.ld8, y);
+        }
+    }
+}
+
+template <int V>
+cudaError_t launch(const NormArgs& a, bool vec, int threads, cudaStream_t stream) {
+    if (threads == 32) {
+        constexpr int kRows = 4;
+        const dim3 grid((a.T_cap + kRows - 1) / kRows), block(32 * kRows);
+        return vec ? dcut_launch_pdl(rms_norm_kernel<V, true, false>, grid, block, 0, stream, a)
+                   : dcut_launch_pdl(rms_norm_kernel<V, false, false>, grid, block, 0, stream, a);
+    }
+    return vec ? dcut_launch_pdl(rms_norm_kernel<V, true, true>, dim3(a.T_cap), dim3(threads), 0, stream, a)
+               : dcut_launch_pdl(rms_norm_kernel<V, false, true>, dim3(a.T_cap), dim3(threads), 0, stream, a);
+}
+
+}  // namespace
+
+dcut_status dcut_launch_rms_norm(dcut_ctx* ctx, const dcut_norm_args* n, const int* cu_q, int B, int T_cap, cudaStream_t stream) {
+    NormArgs a;
+    a.x = static_cast<const __nv_bfloat16*>(n->x);
+    a.residual = static_cast<const __nv_bfloat16*>(n->residual);
+    a.gain = static_cast<const __nv_bfloat16*>(n->gain);
+    a.ldx = n->ldx, a.ldr = n->ldr, a.ldh = n->ldh, a.ldo = n->ldo, a.ld8 = n->ld8;
+    a.h_out = static_cast<__nv_bfloat16*>(n->h_out);
+    a.out = static_cast<__nv_bfloat16*>(n->out);
+    a.out8 = static_cast<unsigned char*>(n->out8);
+    a.scale8 = n->scale8;
+    a.cu_q = cu_q, a.B = B, a.T_cap = T_cap, a.width = n->width, a.normed = n->normed != 0;
+    a.eps = n->rms_eps, a.gain_add = n->gain_plus_one ? 1.0f : 0.0f;
+    a.status = ctx->d_status;
+    auto rows16 = [](const void* p, long long ld) { return !p || (!(reinterpret_cast<uintptr_t>(p) & 15) && ld % 8 == 0); };
+    const bool vec = rows16(a.x, a.ldx) && rows16(a.residual, a.ldr) && rows16(a.gain, 0) && rows16(a.h_out, a.ldh) && rows16(a.out, a.ldo) &&
+                     !((reinterpret_cast<uintptr_t>(a.out8) | (uintptr_t)(a.out8 ? a.ld8 : 0)) & 7);
+    const int slots = (a.width + 7) / 8;
+    const int per = slots > 4 * 512 ? 4 : slots > 256 ? 2 : 1;
+    int threads = ((slots + per - 1) / per + 31) & ~31;
+    cudaError_t e = per == 1 ? launch<1>(a, vec, threads, stream) : per == 2 ? launch<2>(a, vec, threads, stream) : launch<4>(a, vec, threads, stream);
+    return dcut_check_cuda(ctx, e, "launch rms_norm_kernel");
+}

@@ -67,3 +67,15 @@ def linear(a, w, bias=None, act="none", w2=None, bias2=None, residual=None):
     if w2 is not None:
         z = z * (a @ w2.T + (0 if bias2 is None else bias2))
     return z if residual is None else z + residual
+
+
+def rms_norm(x, residual, normed, gain, eps, plus_one):
+    """(h, y) of dcut_rms_norm in 64 bits."""
+    h = x if residual is None else x + residual
+    y = h
+    if normed:
+        big = np.maximum(np.abs(h).max(1, keepdims=True), 1.0)                 # (squares of large values)
+        y = h / big / np.sqrt(((h / big) ** 2).mean(1, keepdims=True) + eps / big / big)
+        if gain is not None:
+            y = y * (gain + (1.0 if plus_one else 0.0))
+    return h, y
