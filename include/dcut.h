@@ -541,6 +541,34 @@ typedef struct {
 dcut_status dcut_rms_norm(dcut_ctx* ctx, const dcut_norm_args* args, const int* cu_q, int B, int T_cap, void* stream);
 
 /*
+ * dcut_linear on 8-bit operands with a scale per row of each (dcut_rms_norm makes both):
+ *   out[r, :] = residual[r, :] + act((a8[r, :] . w8^T) a_scale[r] w_scale + bias)                                           w2 NULL
+ *   out[r, :] = residual[r, :] + act((a8[r, :] . w8^T) a_scale[r] w_scale + bias) * ((a8[r, :] . w2^T) a_scale[r] w2_scale + bias2)
+ * a, w, w2: e4m3 [T_cap, K], [N, K], [N, K]; a_scale fp32 [T_cap], w_scale and w2_scale fp32 [N]; everything else as dcut_linear:
+ * products accumulated in fp32, scales, bias, activation, gate and residual in fp32, one rounding to bf16.
+ * lda and ldw are multiples of 16 elements (bytes), bases 16-byte aligned (scales 4-byte).
+ */
+typedef struct {
+    const void* a;
+    long long lda;
+    const float* a_scale;
+    const void* w;
+    const void* w2;
+    long long ldw;
+    const float* w_scale;
+    const float* w2_scale;
+    const void* bias;
+    const void* bias2;
+    const void* residual;
+    long long ldr;
+    void* out;
+    long long ldo;
+    int N, K;
+    int act;                   /* dcut_act */
+} dcut_linear8_args;
+dcut_status dcut_linear8(dcut_ctx* ctx, const dcut_linear8_args* args, const int* cu_q, int B, int T_cap, void* stream);
+
+/*
  * dcut_accept without any allocation.  (The paper has no counterpart: this entry point exists for
  * the way the library gets embedded, not for the method.)
  *
@@ -630,8 +658,8 @@ dcut_status dcut_verify_step_host(dcut_ctx* ctx, const dcut_host_step* step, voi
  * (rows at or past T_cap were left out: nothing outside the caller's T_cap rows is read or written), 8 =
  * dcut_rope_append met a token whose request, group or position has no place in the block table (it was left out), 9 =
  * dcut_prefix_attn met groups that do not cover the batch, a prefix or own positions that do not fit (nothing was written;
- * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear, dcut_rope_append or dcut_rms_norm met a
- * cu_q[B] above T_cap (rows from T_cap on were left out). */
+ * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear, dcut_linear8, dcut_rope_append or
+ * dcut_rms_norm met a cu_q[B] above T_cap (rows from T_cap on were left out). */
 dcut_status dcut_poll_device_status(dcut_ctx* ctx, int* code, void* stream);
 
 #ifdef __cplusplus

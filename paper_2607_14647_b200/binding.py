@@ -33,7 +33,7 @@ EXPORTS = ["dcut_create", "dcut_destroy", "dcut_last_error", "dcut_set_cost_dens
            "dcut_enable_plan_in_select", "dcut_cost_grid_create", "dcut_cost_grid_destroy", "dcut_cost_grid_budget",
            "dcut_cost_grid_record", "dcut_cost_grid_get", "dcut_cost_grid_nearest", "dcut_cost_grid_buckets",
            "dcut_set_cost_from_grid", "dcut_layer_attn_part", "dcut_layer_mlp_part", "dcut_residual_add",
-           "dcut_rope_append", "dcut_enable_prefix_attn", "dcut_prefix_attn", "dcut_linear", "dcut_rms_norm"]
+           "dcut_rope_append", "dcut_enable_prefix_attn", "dcut_prefix_attn", "dcut_linear", "dcut_rms_norm", "dcut_linear8"]
 
 
 class Limits(C.Structure):
@@ -132,6 +132,14 @@ ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 _lib.dcut_linear.argtypes = [_vp, C.POINTER(LinearArgs), _vp, _i, _i, _vp]
 _lib.dcut_enable_prefix_attn.argtypes = [_vp, _i]
 _lib.dcut_prefix_attn.argtypes = [_vp, _vp, _vp, _vp, _ll, _vp, _i, _vp, _vp, _i, _i, C.POINTER(PrefixGroupsRec), _f, _vp, _vp, _vp]
+
+
+class Linear8Args(C.Structure):
+    _fields_ = [("a", _vp), ("lda", _ll), ("a_scale", _vp), ("w", _vp), ("w2", _vp), ("ldw", _ll), ("w_scale", _vp), ("w2_scale", _vp), ("bias", _vp),
+                ("bias2", _vp), ("residual", _vp), ("ldr", _ll), ("out", _vp), ("ldo", _ll), ("N", _i), ("K", _i), ("act", _i)]
+
+
+_lib.dcut_linear8.argtypes = [_vp, C.POINTER(Linear8Args), _vp, _i, _i, _vp]
 
 
 class NormArgs(C.Structure):
@@ -623,6 +631,27 @@ class Context:
         l = LinearArgs(ap, lda, wp, w2p, ldw, _on(dev, bias, torch.bfloat16), _on(dev, bias2, torch.bfloat16), rp, ldr, op, ldo, N, K,
                        ACTIVATIONS[act])
         self._check(_lib.dcut_linear(self._h, C.byref(l), _on(dev, cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, self._stream()))
+        return out
+
+    def linear8(self, a, a_scale, w, w_scale, cu_q, T_cap: int, out=None, bias=None, act: str = "none", w2=None, w2_scale=None, bias2=None, residual=None):
+        """dcut_linear8: linear on e4m3 a [T_cap rows, K] and w [N, K] (rows a multiple of 16 elements apart: rows8, quantize) with
+        fp32 scales a_scale [T_cap] and w_scale [N]; bias, residual and out are bf16."""
+        (N, K), dev = w.shape, self.device
+        assert a.shape[1] == K and a.shape[0] >= T_cap, "a must be [T_cap rows, K]"
+        assert a_scale.numel() >= T_cap and w_scale.shape == (N,)
+        assert bias is None or bias.shape == (N,)
+        assert bias2 is None or bias2.shape == (N,)
+        assert residual is None or (residual.shape[0] >= T_cap and residual.shape[1] == N)
+        if out is None:
+            out = torch.empty((T_cap, N), dtype=torch.bfloat16, device=a.device)
+        assert out.shape[0] >= T_cap and out.shape[1] == N
+        (ap, lda), (wp, ldw), (w2p, ldw2) = (_rows(dev, t, torch.float8_e4m3fn, 16) for t in (a, w, w2))
+        (rp, ldr), (op, ldo) = _rows(dev, residual), _rows(dev, out)
+        assert w2 is None or (w2.shape == w.shape and ldw2 == ldw and w2_scale.shape == (N,)), "w2 must have the shape and strides of w"
+        f32, bf16 = torch.float32, torch.bfloat16
+        l = Linear8Args(ap, lda, _on(dev, a_scale, f32), wp, w2p, ldw, _on(dev, w_scale, f32), _on(dev, w2_scale, f32), _on(dev, bias, bf16),
+                        _on(dev, bias2, bf16), rp, ldr, op, ldo, N, K, ACTIVATIONS[act])
+        self._check(_lib.dcut_linear8(self._h, C.byref(l), _on(dev, cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, self._stream()))
         return out
 
     def rms_norm(self, x, cu_q, T_cap: int, gain=None, rms_eps: float = 1e-6, residual=None, h_out=None, out=None, out8=None, scale8=None,

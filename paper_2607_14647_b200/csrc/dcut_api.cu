@@ -99,6 +99,25 @@ void free_all(dcut_ctx* c) {
     if (c->hs_ev_join) cudaEventDestroy(c->hs_ev_join);
 }
 
+// What dcut_linear and dcut_linear8 ask of their arguments; `step`: elements of 16 bytes.
+template <typename ARGS>
+dcut_status check_linear(dcut_ctx* c, const ARGS* l, int step, const int* cu_q, int B, int T_cap) {
+    if (c->lim.n_q_heads <= 0) return dcut_fail(c, DCUT_EINVAL, "context was created without attention shapes (no tensor-map encoder)");
+    if (!l || !l->a || !l->w || !l->out || !cu_q || (l->bias2 && !l->w2)) return dcut_fail(c, DCUT_EINVAL, "null pointer argument (bias2 goes with w2)");
+    if (B < 1 || T_cap < 1 || l->N < 1 || l->K < 1) return dcut_fail(c, DCUT_EINVAL, "need B, T_cap, N, K >= 1");
+    if (l->N > (1 << 21) || l->K > (1 << 30) || T_cap > (1 << 21)) return dcut_fail(c, DCUT_ECAPACITY, "N and T_cap go up to 2^21, K to 2^30");
+    if (l->act < DCUT_ACT_NONE || l->act > DCUT_ACT_SILU) return dcut_fail(c, DCUT_EINVAL, "unknown activation %d", l->act);
+    if (l->lda < l->K || l->lda % step || l->ldw < l->K || l->ldw % step || l->lda > (1ll << 32) || l->ldw > (1ll << 32))
+        return dcut_fail(c, DCUT_EINVAL, "lda and ldw must be multiples of %d elements, >= K and <= 2^32", step);
+    if (l->ldo < l->N || (l->residual && l->ldr < l->N)) return dcut_fail(c, DCUT_EINVAL, "ldo and ldr must be >= N");
+    if ((reinterpret_cast<uintptr_t>(l->a) | reinterpret_cast<uintptr_t>(l->w) | reinterpret_cast<uintptr_t>(l->w2)) & 15)
+        return dcut_fail(c, DCUT_EINVAL, "a, w and w2 must be 16-byte aligned");
+    if ((reinterpret_cast<uintptr_t>(l->out) | reinterpret_cast<uintptr_t>(l->residual) | reinterpret_cast<uintptr_t>(l->bias) | reinterpret_cast<uintptr_t>(l->bias2)) & 1)
+        return dcut_fail(c, DCUT_EINVAL, "out, residual and biases must be 2-byte aligned");
+    if (l->residual == l->out && l->ldr != l->ldo) return dcut_fail(c, DCUT_EINVAL, "out over the residual needs the same stride");
+    return DCUT_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -624,21 +643,21 @@ dcut_status dcut_prefix_attn(dcut_ctx* c, const void* q, const void* k_cache, co
 
 dcut_status dcut_linear(dcut_ctx* c, const dcut_linear_args* l, const int* cu_q, int B, int T_cap, void* stream) {
     if (!c) return DCUT_EINVAL;
-    if (c->lim.n_q_heads <= 0) return dcut_fail(c, DCUT_EINVAL, "context was created without attention shapes (no tensor-map encoder)");
-    if (!l || !l->a || !l->w || !l->out || !cu_q || (l->bias2 && !l->w2)) return dcut_fail(c, DCUT_EINVAL, "null pointer argument (bias2 goes with w2)");
-    if (B < 1 || T_cap < 1 || l->N < 1 || l->K < 1) return dcut_fail(c, DCUT_EINVAL, "need B, T_cap, N, K >= 1");
-    if (l->N > (1 << 21) || l->K > (1 << 30) || T_cap > (1 << 21)) return dcut_fail(c, DCUT_ECAPACITY, "N and T_cap go up to 2^21, K to 2^30");
-    if (l->act < DCUT_ACT_NONE || l->act > DCUT_ACT_SILU) return dcut_fail(c, DCUT_EINVAL, "unknown activation %d", l->act);
-    if (l->lda < l->K || l->lda % 8 || l->ldw < l->K || l->ldw % 8 || l->lda > (1ll << 32) || l->ldw > (1ll << 32))
-        return dcut_fail(c, DCUT_EINVAL, "lda and ldw must be multiples of 8 elements, >= K and <= 2^32");
-    if (l->ldo < l->N || (l->residual && l->ldr < l->N)) return dcut_fail(c, DCUT_EINVAL, "ldo and ldr must be >= N");
-    if ((reinterpret_cast<uintptr_t>(l->a) | reinterpret_cast<uintptr_t>(l->w) | reinterpret_cast<uintptr_t>(l->w2)) & 15)
-        return dcut_fail(c, DCUT_EINVAL, "a, w and w2 must be 16-byte aligned");
-    if ((reinterpret_cast<uintptr_t>(l->out) | reinterpret_cast<uintptr_t>(l->residual) | reinterpret_cast<uintptr_t>(l->bias) | reinterpret_cast<uintptr_t>(l->bias2)) & 1)
-        return dcut_fail(c, DCUT_EINVAL, "out, residual and biases must be 2-byte aligned");
-    if (l->residual == l->out && l->ldr != l->ldo) return dcut_fail(c, DCUT_EINVAL, "out over the residual needs the same stride");
+    const dcut_status st = check_linear(c, l, 8, cu_q, B, T_cap);
+    if (st != DCUT_OK) return st;
     DCUT_ON_DEVICE(c);
     return dcut_launch_linear(c, l, cu_q, B, T_cap, static_cast<cudaStream_t>(stream));
+}
+
+dcut_status dcut_linear8(dcut_ctx* c, const dcut_linear8_args* l, const int* cu_q, int B, int T_cap, void* stream) {
+    if (!c) return DCUT_EINVAL;
+    const dcut_status st = check_linear(c, l, 16, cu_q, B, T_cap);
+    if (st != DCUT_OK) return st;
+    if (!l->a_scale || !l->w_scale || (l->w2 != nullptr) != (l->w2_scale != nullptr)) return dcut_fail(c, DCUT_EINVAL, "null scales (w2_scale goes with w2)");
+    if ((reinterpret_cast<uintptr_t>(l->a_scale) | reinterpret_cast<uintptr_t>(l->w_scale) | reinterpret_cast<uintptr_t>(l->w2_scale)) & 3)
+        return dcut_fail(c, DCUT_EINVAL, "scales must be 4-byte aligned");
+    DCUT_ON_DEVICE(c);
+    return dcut_launch_linear8(c, l, cu_q, B, T_cap, static_cast<cudaStream_t>(stream));
 }
 
 dcut_status dcut_rms_norm(dcut_ctx* c, const dcut_norm_args* n, const int* cu_q, int B, int T_cap, void* stream) {

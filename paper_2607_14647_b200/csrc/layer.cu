@@ -14,6 +14,8 @@
 //                         are staged by TMA as 128-byte-swizzled K-major tiles (BK = 64); one elected lane issues the
 //                         MMAs and releases stages with tcgen05.commit; two accumulators in tensor memory let the four
 //                         epilogue warps (tcgen05.ld) work on one tile while the next is being multiplied.
+//                         Operands are bf16 or (dcut_linear8) e4m3: a k-block is 128 bytes of a row either way, so tiles, stages,
+//                         swizzle and descriptors are the same and an MMA takes twice the elements.
 //                         Epilogues: plain bf16, + residual, SwiGLU (the B tile is 128 gate rows and the 128 matching
 //                         up rows, so silu(g) * u is formed in registers and the [T, 2I] intermediate never exists),
 //                         row argmax (the LM head fused with acceptance: the logits are never stored), or dcut_linear's:
@@ -48,13 +50,17 @@ constexpr int kGemmThreads = 192;              // warp 0: TMA, warp 1: MMA + TME
 constexpr int kTmemCols = 512;              // two 128 x 256 fp32 accumulators
 constexpr int kMaxStages = 12;                 // a narrow tile's stage is smaller: more of them fit the same operand area
 constexpr int kGemmSmem = kGemmStages * kGemmStageBytes + 1024 /* align */ + 512 /* two sets of barriers, tmem ptr */;
-constexpr int kLinearSmem = kGemmSmem + 4 * (32 * 33 + 32 + BN) * 4;   // + LinearShared of four epilogue warps
+constexpr int kLinearSmem = kGemmSmem + 4 * (32 * 33 + 32 + 2 * BN) * 4;   // + LinearShared of four epilogue warps
 constexpr int kWaitLimit = 1 << 22;
 
-enum GemmMode { kPlain = 0, kResidual = 1, kSwiGLU = 2, kArgmax = 3, kLinear = 4, kLinearGated = 5 };
-__host__ __device__ constexpr bool is_gated(int mode) { return mode == kSwiGLU || mode == kLinearGated; }        // two weights share a tile
-__host__ __device__ constexpr bool is_linear(int mode) { return mode == kLinear || mode == kLinearGated; }
-__host__ __device__ constexpr bool may_split_k(int mode) { return mode == kPlain || mode == kResidual || mode == kLinear; }
+enum GemmMode { kPlain = 0, kResidual = 1, kSwiGLU = 2, kArgmax = 3, kLinear = 4, kLinearGated = 5, kLinear8 = 6, kLinear8Gated = 7 };
+__host__ __device__ constexpr bool is_fp8(int mode) { return mode == kLinear8 || mode == kLinear8Gated; }        // e4m3 operands with scales
+__host__ __device__ constexpr bool is_gated(int mode) { return mode == kSwiGLU || mode == kLinearGated || mode == kLinear8Gated; }   // two weights share a tile
+__host__ __device__ constexpr bool is_linear(int mode) { return mode == kLinear || mode == kLinearGated || is_fp8(mode); }
+__host__ __device__ constexpr bool may_split_k(int mode) { return mode == kPlain || mode == kResidual || mode == kLinear || mode == kLinear8; }
+__host__ __device__ constexpr bool is_split_linear(int mode) { return is_linear(mode) && may_split_k(mode); }
+// A k-block is 128 bytes of a row of either operand: 64 bf16 or 128 e4m3 elements.
+__host__ __device__ constexpr int kb_elements(int mode) { return is_fp8(mode) ? 2 * BK : BK; }
 
 struct BMaps {
     CUtensorMap m[kNumBn];
@@ -108,12 +114,19 @@ __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// D[tmem] (+)= A[smem desc] . B[smem desc]^T, M128 N256 K16, bf16 in, fp32 accumulate
+// D[tmem] (+)= A[smem desc] . B[smem desc]^T, M128 N256, 32 bytes along K: K16 of bf16 or K32 of e4m3, fp32 accumulate
+template <bool FP8>
 __device__ __forceinline__ void tc_mma(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-        ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
+    if (FP8)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
 }
 __device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&r)[32]) {
     asm volatile(
@@ -138,8 +151,12 @@ __device__ __forceinline__ uint64_t umma_desc_sw128(uint32_t smem_addr) {
     d |= (uint64_t)2 << 61;                               // SWIZZLE_128B
     return d;
 }
-// Instruction descriptor: fp32 accumulator, bf16 A and B, both K-major, N = 256, M = 128.
-constexpr uint32_t kIdescNoN = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24);   // N >> 3 goes to bits 17..22
+// Instruction descriptor: fp32 accumulator, both operands K-major and bf16 (1 in bits 7.. and 10.. of kind::f16) or e4m3 (0 there
+// in kind::f8f6f4), M; N >> 3 goes to bits 17..22.
+template <bool FP8>
+__device__ __forceinline__ constexpr uint32_t idesc_no_n(int m) {
+    return (1u << 4) | (FP8 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(m >> 4) << 24);
+}
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -160,6 +177,7 @@ struct GemmArgs {
     unsigned long long* row_key;     // kArgmax: one packed (ordered maximum, ~column) word per row
     int V;                           // kArgmax: live columns (rows of the weight)
     const __nv_bfloat16 *bias, *bias2;   // kLinear*: [N_out] or null
+    const float *a_scale, *w_scale, *w2_scale;   // kLinear8*: [T], [N_out], [N_out]
     long long ldo, ldr;              // kLinear*: elements from one row of out / residual to the next
     int T_cap;                       // kLinear*: rows that out has
     int act;                         // kLinear*: dcut_act
@@ -213,19 +231,23 @@ struct LinearShared {
     float stage[32 * kStageRow];
     float pad[32];                       // (16-byte alignment of what follows, whatever the row)
     float bias[BN];                      // gated: bias, then bias2, half each
+    float scale[BN];                     // e4m3 operands: the columns' scales, in the same places
 };
 static_assert(sizeof(LinearShared) % 16 == 0 && offsetof(LinearShared, bias) % 16 == 0, "read in vectors");
 static_assert(kLinearSmem - kGemmSmem == 4 * sizeof(LinearShared), "one per epilogue warp");
 
-// Before the accumulator is complete: the biases of a tile's columns, zeros where there are none.
-template <bool GATED>
+// Before the accumulator is complete: the biases (and scales) of a tile's columns, zeros where there are none.
+template <int MODE>
 __device__ __forceinline__ void linear_stage_bias(const GemmArgs& g, int n_tile, int bn, LinearShared& sh) {
+    constexpr bool GATED = is_gated(MODE);
     const int lane = threadIdx.x & 31, width = GATED ? bn >> 1 : bn, col0 = n_tile * width;
     __syncwarp();                                                      // (the previous tile's have been read)
     for (int c = lane; c < width; c += 32) {
         const bool there = col0 + c < g.N_out;
         sh.bias[c] = there && g.bias ? __bfloat162float(g.bias[col0 + c]) : 0.0f;
         if (GATED) sh.bias[BN / 2 + c] = there && g.bias2 ? __bfloat162float(g.bias2[col0 + c]) : 0.0f;
+        if (is_fp8(MODE)) sh.scale[c] = there ? g.w_scale[col0 + c] : 0.0f;
+        if (is_fp8(MODE) && GATED) sh.scale[BN / 2 + c] = there ? g.w2_scale[col0 + c] : 0.0f;
     }
     __syncwarp();
 }
@@ -256,9 +278,11 @@ __device__ __forceinline__ void linear_fetch(const GemmArgs& g, int T, int row0,
 // accesses are read and written by the thread that owns the row.  Others (an odd N, say) would be 2-byte accesses to 32
 // rows at a time, 32 lines each: they go through shared memory, so that a warp reads and writes 32 columns of one row at a
 // time (333 x 2051 with a residual, K = 1003: 21.1 us without that, 12.3 with it).
-template <bool GATED>
+// a_scale: the row's (e4m3 operands; the column's scale is applied first).
+template <int MODE>
 __device__ __forceinline__ void linear_finish32(const GemmArgs& g, int T, int row0, int col, int c, LinearShared& sh, const LinearAhead& f,
-                                                const float (&x)[32], const float (&u)[32]) {
+                                                float a_scale, const float (&x)[32], const float (&u)[32]) {
+    constexpr bool GATED = is_gated(MODE), FP8 = is_fp8(MODE);
     const int lane = threadIdx.x & 31, row = row0 + lane;
     const bool by_vector = linear_by_vector(g, col);
 #pragma unroll
@@ -268,11 +292,23 @@ __device__ __forceinline__ void linear_finish32(const GemmArgs& g, int T, int ro
         for (int h = 0; h < 2; ++h) {
             const int e = 8 * v + 4 * h;
             const float4 b = *reinterpret_cast<const float4*>(sh.bias + c + e);
-            y[h] = make_float4(x[e] + b.x, x[e + 1] + b.y, x[e + 2] + b.z, x[e + 3] + b.w);
+            if (FP8) {
+                const float4 w = *reinterpret_cast<const float4*>(sh.scale + c + e);
+                y[h] = make_float4(fmaf(x[e] * w.x, a_scale, b.x), fmaf(x[e + 1] * w.y, a_scale, b.y), fmaf(x[e + 2] * w.z, a_scale, b.z),
+                                   fmaf(x[e + 3] * w.w, a_scale, b.w));
+            } else {
+                y[h] = make_float4(x[e] + b.x, x[e + 1] + b.y, x[e + 2] + b.z, x[e + 3] + b.w);
+            }
             if (g.act != DCUT_ACT_NONE) y[h] = activate4(g.act, y[h]);
             if (GATED) {
                 const float4 b2 = *reinterpret_cast<const float4*>(sh.bias + BN / 2 + c + e);
-                y[h].x *= u[e] + b2.x, y[h].y *= u[e + 1] + b2.y, y[h].z *= u[e + 2] + b2.z, y[h].w *= u[e + 3] + b2.w;
+                if (FP8) {
+                    const float4 w = *reinterpret_cast<const float4*>(sh.scale + BN / 2 + c + e);
+                    y[h].x *= fmaf(u[e] * w.x, a_scale, b2.x), y[h].y *= fmaf(u[e + 1] * w.y, a_scale, b2.y);
+                    y[h].z *= fmaf(u[e + 2] * w.z, a_scale, b2.z), y[h].w *= fmaf(u[e + 3] * w.w, a_scale, b2.w);
+                } else {
+                    y[h].x *= u[e] + b2.x, y[h].y *= u[e + 1] + b2.y, y[h].z *= u[e + 2] + b2.z, y[h].w *= u[e + 3] + b2.w;
+                }
             }
         }
         if (!by_vector) {
@@ -304,23 +340,25 @@ __device__ __forceinline__ void linear_finish32(const GemmArgs& g, int T, int ro
 template <int MODE>
 __device__ __forceinline__ void gemm_epilogue(const GemmArgs& g, int T, int row, int n_tile, uint32_t t_row, int bn, LinearShared& sh) {
     if (is_linear(MODE)) {
-        const int width = MODE == kLinearGated ? bn >> 1 : bn, col0 = n_tile * width, row0 = row - (threadIdx.x & 31);
+        constexpr bool GATED = is_gated(MODE);
+        const int width = GATED ? bn >> 1 : bn, col0 = n_tile * width, row0 = row - (threadIdx.x & 31);
         if (row0 >= T) return;                                          // (the whole warp: none of its rows exists)
+        const float a_scale = is_fp8(MODE) && row < T ? g.a_scale[row] : 0.0f;
         LinearAhead ahead;
         linear_fetch(g, T, row0, col0, ahead);
 #pragma unroll 1
         for (int c = 0; c < width && col0 + c < g.N_out; c += 32) {
             uint32_t av[32], uv[32];
             tc_ld32(t_row + c, av);
-            if (MODE == kLinearGated) tc_ld32(t_row + width + c, uv);
+            if (GATED) tc_ld32(t_row + width + c, uv);
             tc_wait_ld();
             float x[32], u[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
                 x[j] = __uint_as_float(av[j]);
-                u[j] = MODE == kLinearGated ? __uint_as_float(uv[j]) : 0.0f;
+                u[j] = GATED ? __uint_as_float(uv[j]) : 0.0f;
             }
-            linear_finish32<MODE == kLinearGated>(g, T, row0, col0 + c, c, sh, ahead, x, u);
+            linear_finish32<MODE>(g, T, row0, col0 + c, c, sh, ahead, a_scale, x, u);
             if (c + 32 < width) linear_fetch(g, T, row0, col0 + c + 32, ahead);
         }
     } else if (MODE == kSwiGLU) {
@@ -422,7 +460,6 @@ __device__ __forceinline__ void gemm_epilogue(const GemmArgs& g, int T, int row,
 
 constexpr int kG2Stages = 6;
 constexpr int kG2StageBytes = kATile + kBTile / 2;     // 32 KB
-constexpr uint32_t kIdesc2NoN = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)((2 * BM) >> 4) << 24);
 
 __device__ __forceinline__ uint32_t cluster_ctarank() {
     uint32_t r;
@@ -448,11 +485,18 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar_cluster_addr) : "memory");
 }
+template <bool FP8>
 __device__ __forceinline__ void tc_mma2(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n\t}"
-        ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
+    if (FP8)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n\t}"
+            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n\t}"
+            ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
 }
 // arrives on the barrier at the same offset in both CTAs of the pair once the MMAs issued so far have completed
 __device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
@@ -483,7 +527,8 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars2 + 2 * kG2Stages + 4);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     LinearShared& sh = reinterpret_cast<LinearShared*>(smem + kGemmSmem - 1024)[warp & 3];   // (linear modes only) behind the barriers
-    const int n_kb = g.K / BK;
+    constexpr int kKb = kb_elements(MODE);
+    const int n_kb = g.K / kKb;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kMaxStages; ++s) {
@@ -582,9 +627,9 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                     const uint32_t a_dst = smem_u32(smem + s * stage_stride), b_dst = a_dst + a_bytes;
                     const uint32_t bar = full_bar + 8 * s;
                     mbar_arrive_expect_tx(bar, stage_tx);
-                    tma_load_2d(a_dst, a_map1, kb * BK, m0, bar);
-                    tma_load_2d(b_dst, b_map, kb * BK, n_tile * bn, bar);
-                    tma_load_2d(b_dst + half_rows * BK * 2, b_map, kb * BK, n_tile * bn + half_rows, bar);
+                    tma_load_2d(a_dst, a_map1, kb * kKb, m0, bar);
+                    tma_load_2d(b_dst, b_map, kb * kKb, n_tile * bn, bar);
+                    tma_load_2d(b_dst + half_rows * BK * 2, b_map, kb * kKb, n_tile * bn + half_rows, bar);
                 }
                 __syncwarp();
                 if (++s == n_stages) {
@@ -593,7 +638,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                 }
             }
         } else if (has_tile && warp == 1) {
-            const uint32_t idesc = kIdescNoN | ((uint32_t)(bn >> 3) << 17);
+            const uint32_t idesc = idesc_no_n<is_fp8(MODE)>(BM) | ((uint32_t)(bn >> 3) << 17);
             for (int kb = kb0, kc = 0, s = 0, use = 0; kb < kb1; ++kb, ++kc) {
                 if (!__all_sync(0xffffffffu, mbar_wait(full_bar + 8 * s, use & 1))) {
                     failed = true;
@@ -604,7 +649,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                     const uint32_t a_addr = smem_u32(smem + s * stage_stride);
                     const uint64_t da = umma_desc_sw128(a_addr), db = umma_desc_sw128(a_addr + a_bytes);
 #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k) tc_mma(tmem_base, da + 2 * k, db + 2 * k, idesc, (kc | k) ? 1u : 0u);
+                    for (int k = 0; k < BK / 16; ++k) tc_mma<is_fp8(MODE)>(tmem_base, da + 2 * k, db + 2 * k, idesc, (kc | k) ? 1u : 0u);
                     tc_commit(empty_bar + 8 * s);
                 }
                 __syncwarp();
@@ -616,7 +661,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
             if (!failed && elect_one()) tc_commit(acc_full);    // this CTA's partial sums are complete
             __syncwarp();
         } else if (has_tile) {
-            if (MODE == kLinear) linear_stage_bias<false>(g, n_tile, bn, sh);
+            if (is_split_linear(MODE)) linear_stage_bias<MODE>(g, n_tile, bn, sh);
             if (!__all_sync(0xffffffffu, mbar_wait(acc_full, 0))) failed = true;   // ... and its operand ring is idle
             tc_fence_after();
         }
@@ -626,10 +671,11 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
         const int quarter = warp & 3, row_in_tile = quarter * 32 + lane;
         const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16);
         const uint32_t stage_local = smem_u32(smem);              // [column / 4][row] vectors of four fp32: 64 KB at most
-        LinearAhead ahead;                                        // (kLinear only)
+        LinearAhead ahead;                                        // (linear modes only)
         const int row0 = m0 + quarter * 32;
         const bool rows_here = row0 < T;                          // (a warp without rows has nothing to exchange)
-        if (MODE == kLinear && has_tile && warp >= 2 && rows_here) linear_fetch(g, T, row0, n_tile * bn + own0, ahead);
+        const float a_scale = is_fp8(MODE) && has_tile && warp >= 2 && row0 + lane < T ? g.a_scale[row0 + lane] : 0.0f;
+        if (is_split_linear(MODE) && has_tile && warp >= 2 && rows_here) linear_fetch(g, T, row0, n_tile * bn + own0, ahead);
         tc_fence_before();
         cluster_sync_all();                                       // both accumulators complete, both rings idle
         tc_fence_after();
@@ -658,10 +704,10 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
             const __nv_bfloat16* rrow = MODE == kResidual ? g.residual + (size_t)row * g.N_out + col0 : nullptr;
 #pragma unroll 1
             for (int c = own0; c < own1; c += 32) {
-                if (MODE == kLinear && col0 + c >= g.N_out) break;
+                if (is_split_linear(MODE) && col0 + c >= g.N_out) break;
                 uint32_t av[32];
                 tc_ld32(t_row + c, av);
-                if (MODE == kLinear) {
+                if (is_split_linear(MODE)) {
                     tc_wait_ld();
                     float x[32];
 #pragma unroll
@@ -673,7 +719,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                         for (int j = 0; j < 4; ++j)   // (rank 0's half of K) + (rank 1's)
                             x[4 * v + j] = rank ? add[j] + __uint_as_float(av[4 * v + j]) : __uint_as_float(av[4 * v + j]) + add[j];
                     }
-                    linear_finish32<false>(g, T, row0, col0 + c, c, sh, ahead, x, x);
+                    linear_finish32<MODE>(g, T, row0, col0 + c, c, sh, ahead, a_scale, x, x);
                     if (c + 32 < own1) linear_fetch(g, T, row0, col0 + c + 32, ahead);
                     continue;
                 }
@@ -724,13 +770,13 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                         const uint32_t a_dst = smem_u32(smem + s * stage_stride), b_dst = a_dst + a_bytes;
                         const uint32_t bar = full_bar + 8 * s;
                         mbar_arrive_expect_tx(bar, stage_tx);
-                        tma_load_2d(a_dst, a_map1, kb * BK, m0, bar);
+                        tma_load_2d(a_dst, a_map1, kb * kKb, m0, bar);
                         if (is_gated(MODE)) {    // the gate rows, then the up rows of the same features
-                            tma_load_2d(b_dst, b_map, kb * BK, n_tile * half_rows, bar);
-                            tma_load_2d(b_dst + half_rows * BK * 2, b2_map, kb * BK, n_tile * half_rows, bar);
+                            tma_load_2d(b_dst, b_map, kb * kKb, n_tile * half_rows, bar);
+                            tma_load_2d(b_dst + half_rows * BK * 2, b2_map, kb * kKb, n_tile * half_rows, bar);
                         } else {                 // (weight rows past N read as zeros)
-                            tma_load_2d(b_dst, b_map, kb * BK, n_tile * bn, bar);
-                            tma_load_2d(b_dst + half_rows * BK * 2, b_map, kb * BK, n_tile * bn + half_rows, bar);
+                            tma_load_2d(b_dst, b_map, kb * kKb, n_tile * bn, bar);
+                            tma_load_2d(b_dst + half_rows * BK * 2, b_map, kb * kKb, n_tile * bn + half_rows, bar);
                         }
                     }
                     __syncwarp();
@@ -742,7 +788,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
             }
         } else if (warp == 1) {
             // ---------------------------------------------------------------- MMA issuer (whole warp walks, one lane issues)
-            const uint32_t idesc = kIdescNoN | ((uint32_t)(bn >> 3) << 17);
+            const uint32_t idesc = idesc_no_n<is_fp8(MODE)>(BM) | ((uint32_t)(bn >> 3) << 17);
             int s = 0, use = 0, it = 0;
             for (int w = blockIdx.x; w < n_work && !failed; w += gridDim.x, ++it) {
                 const int acc = it & 1;
@@ -764,7 +810,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                         const uint64_t da = umma_desc_sw128(a_addr), db = umma_desc_sw128(a_addr + a_bytes);
     #pragma unroll
                         for (int k = 0; k < BK / 16; ++k)   // 32 bytes along K per step = 2 descriptor address units
-                            tc_mma(tmem_d, da + 2 * k, db + 2 * k, idesc, (kb | k) ? 1u : 0u);
+                            tc_mma<is_fp8(MODE)>(tmem_d, da + 2 * k, db + 2 * k, idesc, (kb | k) ? 1u : 0u);
                         tc_commit(empty_bar + 8 * s);       // the stage is free once these MMAs have read it
                     }
                     __syncwarp();
@@ -785,7 +831,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                 const int n_tile = w / m_tiles, m0 = (w - n_tile * m_tiles) * BM;
                 const int acc = it & 1;
                 const int row = m0 + quarter * 32 + lane;
-                if (is_linear(MODE)) linear_stage_bias<MODE == kLinearGated>(g, n_tile, bn, sh);
+                if (is_linear(MODE)) linear_stage_bias<MODE>(g, n_tile, bn, sh);
                 if (!__all_sync(0xffffffffu, mbar_wait(acc_full + 8 * acc, (it >> 1) & 1))) {
                     failed = true;
                     break;
@@ -824,11 +870,11 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                         const uint32_t a_dst = smem_u32(smem + s * kG2StageBytes), b_dst = a_dst + kATile;
                         if (rank == 0) mbar_arrive_expect_tx(full_bar + 8 * s, pair_tx);
                         const uint32_t bar = lead_full + 8 * s;
-                        tma_load_2d_pair(a_dst, &a_maps.full, kb * BK, m0, bar);
+                        tma_load_2d_pair(a_dst, &a_maps.full, kb * kKb, m0, bar);
                         if (is_gated(MODE))       // the leader's half: 128 gate rows; the peer's: the 128 up rows of the same features
-                            tma_load_2d_pair(b_dst, rank == 0 ? b_map : b2_map, kb * BK, n_tile * half_rows, bar);
+                            tma_load_2d_pair(b_dst, rank == 0 ? b_map : b2_map, kb * kKb, n_tile * half_rows, bar);
                         else
-                            tma_load_2d_pair(b_dst, b_map, kb * BK, n_tile * bn + (int)rank * half_rows, bar);
+                            tma_load_2d_pair(b_dst, b_map, kb * kKb, n_tile * bn + (int)rank * half_rows, bar);
                     }
                     __syncwarp();
                 }
@@ -836,7 +882,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
         } else if (warp == 1) {
             // ---------------------------------------------------------------- MMA issuer (leader CTA only)
             if (rank == 0) {
-                const uint32_t idesc2 = kIdesc2NoN | ((uint32_t)(bn >> 3) << 17);
+                const uint32_t idesc2 = idesc_no_n<is_fp8(MODE)>(2 * BM) | ((uint32_t)(bn >> 3) << 17);
                 int kc = 0, it = 0;
                 for (int w = pair; w < n_work && !failed; w += n_pairs, ++it) {
                     const int acc = it & 1;
@@ -859,7 +905,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                             const uint64_t da = umma_desc_sw128(a_addr), db = umma_desc_sw128(a_addr + kATile);
     #pragma unroll
                             for (int k = 0; k < BK / 16; ++k)
-                                tc_mma2(tmem_d, da + 2 * k, db + 2 * k, idesc2, (kb | k) ? 1u : 0u);
+                                tc_mma2<is_fp8(MODE)>(tmem_d, da + 2 * k, db + 2 * k, idesc2, (kb | k) ? 1u : 0u);
                             tc_commit_pair(empty_bar + 8 * s);     // the stage is free in both CTAs once these MMAs have read it
                         }
                         __syncwarp();
@@ -878,7 +924,7 @@ gemm_tcgen05_kernel(const __grid_constant__ AMaps a_maps, const __grid_constant_
                 const int n_tile = w / m_tiles, m0 = (w - n_tile * m_tiles) * (2 * BM) + (int)rank * BM;
                 const int acc = it & 1;
                 const int row = m0 + quarter * 32 + lane;
-                if (is_linear(MODE)) linear_stage_bias<MODE == kLinearGated>(g, n_tile, bn, sh);
+                if (is_linear(MODE)) linear_stage_bias<MODE>(g, n_tile, bn, sh);
                 if (!__all_sync(0xffffffffu, mbar_wait(acc_full + 8 * acc, (it >> 1) & 1))) {
                     failed = true;
                     break;
@@ -1012,24 +1058,24 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// K-major bf16 matrix [rows, cols] as a 2-D tensor map with a {64 columns, box_rows} box and 128-byte swizzle
-dcut_status make_kmajor_map(dcut_ctx* ctx, CUtensorMap* map, const void* base, long long rows, long long cols, int box_rows, long long ld = 0) {
+// K-major bf16 (or e4m3: bytes) matrix [rows, cols] as a 2-D tensor map with a {128 bytes, box_rows} box and 128-byte swizzle
+dcut_status make_kmajor_map(dcut_ctx* ctx, CUtensorMap* map, const void* base, long long rows, long long cols, int box_rows, long long ld = 0, bool fp8 = false) {
     cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)(ld ? ld : cols) * 2};
-    cuuint32_t box[2] = {BK, (cuuint32_t)box_rows};
+    cuuint64_t strides[1] = {(cuuint64_t)(ld ? ld : cols) * (fp8 ? 1 : 2)};
+    cuuint32_t box[2] = {(cuuint32_t)(fp8 ? 2 * BK : BK), (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1, 1};
     CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(
-        map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+        map, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return dcut_fail(ctx, DCUT_ECUDA, "cuTensorMapEncodeTiled failed for a GEMM operand (%d)", (int)r);
     return DCUT_OK;
 }
 
-dcut_status make_act_maps(dcut_ctx* ctx, AMaps* maps, const void* base, long long rows, long long cols, long long ld = 0) {
-    dcut_status st = make_kmajor_map(ctx, &maps->full, base, rows, cols, BM, ld);
+dcut_status make_act_maps(dcut_ctx* ctx, AMaps* maps, const void* base, long long rows, long long cols, long long ld = 0, bool fp8 = false) {
+    dcut_status st = make_kmajor_map(ctx, &maps->full, base, rows, cols, BM, ld, fp8);
     if (st != DCUT_OK) return st;
-    return make_kmajor_map(ctx, &maps->half, base, rows, cols, BM / 2, ld);
+    return make_kmajor_map(ctx, &maps->half, base, rows, cols, BM / 2, ld, fp8);
 }
 
 // The weight's tensor maps for the tile widths in `mask` (box = half the width in rows)
@@ -1045,7 +1091,7 @@ dcut_status make_weight_maps(dcut_ctx* ctx, BMaps* maps, const void* w, long lon
 // Fills in how a launch runs (gemm_plan.cuh); returns its grid
 template <int MODE>
 int plan_gemm(dcut_ctx* ctx, int T_cap, unsigned bn_mask, GemmArgs& ga) {
-    const Shape shape = {ga.N_out, ga.K, T_cap, is_gated(MODE), may_split_k(MODE), is_linear(MODE)};
+    const Shape shape = {ga.N_out, ga.K / kb_elements(MODE) * BK, T_cap, is_gated(MODE), may_split_k(MODE), is_linear(MODE)};   // (K in k-blocks)
     const Launch l = plan(shape, Device{ctx->sm_count, ctx->ly_gemm_pairs, ctx->ly_gemm_pair_mode != 0, ctx->ly_gemm_force, bn_mask});
     static_assert(sizeof(ga.plan_by_m) == sizeof(l.by_m), "one table");
     memcpy(ga.plan_by_m, l.by_m, sizeof(l.by_m));
@@ -1084,9 +1130,10 @@ dcut_status launch_gemm(dcut_ctx* ctx, const AMaps& a, const BMaps& b, const BMa
 }
 
 // dcut_linear: any N and K (the tensor maps' zero fill completes the last tile and the last k-block), rows of any stride.
-// Encodes maps for the tile widths that the plan can pick only (about 0.3 us of host time each).
-template <int MODE>
-dcut_status launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, int T_cap, GemmArgs& g, cudaStream_t stream) {
+// Encodes maps for the tile widths that the plan can pick only (about 0.3 us of host time each).  ARGS: dcut_linear_args or
+// dcut_linear8_args.
+template <int MODE, typename ARGS>
+dcut_status launch_linear(dcut_ctx* ctx, const ARGS* l, int T_cap, GemmArgs& g, cudaStream_t stream) {
     const unsigned mask = (is_gated(MODE) ? ctx->ly_gemm_bn_mask & kBnMaskSwiGLU : ctx->ly_gemm_bn_mask) | 1u;
     const int grid = plan_gemm<MODE>(ctx, T_cap, mask, g);
     unsigned used = 0;
@@ -1094,11 +1141,11 @@ dcut_status launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, int T_cap, G
     AMaps am;
     BMaps bm = {}, b2m = {};
     dcut_status st;
-    if ((st = make_act_maps(ctx, &am, l->a, T_cap, l->K, l->lda)) != DCUT_OK) return st;
+    if ((st = make_act_maps(ctx, &am, l->a, T_cap, l->K, l->lda, is_fp8(MODE))) != DCUT_OK) return st;
     for (int i = 0; i < kNumBn; ++i) {
         if (!((used >> i) & 1)) continue;
-        if ((st = make_kmajor_map(ctx, &bm.m[i], l->w, l->N, l->K, bn_of(i) / 2, l->ldw)) != DCUT_OK) return st;
-        if (is_gated(MODE) && (st = make_kmajor_map(ctx, &b2m.m[i], l->w2, l->N, l->K, bn_of(i) / 2, l->ldw)) != DCUT_OK) return st;
+        if ((st = make_kmajor_map(ctx, &bm.m[i], l->w, l->N, l->K, bn_of(i) / 2, l->ldw, is_fp8(MODE))) != DCUT_OK) return st;
+        if (is_gated(MODE) && (st = make_kmajor_map(ctx, &b2m.m[i], l->w2, l->N, l->K, bn_of(i) / 2, l->ldw, is_fp8(MODE))) != DCUT_OK) return st;
     }
     return launch_planned_gemm<MODE>(ctx, am, bm, b2m, grid, g, stream);
 }
@@ -1125,6 +1172,8 @@ dcut_status dcut_init_layer(dcut_ctx* ctx) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kArgmax>, cudaFuncAttributeMaxDynamicSharedMemorySize, kGemmSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kLinear>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kLinearGated>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kLinear8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(gemm_tcgen05_kernel<kLinear8Gated>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinearSmem);
     if (e != cudaSuccess) return dcut_check_cuda(ctx, e, "cudaFuncSetAttribute(gemm)");
     {
         // The GEMM is launched as clusters of two CTAs so that it can run tiles on pairs of SMs where that pays
@@ -1262,12 +1311,15 @@ dcut_status dcut_launch_gemm(dcut_ctx* ctx, const void* a, const void* w, const 
     return launch_gemm<kPlain>(ctx, am, bm, b2m, T_cap, mask, g, stream);
 }
 
-dcut_status dcut_launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, const int* cu_q, int B, int T_cap, cudaStream_t stream) {
+namespace {
+// What dcut_linear and dcut_linear8 share; whole k-blocks: the tail reads as zeros in both operands.
+template <typename ARGS>
+GemmArgs linear_args(dcut_ctx* ctx, const ARGS* l, int k_block, const int* cu_q, int B, int T_cap) {
     GemmArgs g = {};
     g.cu_q = cu_q;
     g.B = B;
     g.N_out = l->N;
-    g.K = (l->K + BK - 1) / BK * BK;      // whole k-blocks: the tail reads as zeros in both operands
+    g.K = (l->K + k_block - 1) / k_block * k_block;
     g.out = static_cast<__nv_bfloat16*>(l->out);
     g.residual = static_cast<const __nv_bfloat16*>(l->residual);
     g.bias = static_cast<const __nv_bfloat16*>(l->bias);
@@ -1279,7 +1331,21 @@ dcut_status dcut_launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, const i
     auto vec = [](const void* p, long long ld) { return !(reinterpret_cast<uintptr_t>(p) & 15) && ld % 8 == 0; };
     g.vec = vec(l->out, l->ldo) && (!l->residual || vec(l->residual, l->ldr));
     g.status = ctx->d_status;
+    return g;
+}
+}  // namespace
+
+dcut_status dcut_launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, const int* cu_q, int B, int T_cap, cudaStream_t stream) {
+    GemmArgs g = linear_args(ctx, l, kb_elements(kLinear), cu_q, B, T_cap);
     return l->w2 ? launch_linear<kLinearGated>(ctx, l, T_cap, g, stream) : launch_linear<kLinear>(ctx, l, T_cap, g, stream);
+}
+
+dcut_status dcut_launch_linear8(dcut_ctx* ctx, const dcut_linear8_args* l, const int* cu_q, int B, int T_cap, cudaStream_t stream) {
+    GemmArgs g = linear_args(ctx, l, kb_elements(kLinear8), cu_q, B, T_cap);
+    g.a_scale = l->a_scale;
+    g.w_scale = l->w_scale;
+    g.w2_scale = l->w2_scale;
+    return l->w2 ? launch_linear<kLinear8Gated>(ctx, l, T_cap, g, stream) : launch_linear<kLinear8>(ctx, l, T_cap, g, stream);
 }
 
 dcut_status dcut_launch_layer(dcut_ctx* ctx, const dcut_layer_weights* w, const void* x, void* y, void* k_cache,
