@@ -569,6 +569,47 @@ typedef struct {
 dcut_status dcut_linear8(dcut_ctx* ctx, const dcut_linear8_args* args, const int* cu_q, int B, int T_cap, void* stream);
 
 /*
+ * Low-rank adapters of many requests beside a shared projection.  base [T, N] is what the projection gave (dcut_linear,
+ * dcut_linear8, without an activation); for the rows of request i with the adapter t = adapter[i] >= 0
+ *   d[r, n] = scale[t] sum_j (x[r, :] . a[t][s(n) rank + j, :]) b[t][n, j],   j = 0 .. rank - 1
+ * and d = 0 where adapter[i] < 0.  The columns fall into n_slices slices, slice s = columns slice_end[s-1] .. slice_end[s]-1 (the last
+ * one ends at N), with rows of `a` of their own: q|k|v or gate|up of one projection; s(n) is the slice of column n.
+ *   out = act(base + d)                                                                    [T, N]
+ *   out[:, j] = act((base + d)[:, j]) * (base + d)[:, N/2 + j],   gated != 0               [T, N/2] (N even; one slice, or two halves)
+ * fp32 sums; s = x . a^T is scaled and then rounded to bf16 for the second product; one rounding of out.  Needs no scratch and
+ * no context shapes; requests of any length, T_cap is not bound by dcut_limits.
+ * DEVICE in: x bf16 [T_cap, K] with ldx elements from row to row; a bf16 [n_adapters, n_slices * rank, K] with lda elements from row to row
+ *   (adapters follow one another: n_slices * rank * lda); b bf16 [n_adapters, N, rank] dense; scale fp32 [n_adapters] or NULL (1);
+ *   adapter int32 [B]; base bf16 [T_cap, N] with ldbase; cu_q int32 [B+1].  x, a, b 16-byte aligned, ldx and lda multiples of 8; base and out of any
+ *   stride and alignment (rows and slices that start on 16 bytes are moved in vectors).
+ * DEVICE out: out bf16 with ldo.  It may be base (same stride, not gated): rows without an adapter then stay as they are; nothing else
+ *   may overlap.  Rows that no request owns are not touched.
+ * rank a multiple of 8 (smaller ones: pad with zeros), n_slices * rank <= DCUT_LORA_MAX_RANKS.  An adapter >= n_adapters sets device status 11
+ * and counts as none; a cu_q[B] above T_cap sets status 10.  The struct is HOST memory, read during the call.
+ */
+#define DCUT_LORA_MAX_SLICES 4
+#define DCUT_LORA_MAX_RANKS 256
+typedef struct {
+    const void* x;
+    long long ldx;
+    const void* a;
+    long long lda;
+    const void* b;
+    const float* scale;
+    const int* adapter;
+    int n_adapters, rank, n_slices;
+    int slice_end[DCUT_LORA_MAX_SLICES];
+    int K;
+    int act;                   /* dcut_act */
+    int gated;
+    const void* base;
+    long long ldbase;
+    void* out;
+    long long ldo;
+} dcut_lora_args;
+dcut_status dcut_lora(dcut_ctx* ctx, const dcut_lora_args* args, const int* cu_q, int B, int T_cap, void* stream);
+
+/*
  * dcut_accept without any allocation.  (The paper has no counterpart: this entry point exists for
  * the way the library gets embedded, not for the method.)
  *
@@ -658,8 +699,9 @@ dcut_status dcut_verify_step_host(dcut_ctx* ctx, const dcut_host_step* step, voi
  * (rows at or past T_cap were left out: nothing outside the caller's T_cap rows is read or written), 8 =
  * dcut_rope_append met a token whose request, group or position has no place in the block table (it was left out), 9 =
  * dcut_prefix_attn met groups that do not cover the batch, a prefix or own positions that do not fit (nothing was written;
- * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear, dcut_linear8, dcut_rope_append or
- * dcut_rms_norm met a cu_q[B] above T_cap (rows from T_cap on were left out). */
+ * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear, dcut_linear8, dcut_rope_append,
+ * dcut_rms_norm or dcut_lora met a cu_q[B] above T_cap (rows from T_cap on were left out), 11 = dcut_lora met an adapter >= n_adapters
+ * (the request counts as one without). */
 dcut_status dcut_poll_device_status(dcut_ctx* ctx, int* code, void* stream);
 
 #ifdef __cplusplus

@@ -33,7 +33,7 @@ EXPORTS = ["dcut_create", "dcut_destroy", "dcut_last_error", "dcut_set_cost_dens
            "dcut_enable_plan_in_select", "dcut_cost_grid_create", "dcut_cost_grid_destroy", "dcut_cost_grid_budget",
            "dcut_cost_grid_record", "dcut_cost_grid_get", "dcut_cost_grid_nearest", "dcut_cost_grid_buckets",
            "dcut_set_cost_from_grid", "dcut_layer_attn_part", "dcut_layer_mlp_part", "dcut_residual_add",
-           "dcut_rope_append", "dcut_enable_prefix_attn", "dcut_prefix_attn", "dcut_linear", "dcut_rms_norm", "dcut_linear8"]
+           "dcut_rope_append", "dcut_enable_prefix_attn", "dcut_prefix_attn", "dcut_linear", "dcut_rms_norm", "dcut_linear8", "dcut_lora"]
 
 
 class Limits(C.Structure):
@@ -148,6 +148,14 @@ class NormArgs(C.Structure):
 
 
 _lib.dcut_rms_norm.argtypes = [_vp, C.POINTER(NormArgs), _vp, _i, _i, _vp]
+
+
+class LoraArgs(C.Structure):
+    _fields_ = [("x", _vp), ("ldx", _ll), ("a", _vp), ("lda", _ll), ("b", _vp), ("scale", _vp), ("adapter", _vp), ("n_adapters", _i), ("rank", _i),
+                ("n_slices", _i), ("slice_end", _i * 4), ("K", _i), ("act", _i), ("gated", _i), ("base", _vp), ("ldbase", _ll), ("out", _vp), ("ldo", _ll)]
+
+
+_lib.dcut_lora.argtypes = [_vp, C.POINTER(LoraArgs), _vp, _i, _i, _vp]
 
 
 @dataclass
@@ -680,6 +688,29 @@ class Context:
         n = NormArgs(xp, ldx, rp, ldr, _on(dev, gain, torch.bfloat16), int(gain_plus_one), int(normed), rms_eps, width, hp, ldh, op, ldo, p8, ld8,
                      _on(dev, scale8, torch.float32))
         self._check(_lib.dcut_rms_norm(self._h, C.byref(n), _on(dev, cu_q, torch.int32), 0 if cu_q is None else cu_q.shape[0] - 1, T_cap, self._stream()))
+
+    def lora(self, x, a, b, adapter, base, cu_q, T_cap: int, out=None, scale=None, slices: Optional[Sequence[int]] = None, act: str = "none", gated: bool = False):
+        """dcut_lora: out = act(base + scale (x a^T) b^T) with the adapter of each request (`adapter` int32 [B], below 0: none).  a [adapters, slices *
+        rank, K] (a view with padded rows serves), b [adapters, N, rank], base [T_cap rows, N]; `slices`: the columns at which the slices
+        end (None: one slice).  gated: the first half of the columns, activated, times the second.  out may be base."""
+        (m, N, rank), dev = b.shape, self.device
+        ends = (N,) if slices is None else slices
+        K, width = x.shape[1], N // 2 if gated else N
+        assert len(ends) <= 4 and ends[-1] == N, "at most 4 slices, the last one ending at N"
+        assert a.shape == (m, len(ends) * rank, K), f"a must be [{m}, {len(ends) * rank}, {K}], got {tuple(a.shape)}"
+        lda = a.stride(1) if a.shape[1] > 1 else K
+        assert a.get_device() == dev and a.dtype == torch.bfloat16 and (a.stride(2) == 1 or K == 1) and (m == 1 or a.stride(0) == a.shape[1] * lda), \
+            f"a must be a bf16 tensor on cuda:{dev} with dense rows, one after the other"
+        assert x.shape[0] >= T_cap and base.shape[0] >= T_cap and base.shape[1] == N
+        assert adapter.shape[0] == cu_q.shape[0] - 1 and (scale is None or scale.shape == (m,))
+        if out is None:
+            out = torch.empty((T_cap, width), dtype=torch.bfloat16, device=x.device)
+        assert out.shape[0] >= T_cap and out.shape[1] == width
+        (xp, ldx), (bp, ldb), (op, ldo) = _rows(dev, x), _rows(dev, base), _rows(dev, out)
+        l = LoraArgs(xp, ldx, a.data_ptr(), lda, _on(dev, b, torch.bfloat16), _on(dev, scale, torch.float32), _on(dev, adapter, torch.int32), m, rank, len(ends),
+                     (_i * 4)(*ends), K, ACTIVATIONS[act], int(gated), bp, ldb, op, ldo)
+        self._check(_lib.dcut_lora(self._h, C.byref(l), _on(dev, cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, self._stream()))
+        return out
 
     def make_model(self, layers: list, embed, g_final, w_lm, k_caches: list, v_caches: list, rms_eps: float = 1e-6,
                    rope_theta: float = 1e6) -> "PreparedModel":

@@ -170,6 +170,7 @@ dcut_status dcut_create(dcut_ctx** out, const dcut_limits* lim, int device) {
     }
     if ((st = dcut_init_select(c)) != DCUT_OK) return st;
     if ((st = dcut_init_accept(c)) != DCUT_OK) return st;
+    if ((st = dcut_init_lora(c)) != DCUT_OK) return st;
     if (has_attn) {
         // The work of a call is cut into one segment per SM (attn_plan.cuh): a table of at most two entries per request
         // (row blocks of its query tile), the segment boundaries, and two partial-result slots per segment (an item cut
@@ -680,6 +681,34 @@ dcut_status dcut_rms_norm(dcut_ctx* c, const dcut_norm_args* n, const int* cu_q,
     if (n->out && (n->out == n->h_out || n->out == n->residual)) return dcut_fail(c, DCUT_EINVAL, "out must not be h_out or the residual");
     DCUT_ON_DEVICE(c);
     return dcut_launch_rms_norm(c, n, cu_q, B, T_cap, static_cast<cudaStream_t>(stream));
+}
+
+dcut_status dcut_lora(dcut_ctx* c, const dcut_lora_args* l, const int* cu_q, int B, int T_cap, void* stream) {
+    if (!c) return DCUT_EINVAL;
+    if (!l || !l->x || !l->a || !l->b || !l->adapter || !l->base || !l->out || !cu_q) return dcut_fail(c, DCUT_EINVAL, "null pointer argument");
+    if (B < 1 || T_cap < 1 || l->K < 1 || l->n_adapters < 1) return dcut_fail(c, DCUT_EINVAL, "need B, T_cap, K, n_adapters >= 1");
+    if (l->n_slices < 1 || l->n_slices > DCUT_LORA_MAX_SLICES) return dcut_fail(c, DCUT_EINVAL, "n_slices = %d outside [1, %d]", l->n_slices, DCUT_LORA_MAX_SLICES);
+    if (l->rank < 8 || l->rank % 8) return dcut_fail(c, DCUT_EINVAL, "rank = %d must be a positive multiple of 8 (pad with zeros)", l->rank);
+    if (l->rank > DCUT_LORA_MAX_RANKS / l->n_slices) return dcut_fail(c, DCUT_ECAPACITY, "n_slices * rank exceeds %d", DCUT_LORA_MAX_RANKS);
+    for (int i = 0; i < l->n_slices; ++i)
+        if (l->slice_end[i] <= (i ? l->slice_end[i - 1] : 0)) return dcut_fail(c, DCUT_EINVAL, "slice_end must ascend from above 0");
+    const int N = l->slice_end[l->n_slices - 1];
+    if (N > (1 << 21) || T_cap > (1 << 21) || l->K > (1 << 30) || B > (1 << 20)) return dcut_fail(c, DCUT_ECAPACITY, "N and T_cap go up to 2^21, K to 2^30, B to 2^20");
+    if (l->act < DCUT_ACT_NONE || l->act > DCUT_ACT_SILU) return dcut_fail(c, DCUT_EINVAL, "unknown activation %d", l->act);
+    if (l->gated && (N % 2 || l->n_slices > 2 || (l->n_slices == 2 && l->slice_end[0] != N / 2)))
+        return dcut_fail(c, DCUT_EINVAL, "gated: an even N in one slice or two halves");
+    if (l->ldx < l->K || l->ldx % 8 || l->lda < l->K || l->lda % 8 || l->ldx > (1ll << 32) || l->lda > (1ll << 32))
+        return dcut_fail(c, DCUT_EINVAL, "ldx and lda must be multiples of 8 elements, >= K and <= 2^32");
+    if (l->ldbase < N || l->ldo < (l->gated ? N / 2 : N) || l->ldbase > (1ll << 32) || l->ldo > (1ll << 32))
+        return dcut_fail(c, DCUT_EINVAL, "ldbase and ldo must cover their rows and be <= 2^32");
+    if ((reinterpret_cast<uintptr_t>(l->x) | reinterpret_cast<uintptr_t>(l->a) | reinterpret_cast<uintptr_t>(l->b)) & 15)
+        return dcut_fail(c, DCUT_EINVAL, "x, a and b must be 16-byte aligned");
+    if (((reinterpret_cast<uintptr_t>(l->base) | reinterpret_cast<uintptr_t>(l->out)) & 1) || ((reinterpret_cast<uintptr_t>(l->scale) | reinterpret_cast<uintptr_t>(l->adapter)) & 3))
+        return dcut_fail(c, DCUT_EINVAL, "base and out must be 2-byte aligned, scale and adapter 4-byte");
+    if (l->out == l->base && (l->gated || l->ldo != l->ldbase)) return dcut_fail(c, DCUT_EINVAL, "out over base needs the same stride and no gate");
+    if (l->out == l->x) return dcut_fail(c, DCUT_EINVAL, "out must not be x");
+    DCUT_ON_DEVICE(c);
+    return dcut_launch_lora(c, l, cu_q, B, T_cap, static_cast<cudaStream_t>(stream));
 }
 
 dcut_status dcut_poll_device_status(dcut_ctx* c, int* code, void* stream) {

@@ -20,7 +20,8 @@
 #define DCUT_DEV_BAD_TOKEN 6            // dcut_model_verify: a token id outside [0, vocab)
 #define DCUT_DEV_BAD_CU_Q 7             // acceptance: cu_q is not a packing of B requests of 1..gamma+1 rows within T_cap
 #define DCUT_DEV_BAD_APPEND 8           // dcut_rope_append: a token's request, group or position has no place in the block table
-#define DCUT_DEV_BAD_ROWS 10            // dcut_linear(8), dcut_rope_append, dcut_rms_norm: cu_q[B] above T_cap
+#define DCUT_DEV_BAD_ROWS 10            // dcut_linear(8), dcut_rope_append, dcut_rms_norm, dcut_lora: cu_q[B] above T_cap
+#define DCUT_DEV_BAD_ADAPTER 11        // dcut_lora: an adapter that does not exist
 #define DCUT_DEV_BAD_GROUPS 9           // dcut_prefix_attn: the groups do not cover the batch, a prefix does not fit its table or contexts, or own positions their row of the block table
 
 // One row of the attention work table: a (request, row block of its query tile); it stands for n_kv_heads work items of
@@ -190,6 +191,7 @@ dcut_status dcut_init_accept(dcut_ctx* ctx);
 dcut_status dcut_init_verify_attn(dcut_ctx* ctx);
 dcut_status dcut_init_layer(dcut_ctx* ctx);
 void dcut_free_layer(dcut_ctx* ctx);
+dcut_status dcut_init_lora(dcut_ctx* ctx);
 
 // kernel launchers (one per translation unit)
 dcut_status dcut_launch_select(dcut_ctx* ctx, const float* conf, int B, int gamma, const int* draft_ids,
@@ -242,6 +244,7 @@ dcut_status dcut_launch_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_
                                     int T_cap, const dcut_prefix_groups* groups, float scale, void* out, float* lse, cudaStream_t stream);
 dcut_status dcut_launch_linear(dcut_ctx* ctx, const dcut_linear_args* l, const int* cu_q, int B, int T_cap, cudaStream_t stream);
 dcut_status dcut_launch_linear8(dcut_ctx* ctx, const dcut_linear8_args* l, const int* cu_q, int B, int T_cap, cudaStream_t stream);
+dcut_status dcut_launch_lora(dcut_ctx* ctx, const dcut_lora_args* l, const int* cu_q, int B, int T_cap, cudaStream_t stream);
 dcut_status dcut_launch_rms_norm(dcut_ctx* ctx, const dcut_norm_args* n, const int* cu_q, int B, int T_cap, cudaStream_t stream);
 dcut_status dcut_launch_rope_append(dcut_ctx* ctx, const DcutRopeArgs& a, int T_cap, cudaStream_t stream);
 dcut_status dcut_launch_residual_add(dcut_ctx* ctx, const void* a, const void* b, void* out, int width, const int* cu_q, int B,
