@@ -576,7 +576,7 @@ dcut_status dcut_linear8(dcut_ctx* ctx, const dcut_linear8_args* args, const int
  * one ends at N), with rows of `a` of their own: q|k|v or gate|up of one projection; s(n) is the slice of column n.
  *   out = act(base + d)                                                                    [T, N]
  *   out[:, j] = act((base + d)[:, j]) * (base + d)[:, N/2 + j],   gated != 0               [T, N/2] (N even; one slice, or two halves)
- * fp32 sums; s = x . a^T is scaled and then rounded to bf16 for the second product; one rounding of out.  Needs no scratch and
+ * fp32 sums; x . a^T enters the second product with 16 bits (two bf16 values); one rounding of out.  Needs no scratch and
  * no context shapes; requests of any length, T_cap is not bound by dcut_limits.
  * DEVICE in: x bf16 [T_cap, K] with ldx elements from row to row; a bf16 [n_adapters, n_slices * rank, K] with lda elements from row to row
  *   (adapters follow one another: n_slices * rank * lda); b bf16 [n_adapters, N, rank] dense; scale fp32 [n_adapters] or NULL (1);
