@@ -69,6 +69,7 @@ void free_all(dcut_ctx* c) {
     cudaFree(c->d_row_key);
     cudaFree(c->d_rs_scratch);
     cudaFree(c->d_status);
+    cudaFree(c->lora_scratch);
     cudaFree(c->prefix_scratch);
     cudaFree(c->ly_norm);
     cudaFree(c->ly_qkv);
@@ -170,6 +171,7 @@ dcut_status dcut_create(dcut_ctx** out, const dcut_limits* lim, int device) {
     }
     if ((st = dcut_init_select(c)) != DCUT_OK) return st;
     if ((st = dcut_init_accept(c)) != DCUT_OK) return st;
+    if ((st = dmalloc(c, &c->lora_scratch, DCUT_LORA_SCRATCH, "cudaMalloc(lora scratch)")) != DCUT_OK) return st;
     if ((st = dcut_init_lora(c)) != DCUT_OK) return st;
     if (has_attn) {
         // The work of a call is cut into one segment per SM (attn_plan.cuh): a table of at most two entries per request
@@ -699,8 +701,8 @@ dcut_status dcut_lora(dcut_ctx* c, const dcut_lora_args* l, const int* cu_q, int
         return dcut_fail(c, DCUT_EINVAL, "gated: an even N in one slice or two halves");
     if (l->ldx < l->K || l->ldx % 8 || l->lda < l->K || l->lda % 8 || l->ldx > (1ll << 32) || l->lda > (1ll << 32))
         return dcut_fail(c, DCUT_EINVAL, "ldx and lda must be multiples of 8 elements, >= K and <= 2^32");
-    if (l->ldbase < N || l->ldo < (l->gated ? N / 2 : N) || l->ldbase > (1ll << 32) || l->ldo > (1ll << 32))
-        return dcut_fail(c, DCUT_EINVAL, "ldbase and ldo must cover their rows and be <= 2^32");
+    if (l->ldbase < N || l->ldo < (l->gated ? N / 2 : N) || l->ldbase >= (1ll << 32) || l->ldo >= (1ll << 32))
+        return dcut_fail(c, DCUT_EINVAL, "ldbase and ldo must cover their rows and be below 2^32");
     if ((reinterpret_cast<uintptr_t>(l->x) | reinterpret_cast<uintptr_t>(l->a) | reinterpret_cast<uintptr_t>(l->b)) & 15)
         return dcut_fail(c, DCUT_EINVAL, "x, a and b must be 16-byte aligned");
     if (((reinterpret_cast<uintptr_t>(l->base) | reinterpret_cast<uintptr_t>(l->out)) & 1) || ((reinterpret_cast<uintptr_t>(l->scale) | reinterpret_cast<uintptr_t>(l->adapter)) & 3))

@@ -9,6 +9,7 @@
 
 #define DCUT_MAX_KEYS 8192      // B * gamma handled by the single-CTA selector
 #define DCUT_MAX_BUCKETS 64
+#define DCUT_LORA_SCRATCH (8ll << 20)
 
 // device status word codes (dcut_poll_device_status)
 #define DCUT_DEV_OK 0
@@ -102,6 +103,9 @@ struct dcut_ctx {
     // shared-prefix attention (dcut_enable_prefix_attn)
     unsigned char* prefix_scratch;
     int prefix_max_groups;  // 0: not enabled
+
+    // dcut_lora: the low-rank products between its two kernels
+    unsigned char* lora_scratch;   // [DCUT_LORA_SCRATCH]
 
     int* d_status;          // device status word
 

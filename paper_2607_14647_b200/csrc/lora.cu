@@ -4,14 +4,15 @@
 //   out = act(base + d), or act(base_gate + d_gate) * (base_up + d_up)
 //
 // Two products with a rank between them; each byte of x, base and out moves once, A and B of an adapter once per tile of rows (from
-// L2 but for the first).  A few multiplications per byte: the memory, and for few rows its latency, bounds it, so the products run
-// on warp-level MMAs that take their operands from global memory in 16-byte pieces: the order of a sum's terms is free, so a
-// lane's piece of 8 neighbouring elements serves as its fragments of two MMAs, and the columns of four MMAs are dealt so that
-// a lane ends with 8 neighbouring results.
-// One launch, no scratch: a tile is up to 16, 32 or 64 rows that share an adapter, done by a cluster of 8 CTAs.  Each takes an eighth of K
-// for s (its warps again an eighth each); the partial sums meet through distributed shared memory (every CTA adds an eighth of s in a
-// fixed order and hands it to all), then each takes an eighth of the columns.  s is scaled in fp32 and enters the second product as
-// the sum of two bf16 values (off by 2^-17 of it at most; a single one cost the result up to 1.7 times its error where d outweighs base).
+// L2 but for the first).  A few multiplications per byte: the memory, and for few rows its latency, bounds it, so both products run on
+// warp-level MMAs.  A tile is up to 16, 32 or 64 rows that share an adapter (of several requests, where those share it).
+//   lora_low_kernel   s of a tile, by 1 to 8 CTAs (a cluster) that cut K between them: x and A come through asynchronous copies, several steps
+//                     ahead; the partial sums meet through distributed shared memory, added in a fixed order.  s is scaled in fp32 and kept as
+//                     the sum of two bf16 values (off by 2^-17 of it at most; a single one cost the result up to 1.7 times its error where
+//                     d outweighs base), in the order in which the second product's lanes read it.
+//   lora_out_kernel   32 columns of a tile per warp, 16 rows at a time: no shared memory, no barrier, many warps per SM.
+// One kernel for both, whose clusters kept s to themselves and took an eighth of the columns per CTA each, was 1.5 to 3 times slower at length:
+// with 8 to 16 warps per SM every step waited for its loads.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -20,7 +21,7 @@
 
 namespace {
 
-constexpr int kCluster = 8, kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kMostSplit = 8, kWarps = 8, kThreads = 32 * kWarps;
 constexpr int kMaxSlices = DCUT_LORA_MAX_SLICES;
 
 struct LoraArgs {
@@ -34,10 +35,11 @@ struct LoraArgs {
     int in_place;                        // rows without an adapter keep what they have
     int vec;                             // base and out take 16-byte accesses at columns that are multiples of 8
     int end[kMaxSlices];                 // last column + 1 of each slice
-    int wn;                              // warps side by side over the columns of s
+    int wn;                              // first product: warps side by side over the columns of s; the others of a row block split K
     int part_row;                        // floats from a row of s to the next in the partial sums
-    int s_row;                           // bytes from a row of s to the next (bf16)
-    int front;                           // bytes of the partial sums
+    int tile0, blocks;                   // first tile of this pass; CTAs of the second product per tile
+    unsigned char* scratch;              // per tile: a Tile, then its s
+    long long tile_bytes;
     int* status;
 };
 
@@ -52,6 +54,11 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -62,15 +69,31 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
     return r;
 }
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// 16 bytes where `there`, else zeros.  A predicate and no branch: the loads of a step leave together.  (Not volatile: what it reads does
-// not change while the kernel runs, base excepted, which is read where the value that replaces it depends on it.)
+// Asynchronous copies to shared memory; `bytes` of the 16 are read, the rest is filled with zeros.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }       // ends a group of copies
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }   // all but the last N groups
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t shared_at(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+// what bf16 rounding took from two values (nothing from an infinity): `high` is their packed rounding
+__device__ __forceinline__ uint32_t low_parts(float x, float y, uint32_t high) {
+    const float hx = bf_lo(high), hy = bf_hi(high);
+    return pack_bf16(fabsf(hx) < INFINITY ? x - hx : 0.0f, fabsf(hy) < INFINITY ? y - hy : 0.0f);
+}
+// 16 bytes where `there`, else zeros.  A predicate and no branch: the loads of a step leave together.
 __device__ __forceinline__ uint4 load_if(const __nv_bfloat16* p, bool there) {
     uint4 v;
-    asm("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
-        "@p ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}" : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((int)there));
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+                 "@p ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}" : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((int)there));
     return v;
 }
 // the first `n` of 8 elements, one by one
@@ -82,21 +105,13 @@ __device__ __forceinline__ uint4 load_some(const __nv_bfloat16* p, int n) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// what bf16 rounding took from two values (nothing from an infinity): `high` is their packed rounding
-__device__ __forceinline__ uint32_t low_parts(float x, float y, uint32_t high) {
-    const float hx = bf_lo(high), hy = bf_hi(high);
-    return pack_bf16(fabsf(hx) < INFINITY ? x - hx : 0.0f, fabsf(hy) < INFINITY ? y - hy : 0.0f);
-}
-__device__ __forceinline__ void with_base(const uint4& v, const float (&d)[4][4], int h, float4 (&y)[2]) {
-    y[0] = make_float4(bf_lo(v.x) + d[0][2 * h], bf_hi(v.x) + d[0][2 * h + 1], bf_lo(v.y) + d[1][2 * h], bf_hi(v.y) + d[1][2 * h + 1]);
-    y[1] = make_float4(bf_lo(v.z) + d[2][2 * h], bf_hi(v.z) + d[2][2 * h + 1], bf_lo(v.w) + d[3][2 * h], bf_hi(v.w) + d[3][2 * h + 1]);
-}
-
 // What a cluster works on: up to R rows of one adapter (of several requests, where they share it).
 struct Tile {
     int rows, adapter;                   // rows = 0: there is no such tile
     int row[64];
+    int pad[14];
 };
+static_assert(sizeof(Tile) % 64 == 0, "s follows in 16-byte pieces");
 struct Search {
     int2 request[kThreads];              // adapter and rows
     int warp_sum[kWarps], before, adapter, offset;
@@ -143,10 +158,14 @@ __device__ __forceinline__ void find_tile(const LoraArgs& g, int t, int R, Tile&
         if (grouped) {
             f.request[tid] = make_int2(id, n);
             __syncthreads();
-            for (int j = 0; j < g.B; ++j) {
-                const int2 r = f.request[j];
-                if (r.x == id && j < i) first += r.y;
-                if (r.x == id && j > i) mine += r.y;
+            if (n > 0) {
+#pragma unroll 8
+                for (int j = 0; j < g.B; ++j) {
+                    const int2 r = f.request[j];
+                    const int same = r.x == id ? r.y : 0;
+                    first += j < i ? same : 0;
+                    mine += j > i ? same : 0;
+                }
             }
             if (first > 0 || n == 0) mine = 0;                          // (the first request with rows leads)
         }
@@ -189,37 +208,205 @@ __device__ __forceinline__ Group group_of(const LoraArgs& g, int i, bool gated) 
 // whether the group at column `col` is read and written in 16-byte pieces (the same answer in the whole warp)
 __device__ __forceinline__ bool by_vector(const LoraArgs& g, int col, int end) { return g.vec && !(col & 7) && col + 32 <= end; }
 
-// asks for `bytes` (a multiple of 16) from p on (aligned to 16) to come to L2
-__device__ __forceinline__ void ahead_to_l2(const void* p, uint32_t bytes) {
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+// How s lies in the scratch.  A step of the second product is 32 elements, 8 in a lane.  Ranks that are multiples of 32 take a step with the high
+// parts and again with the low ones (parts = 2); others walk the high parts and then the low ones as one row, so that rank 16 fills a step.
+// Per slice, 16 rows, step and part: rows gr and gr + 8 of the 16, a 16-byte piece per lane each.
+struct Low {
+    int steps, parts;
+    __host__ __device__ Low(int rank) : steps(rank % 32 ? (2 * rank + 31) / 32 : rank / 32), parts(rank % 32 ? 1 : 2) {}
+    __host__ __device__ int pieces() const { return steps * parts * 2; }                 // of 512 bytes, per slice and 16 rows
+    // the piece and the byte within it of element j (high or low part) of row r of a tile of MT blocks of 16 rows
+    __device__ __forceinline__ int at(int blocks16, int rank, int slice, int r, int j, int low) const {
+        const int v = parts == 1 && low ? rank + j : j, part = parts == 1 ? 0 : low;
+        return ((((slice * blocks16 + (r >> 4)) * steps + (v >> 5)) * parts + part) * 2 + ((r >> 3) & 1)) * 512 + (((r & 7) << 2) + ((v >> 3) & 3)) * 16 + (v & 7) * 2;
+    }
+};
+
+constexpr int kChunk = 64;               // elements of K per step of the first product: rows of 128 bytes, 16-byte piece c of row r at c ^ (r & 7)
+constexpr int kRowBytes = 2 * kChunk, kPieces = kRowBytes / 16, kStrideRows = kThreads / kPieces;
+constexpr int kEdgeRow = 80;             // bytes of a row of a group's results on their way to rows that take no vectors
+
+// act(v), in place.  The common ones stand here: a call's cost is that of the registers that live across it.
+template <int N>
+__device__ __forceinline__ void activate(int act, float (&v)[N]) {
+    if (act == DCUT_ACT_NONE) return;
+    if (act == DCUT_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] *= sigmoid(v[j]);
+    } else if (act == DCUT_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = v[j] < 0.0f ? 0.0f : v[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; j += 4) {
+            const float4 y = activate4(act, make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]));
+            v[j] = y.x, v[j + 1] = y.y, v[j + 2] = y.z, v[j + 3] = y.w;
+        }
+    }
 }
 
-// A tile has 16 MT WR rows: WR sets of warps with 16 MT rows each.  NT: 8-column MMA tiles of s that a warp takes at a time.
-// With MT = 1 a step's loads leave one step early; with MT = 2 the registers hold one step, and two CTAs per SM hide its latency.
-template <int WR, int MT, int NT, bool GATED>
-__global__ void __launch_bounds__(kThreads, 2) __cluster_dims__(kCluster, 1, 1) lora_kernel(LoraArgs g) {
-    constexpr int R = 16 * MT * WR, kSet = kWarps / WR, kParts = GATED ? 2 : 1;          // kSet: warps that share their rows
-    constexpr bool kEarly = MT == 1;
+// s of a tile of 16 MT rows.  A warp has 16 rows and up to 8 NT columns; STAGES - 1 steps of K are on their way.
+template <int MT, int NT, int STAGES>
+__global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g) {
+    constexpr int R = 16 * MT, kSet = kWarps / MT;                     // kSet: warps that share 16 rows
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ Tile tile;
     __shared__ Search search;
     dcut_pdl_wait();
     dcut_pdl_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gr = lane >> 2, q = lane & 3;
-    const int rank = (int)cluster_rank(), SR = g.n_slices * g.rank;
-    find_tile(g, blockIdx.x / kCluster, R, tile, search);
+    const int rank = (int)cluster_rank(), split = (int)cluster_size(), SR = g.n_slices * g.rank, number = blockIdx.x / split;
+    find_tile(g, g.tile0 + number, R, tile, search);
     const int rows = tile.rows, adapter = tile.adapter;
-    if (rows == 0) return;                                             // (the whole cluster)
-    const bool live = adapter >= 0;
-    float* red = reinterpret_cast<float*>(smem);                       // [K split][R][part_row]: the warps' sums; their total in the first
-    unsigned char* s_area = smem + g.front;                            // [R][s_row bytes]: per slice the rank's high parts, then the low ones
-    const int row_set = warp / kSet, in_set = warp % kSet, row_w = 16 * MT * row_set;     // this warp's rows: row_w ..
-    int row[MT][2];                                                    // rows that do not exist: the last one that does
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) row[m][h] = tile.row[min(row_w + 16 * m + 8 * h + gr, rows - 1)];
+    unsigned char* record = g.scratch + number * g.tile_bytes;
+    if (rank == 0 && threadIdx.x < 2 + rows) reinterpret_cast<int*>(record)[threadIdx.x] = reinterpret_cast<const int*>(&tile)[threadIdx.x];
+    if (rows == 0 || adapter < 0) return;                              // (the whole cluster)
+    float* sums = reinterpret_cast<float*>(smem);                      // in the ring's place, later: [K split of the warps][R][part_row]; the total in the first
 
+    const int chunks = (g.K + kChunk - 1) / kChunk, c0 = (int)((long long)chunks * rank / split), n_chunks = (int)((long long)chunks * (rank + 1) / split) - c0;
+    const int stage = (R + SR) * kRowBytes;
+    // a thread copies the same 16-byte piece of every 32nd row: of x (zeros where there is no row), then of A
+    const int piece = threadIdx.x % kPieces, r0 = threadIdx.x / kPieces;
+    const uint32_t ring_at = shared_at(smem), to0 = ring_at + r0 * kRowBytes + ((piece ^ (r0 & 7)) << 4);
+    constexpr int kX = (R + kStrideRows - 1) / kStrideRows;
+    const __nv_bfloat16* x_from[kX];                                   // (these two move along K with the steps that are asked for)
+#pragma unroll
+    for (int i = 0; i < kX; ++i) x_from[i] = g.x + (size_t)tile.row[min(r0 + kStrideRows * i, rows - 1)] * g.ldx + (size_t)c0 * kChunk + 8 * piece;
+    const __nv_bfloat16* a_from = g.a + ((size_t)adapter * SR + r0) * g.lda + (size_t)c0 * kChunk + 8 * piece;
+    const long long a_step = kStrideRows * g.lda;
+    int left = 2 * (g.K - c0 * kChunk - 8 * piece), asked = 0;         // bytes from this thread's next piece to the end of its rows; steps asked for
+    auto load = [&](int slot) {
+        if (asked < n_chunks) {
+            const uint32_t to = to0 + slot * stage;
+            const int bytes = min(16, max(0, left));                   // (0: nothing is read, and the address is one that exists)
+#pragma unroll
+            for (int i = 0; i < kX; ++i)
+                if (R % kStrideRows == 0 || r0 + kStrideRows * i < R)
+                    copy16(to + i * kStrideRows * kRowBytes, bytes ? x_from[i] : g.x, r0 + kStrideRows * i < rows ? bytes : 0), x_from[i] += kChunk;
+            const __nv_bfloat16* from = bytes ? a_from : g.a;
+            const long long step = bytes ? a_step : 0;
+            uint32_t to_a = to + R * kRowBytes;
+#pragma unroll 4
+            for (int r = r0; r < SR; r += kStrideRows, to_a += kStrideRows * kRowBytes, from += step) copy16(to_a, from, bytes);
+            a_from += kChunk, left -= kRowBytes, ++asked;
+        }
+        copies_done();
+    };
+    const int wn = min(g.wn, kSet), wk = kSet / wn, m = warp / kSet, in_set = warp % kSet, my_n = in_set % wn, my_k = in_set / wn;
+    const int tiles = SR / 8, per = (tiles + wn - 1) / wn, t0 = my_n * per, nt = min(per, tiles - t0);         // this warp's 8-column tiles of s
+    // this lane's rows for ldmatrix: where they begin in a step, and the swizzle with the half of 16 elements that the lane points to
+    const int x_row = 16 * m + (lane & 15), x_at = x_row * kRowBytes, x_flip = ((x_row & 7) ^ (lane >> 4)) << 4;
+    const int a_flip = ((lane & 7) ^ ((lane >> 3) & 1)) << 4;          // (R and the tiles' first rows are multiples of 8)
+    int a_at[(NT + 1) / 2];                                            // (a tile that does not exist: the last one that does)
+#pragma unroll
+    for (int n = 0; n < NT; n += 2) a_at[n / 2] = (R + 8 * min(t0 + n + (lane >> 4), tiles - 1) + (lane & 7)) * kRowBytes;
+    float acc[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < STAGES - 1; ++c) load(c);
+    for (int c = 0, slot = 0, ahead = STAGES - 1; c < n_chunks; ++c) {
+        copies_wait<STAGES - 2>();
+        __syncthreads();                                               // step c has arrived, step c - 1 has been read
+        load(ahead);
+        const uint32_t at = ring_at + slot * stage;
+        auto multiply = [&](int k) {                                   // 16 elements of K
+            uint32_t xf[4];
+            ldmatrix4(xf, at + x_at + ((32 * k) ^ x_flip));
+#pragma unroll
+            for (int n = 0; n < NT; n += 2) {
+                if (n >= nt) break;
+                uint32_t af[4];                                        // two tiles' fragments
+                ldmatrix4(af, at + a_at[n / 2] + ((32 * k) ^ a_flip));
+                mma16816(acc[n], xf[0], xf[1], xf[2], xf[3], af[0], af[1]);
+                if (n + 1 < nt) mma16816(acc[n + 1], xf[0], xf[1], xf[2], xf[3], af[2], af[3]);
+            }
+        };
+        if (wk == 1) {
+#pragma unroll
+            for (int k = 0; k < kChunk / 16; ++k) multiply(k);
+        } else {                                                       // the warps of a set take turns
+            for (int k = (my_k - c * (kChunk / 16)) & (wk - 1); k < kChunk / 16; k += wk) multiply(k);
+        }
+        slot = slot + 1 == STAGES ? 0 : slot + 1;
+        ahead = ahead + 1 == STAGES ? 0 : ahead + 1;
+    }
+    copies_wait<0>();
+    __syncthreads();                                                   // the ring is free
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        if (n >= nt) break;
+        float* p = sums + (my_k * R + 16 * m + gr) * g.part_row + 8 * (t0 + n) + 2 * q;
+        *reinterpret_cast<float2*>(p) = make_float2(acc[n][0], acc[n][1]);
+        *reinterpret_cast<float2*>(p + 8 * g.part_row) = make_float2(acc[n][2], acc[n][3]);
+    }
+    const int quads = SR / 4;
+    if (wk > 1) {
+        __syncthreads();
+        for (int e = threadIdx.x; e < R * quads; e += kThreads) {
+            const int r = e / quads, c = 4 * (e - r * quads);
+            float* p = sums + r * g.part_row + c;
+            float4 s = *reinterpret_cast<const float4*>(p);
+            for (int w = 1; w < wk; ++w) {
+                const float4 v = *reinterpret_cast<const float4*>(p + w * R * g.part_row);
+                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+            }
+            *reinterpret_cast<float4*>(p) = s;
+        }
+    }
+    cluster_sync();                                                    // every CTA's share is complete
+    const float scale = g.scale ? g.scale[adapter] : 1.0f;
+    const uint32_t sums_at = shared_at(sums);
+    const Low low(g.rank);
+    unsigned char* s_out = record + sizeof(Tile);
+    const int each = R * quads / split;                                // (R is a multiple of 16, SR of 8, the split of 8 a divisor)
+    for (int e = rank * each + threadIdx.x; e < (rank + 1) * each; e += kThreads) {
+        const int r = e / quads, c = 4 * (e - r * quads), slice = c / g.rank, j = c - slice * g.rank;
+        float4 s = make_float4(0, 0, 0, 0), v[kMostSplit];
+#pragma unroll
+        for (int p = 0; p < kMostSplit; ++p)
+            if (p < split)
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[p].x), "=f"(v[p].y), "=f"(v[p].z), "=f"(v[p].w)
+                             : "r"(in_cta(sums_at + 4 * (r * g.part_row + c), p)) : "memory");
+#pragma unroll
+        for (int p = 0; p < kMostSplit; ++p)
+            if (p < split) s.x += v[p].x, s.y += v[p].y, s.z += v[p].z, s.w += v[p].w;
+        s.x *= scale, s.y *= scale, s.z *= scale, s.w *= scale;
+        const uint32_t hi0 = pack_bf16(s.x, s.y), hi1 = pack_bf16(s.z, s.w);
+        *reinterpret_cast<uint2*>(s_out + low.at(MT, g.rank, slice, r, j, 0)) = make_uint2(hi0, hi1);
+        *reinterpret_cast<uint2*>(s_out + low.at(MT, g.rank, slice, r, j, 1)) = make_uint2(low_parts(s.x, s.y, hi0), low_parts(s.z, s.w, hi1));
+    }
+    if (low.parts == 1 && rank == split - 1) {                         // what fills up the last step
+        const int rest = (32 * low.steps - 2 * g.rank) / 4;
+        for (int e = threadIdx.x; e < g.n_slices * R * rest; e += kThreads) {
+            const int sr = e / rest, v = 2 * g.rank + 4 * (e - sr * rest);
+            *reinterpret_cast<uint2*>(s_out + low.at(MT, g.rank, sr / R, sr % R, v, 0)) = make_uint2(0, 0);
+        }
+    }
+    cluster_sync();                                                    // nobody leaves while its sums are read
+}
+
+// out of a tile: a warp has 32 columns, 16 rows at a time.  The MMA's column n of tile t is column 8 (n >> 1) + 2 t + (n & 1) of the 32, so that
+// a lane ends with the 8 neighbouring columns 8 q .. + 7; its 8 neighbouring elements of s and of B serve as its fragments of two MMAs
+// (the order of a sum's terms is free).  KEEP: the rank's steps, where B's fragments stay in registers for all rows; 0: they are read again.
+// `early`: the CTA finds its tile itself and asks for B and its first rows of base while the first product runs (what that one waited for is
+// complete once this grid has started); otherwise it reads the tile from the scratch.
+template <bool GATED, int KEEP>
+__global__ void __launch_bounds__(kThreads, GATED || KEEP > 1 ? 2 : 3) lora_out_kernel(LoraArgs g, int blocks16, int early) {
+    constexpr int kParts = GATED ? 2 : 1;
+    __shared__ __align__(16) unsigned char edges[kWarps][16 * kEdgeRow];
+    __shared__ Tile tile;
+    __shared__ Search search;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gr = lane >> 2, q = lane & 3;
+    const int number = blockIdx.x / g.blocks;
+    const unsigned char* record = g.scratch + number * g.tile_bytes;
+    if (early) find_tile(g, g.tile0 + number, 16 * blocks16, tile, search);
+    else {
+        dcut_pdl_wait();
+        if (threadIdx.x < 66) reinterpret_cast<int*>(&tile)[threadIdx.x] = reinterpret_cast<const int*>(record)[threadIdx.x];
+        __syncthreads();
+    }
+    const int rows = tile.rows, adapter = tile.adapter;
     const int width = GATED ? g.N / 2 : g.N;                           // columns of out
     int groups = 0;
     if (GATED) groups = (width + 31) / 32;
@@ -228,274 +415,197 @@ __global__ void __launch_bounds__(kThreads, 2) __cluster_dims__(kCluster, 1, 1) 
             groups += (g.end[s] - lo + 31) / 32;
             lo = g.end[s];
         }
-    const int g0 = (int)((long long)groups * rank / kCluster), g1 = (int)((long long)groups * (rank + 1) / kCluster);
-    const __nv_bfloat16* b = g.b + (size_t)max(adapter, 0) * g.N * g.rank;
-    if (live && warp == kWarps - 1 && lane < kParts && g0 < g1) {       // this CTA's rows of B
-        const Group from = group_of(g, g0, GATED), to = group_of(g, g1 - 1, GATED);
-        const int n = min(to.col + 32, to.end) - from.col;
-        ahead_to_l2(b + (size_t)(lane * width + from.col) * g.rank, (uint32_t)n * g.rank * 2);
-    }
-    // s is kept as the sum of two bf16 values.  A step is 32 elements of the rank, 8 in a lane, and both parts take it (wide); ranks that
-    // are no multiple of 32 walk the high parts and the low ones as one row of 2 rank elements instead, so that rank 16 fills a step.
-    const bool wide = g.rank % 32 == 0;
-    const int row_len = wide ? g.rank : 2 * g.rank, steps = live ? (row_len + 31) / 32 : 0;
-
-    // rows col + 8 (n >> 1) + 2 t + (n & 1) of B, n the MMA's column: a lane ends with columns col + 8 q .. + 7 of the results
-    auto load_b = [&](const Group& at, int part, int step, uint4 (&bv)[4]) {
-        const int v = 32 * step + 8 * q, k = v >= g.rank ? v - g.rank : v;
-        const int first = part ? width + at.col : at.col, end = part ? g.N : at.end;
+    const int i = (blockIdx.x - number * g.blocks) * kWarps + warp;
+    const bool work = rows > 0 && i < groups, live = work && adapter >= 0;
+    const Group at = group_of(g, work ? i : 0, GATED);
+    const Low low(g.rank);
+    const bool vec = by_vector(g, at.col, at.end), vec_up = GATED && by_vector(g, width + at.col, g.N);
+    // B: rows b_row + 2 t of a part's columns; elements from this lane's first one of a step on (behind both parts s is zero, and so is this)
+    const int b_row = 8 * (gr >> 1) + (gr & 1);
+    const __nv_bfloat16* b = g.b + ((size_t)max(adapter, 0) * g.N + at.col + b_row) * g.rank;
+    const int left = at.end - at.col - b_row, left_up = g.N - width - at.col - b_row;
+    auto load_b = [&](int part, int step, uint4 (&bv)[4]) {
+        const int v = 32 * step + 8 * q, k = v < g.rank ? v : v - g.rank;
+        const __nv_bfloat16* p = b + (part ? (size_t)width * g.rank : 0) + k;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int n = first + 8 * (gr >> 1) + 2 * t + (gr & 1);
-            bv[t] = load_if(b + (size_t)n * g.rank + k, n < end && v < row_len);
+        for (int t = 0; t < 4; ++t, p += 2 * g.rank) bv[t] = load_if(p, 2 * t < (part ? left_up : left) && v < 2 * g.rank);
+    };
+    // base at this lane's 8 columns of rows gr and gr + 8 of block m (those that do not exist: of the last one that does)
+    auto fetch = [&](int m, int (&row)[2], uint4 (&v)[kParts][2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            row[h] = tile.row[min(16 * m + 8 * h + gr, rows - 1)];
+            const __nv_bfloat16* p = g.base + (unsigned long long)(unsigned)row[h] * (unsigned)g.ldbase + at.col + 8 * q;
+            v[0][h] = vec ? *reinterpret_cast<const uint4*>(p) : load_some(p, at.end - at.col - 8 * q);
+            if (GATED) v[kParts - 1][h] = vec_up ? *reinterpret_cast<const uint4*>(p + width) : load_some(p + width, at.end - at.col - 8 * q);
         }
     };
-    // base at this lane's 8 columns of its rows
-    auto fetch = [&](const Group& at, int part, uint4 (&v)[MT][2]) {
-        const int col = (part ? width + at.col : at.col) + 8 * q, end = part ? g.N : at.end;
-        const bool vec = by_vector(g, col - 8 * q, end);
+    uint4 kept[KEEP ? kParts * KEEP : 1][4], base[kParts][2];
+    int row[2];
+    if (work) fetch(0, row, base);
+    if (KEEP && live) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int part = 0; part < kParts; ++part)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const bool there = row_w + 16 * m + 8 * h + gr < rows;
-                const __nv_bfloat16* p = g.base + (size_t)row[m][h] * g.ldbase + col;
-                v[m][h] = vec ? load_if(p, there) : load_some(p, there ? end - col : 0);
-            }
-    };
-
-    Group at = {0, 0, 0};
-    uint4 bv[4], base[MT][2];
-    int i = g0 + in_set;
-    if (i < g1) {
-        at = group_of(g, i, GATED);
-        if (kEarly) {                                                  // what the first columns need does not wait for s
-            if (live) load_b(at, 0, 0, bv);
-            fetch(at, 0, base);
-        }
+            for (int step = 0; step < KEEP; ++step) load_b(part, step, kept[part * KEEP + step]);
     }
+    if (early) dcut_pdl_wait();
+    dcut_pdl_launch_dependents();
+    if (!work) return;
 
-    if (live) {
-        // ---- s = x . A^T: this CTA's eighth of K; the warps of a set share the columns (wn of them) and then K (wk of them)
-        const __nv_bfloat16* a = g.a + (size_t)adapter * SR * g.lda + 8 * q;
-        const int chunks = (g.K + 31) / 32, c0 = (int)((long long)chunks * rank / kCluster), c1 = (int)((long long)chunks * (rank + 1) / kCluster);
-        const int wn = min(g.wn, kSet), wk = kSet / wn, my_n = in_set % wn, my_k = in_set / wn;
-        const __nv_bfloat16* xp[MT][2];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) xp[m][h] = g.x + (size_t)row[m][h] * g.ldx + 8 * q;
-        for (int n0 = 8 * NT * my_n; n0 < SR; n0 += 8 * NT * wn) {
-            float acc[MT][NT][4];
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) acc[m][n][0] = acc[m][n][1] = acc[m][n][2] = acc[m][n][3] = 0.0f;
-            auto load = [&](int c, uint4 (&xv)[MT][2], uint4 (&av)[NT]) {
-                const int left = g.K - 32 * c - 8 * q;                  // elements from this lane's first one on
-                const bool there = left >= 8 && c < c1;
-#pragma unroll
-                for (int m = 0; m < MT; ++m) xv[m][0] = load_if(xp[m][0] + 32 * c, there), xv[m][1] = load_if(xp[m][1] + 32 * c, there);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) av[n] = load_if(a + (size_t)(n0 + 8 * n + gr) * g.lda + 32 * c, there && n0 + 8 * n < SR);
-                if ((g.K & 7) && c == chunks - 1 && c < c1 && left > 0 && left < 8) {
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) xv[m][0] = load_some(xp[m][0] + 32 * c, left), xv[m][1] = load_some(xp[m][1] + 32 * c, left);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) av[n] = load_some(a + (size_t)(n0 + 8 * n + gr) * g.lda + 32 * c, n0 + 8 * n < SR ? left : 0);
-                }
-            };
-            uint4 xv[MT][2], av[NT], xn[MT][2], an[NT];
-            if (kEarly) load(c0 + my_k, xv, av);
-            for (int c = c0 + my_k; c < c1; c += wk) {
-                if (kEarly) load(c + wk, xn, an);
-                else load(c, xv, av);
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        mma16816(acc[m][n], xv[m][0].x, xv[m][1].x, xv[m][0].y, xv[m][1].y, av[n].x, av[n].y);
-                        mma16816(acc[m][n], xv[m][0].z, xv[m][1].z, xv[m][0].w, xv[m][1].w, av[n].z, av[n].w);
-                    }
-                if (kEarly) {
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) xv[m][0] = xn[m][0], xv[m][1] = xn[m][1];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) av[n] = an[n];
-                }
-            }
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if (n0 + 8 * n >= SR) continue;
-                    float* p = red + (my_k * R + row_w + 16 * m + gr) * g.part_row + n0 + 8 * n + 2 * q;
-                    *reinterpret_cast<float2*>(p) = make_float2(acc[m][n][0], acc[m][n][1]);
-                    *reinterpret_cast<float2*>(p + 8 * g.part_row) = make_float2(acc[m][n][2], acc[m][n][3]);
-                }
-        }
-        const int quads = SR / 4;
-        if (wk > 1) {
-            __syncthreads();
-            for (int e = threadIdx.x; e < R * quads; e += kThreads) {
-                const int r = e / quads, c = 4 * (e - r * quads);
-                float* p = red + r * g.part_row + c;
-                float4 s = *reinterpret_cast<const float4*>(p);
-                for (int w = 1; w < wk; ++w) {
-                    const float4 v = *reinterpret_cast<const float4*>(p + w * R * g.part_row);
-                    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-                }
-                *reinterpret_cast<float4*>(p) = s;
-            }
-        }
-        cluster_sync();                                                // every CTA's share is complete
-        const float scale = g.scale ? g.scale[adapter] : 1.0f;
-        const uint32_t red_at = static_cast<uint32_t>(__cvta_generic_to_shared(red)), s_at = static_cast<uint32_t>(__cvta_generic_to_shared(s_area));
-        const int each = R * quads / kCluster;                         // (R is a multiple of 16, SR of 8)
-        for (int e = rank * each + threadIdx.x; e < (rank + 1) * each; e += kThreads) {
-            const int r = e / quads, c = 4 * (e - r * quads), slice = c / g.rank;
-            float4 v[kCluster], s = make_float4(0, 0, 0, 0);
-#pragma unroll
-            for (int p = 0; p < kCluster; ++p)
-                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[p].x), "=f"(v[p].y), "=f"(v[p].z), "=f"(v[p].w)
-                             : "r"(in_cta(red_at + 4 * (r * g.part_row + c), p)) : "memory");
-#pragma unroll
-            for (int p = 0; p < kCluster; ++p) s.x += v[p].x, s.y += v[p].y, s.z += v[p].z, s.w += v[p].w;
-            s.x *= scale, s.y *= scale, s.z *= scale, s.w *= scale;
-            const uint32_t hi0 = pack_bf16(s.x, s.y), hi1 = pack_bf16(s.z, s.w);
-            const uint32_t lo0 = low_parts(s.x, s.y, hi0), lo1 = low_parts(s.z, s.w, hi1);
-            const uint32_t to = s_at + r * g.s_row + 2 * (c + slice * g.rank);
-#pragma unroll
-            for (int p = 0; p < kCluster; ++p) {
-                const uint32_t there = in_cta(to, p);
-                asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(there), "r"(hi0), "r"(hi1) : "memory");
-                asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(there + 2 * g.rank), "r"(lo0), "r"(lo1) : "memory");
-            }
-        }
-        cluster_sync();                                                // s is complete everywhere; nothing remote is read or written after this
-    }
-
-    // ---- this CTA's eighth of the columns
-    for (; i < g1; i += kSet) {
-        const Group next = i + kSet < g1 ? group_of(g, i + kSet, GATED) : at;
-        float y[MT][2][8];                                             // this lane's results, row by row
+    const uint4* s_in = reinterpret_cast<const uint4*>(record + sizeof(Tile)) + lane;
+    for (int m = 0; 16 * m < rows; ++m) {
+        float y[2][8];
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
-            uint4 here[MT][2], bn[4];
-            if (kEarly) {                                              // on their way: what follows this part
+            float d[4][4];
 #pragma unroll
-                for (int m = 0; m < MT; ++m) here[m][0] = base[m][0], here[m][1] = base[m][1];
-                if (part + 1 < kParts) fetch(at, part + 1, base);
-                else fetch(next, 0, base);
-            } else {
-                if (live) load_b(at, part, 0, bv);
-                fetch(at, part, here);
-            }
-            float d[MT][4][4];
+            for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.0f;
+            if (live) {
+                const uint4* s_at = s_in + ((GATED ? (g.n_slices == 2 ? part : 0) : at.slice) * blocks16 + m) * low.pieces() * 32;
+                auto multiply = [&](const uint4 (&bv)[4]) {
+                    const uint4 s0 = s_at[0], s1 = s_at[32];
+                    s_at += 64;
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+                    for (int t = 0; t < 4; ++t) mma16816(d[t], s0.x, s1.x, s0.y, s1.y, bv[t].x, bv[t].y);
 #pragma unroll
-                for (int t = 0; t < 4; ++t) d[m][t][0] = d[m][t][1] = d[m][t][2] = d[m][t][3] = 0.0f;
-            const int slice = GATED ? (g.n_slices == 2 ? part : 0) : at.slice;
+                    for (int t = 0; t < 4; ++t) mma16816(d[t], s0.z, s1.z, s0.w, s1.w, bv[t].z, bv[t].w);
+                };
+                if (KEEP) {
+#pragma unroll
+                    for (int step = 0; step < KEEP; ++step) {
+                        multiply(kept[part * KEEP + step]);
+                        if (low.parts == 2) multiply(kept[part * KEEP + step]);
+                    }
+                } else {
 #pragma unroll 1
-            for (int step = 0; step < steps; ++step) {
-                if (step + 1 < steps) load_b(at, part, step + 1, bn);
-                else if (kEarly) {
-                    if (part + 1 < kParts) load_b(at, part + 1, 0, bn);
-                    else load_b(next, 0, 0, bn);
-                }
-                const int v = 32 * step + 8 * q;
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const unsigned char* p = s_area + (row_w + 16 * m + gr) * g.s_row + 2 * (2 * slice * g.rank + v);
-#pragma unroll
-                    for (int low = 0; low < 2; ++low) {
-                        if (low && !wide) break;
-                        uint4 s0 = make_uint4(0, 0, 0, 0), s1 = s0;
-                        if (v < row_len) {
-                            s0 = *reinterpret_cast<const uint4*>(p + 2 * low * g.rank);
-                            s1 = *reinterpret_cast<const uint4*>(p + 2 * low * g.rank + 8 * g.s_row);
-                        }
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) {
-                            mma16816(d[m][t], s0.x, s1.x, s0.y, s1.y, bv[t].x, bv[t].y);
-                            mma16816(d[m][t], s0.z, s1.z, s0.w, s1.w, bv[t].z, bv[t].w);
-                        }
+                    for (int step = 0; step < low.steps; ++step) {
+                        uint4 bv[4];
+                        load_b(part, step, bv);
+                        multiply(bv);
+                        if (low.parts == 2) multiply(bv);
                     }
                 }
-#pragma unroll
-                for (int t = 0; t < 4; ++t) bv[t] = bn[t];
             }
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    float4 z[2];
-                    with_base(here[m][h], d[m], h, z);
-                    if (part == 0 && g.act != DCUT_ACT_NONE) z[0] = activate4(g.act, z[0]), z[1] = activate4(g.act, z[1]);
-                    const float zs[8] = {z[0].x, z[0].y, z[0].z, z[0].w, z[1].x, z[1].y, z[1].z, z[1].w};
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y[m][h][j] = part == 0 ? zs[j] : y[m][h][j] * zs[j];
-                }
-        }
-        const int mine = at.col + 8 * q;
-        const bool vec = by_vector(g, at.col, at.end);
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (row_w + 16 * m + 8 * h + gr >= rows) continue;
-                __nv_bfloat16* o = g.out + (size_t)row[m][h] * g.ldo + mine;
-                const float(&v)[8] = y[m][h];
-                const uint32_t w[4] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-                if (vec) *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
-                else
+                const uint4 w = base[part][h];
+                float v[8] = {bf_lo(w.x) + d[0][2 * h], bf_hi(w.x) + d[0][2 * h + 1], bf_lo(w.y) + d[1][2 * h], bf_hi(w.y) + d[1][2 * h + 1],
+                              bf_lo(w.z) + d[2][2 * h], bf_hi(w.z) + d[2][2 * h + 1], bf_lo(w.w) + d[3][2 * h], bf_hi(w.w) + d[3][2 * h + 1]};
+                if (part == 0) activate(g.act, v);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (mine + j < at.end) reinterpret_cast<unsigned short*>(o)[j] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+                for (int j = 0; j < 8; ++j) y[h][j] = part ? y[h][j] * v[j] : v[j];
             }
-        at = next;
+        }
+        const int row_now[2] = {row[0], row[1]};
+        if (16 * (m + 1) < rows) fetch(m + 1, row, base);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float(&v)[8] = y[h];
+            const uint4 w = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            const int r = 8 * h + gr;
+            if (!vec) *reinterpret_cast<uint4*>(edges[warp] + r * kEdgeRow + 16 * q) = w;
+            else if (16 * m + r < rows)
+                *reinterpret_cast<uint4*>(g.out + (unsigned long long)(unsigned)row_now[h] * (unsigned)g.ldo + at.col + 8 * q) = w;
+        }
+        if (!vec) {                                                    // a row's 32 columns at a time
+            __syncwarp();
+            if (at.col + lane < at.end)
+                for (int r = 0; r < 16 && 16 * m + r < rows; ++r)
+                    reinterpret_cast<unsigned short*>(g.out)[(size_t)tile.row[16 * m + r] * g.ldo + at.col + lane] =
+                        *reinterpret_cast<const unsigned short*>(edges[warp] + r * kEdgeRow + 2 * lane);
+            __syncwarp();
+        }
     }
 }
 
-template <int WR, int MT, int NT, bool GATED>
-dcut_status launch(dcut_ctx* ctx, LoraArgs& g, cudaStream_t stream) {
-    constexpr int R = 16 * MT * WR, kSet = kWarps / WR;
-    const int SR = g.n_slices * g.rank, share = (SR + 8 * NT - 1) / (8 * NT);
-    g.wn = share > 2 ? 4 : share;                                      // warps side by side over the columns of s; the others split K
-    const int wk = kSet / (g.wn < kSet ? g.wn : kSet);
-    g.front = (wk * R * g.part_row * 4 + 127) & ~127;
-    const size_t smem = (size_t)g.front + (size_t)R * g.s_row;
-    // the sum of ceil(rows / R) over the units that are cut into tiles, at most: adapters (and the rows without one), or requests
-    const int units = g.B <= kThreads && g.n_adapters < g.B ? g.n_adapters + 1 : g.B;
-    const long long tiles = ((long long)g.T_cap + (long long)units * (R - 1)) / R;
-    return dcut_check_cuda(ctx, dcut_launch_pdl(lora_kernel<WR, MT, NT, GATED>, dim3((unsigned)(tiles * kCluster)), dim3(kThreads), smem, stream, g),
-                           "launch lora_kernel");
+constexpr int kMostShared = 110 * 1024;                                 // two CTAs of the first product per SM
+
+template <int MT, int NT, int STAGES>
+dcut_status launch_low(dcut_ctx* ctx, const LoraArgs& g, int grid, int split, size_t smem, cudaStream_t stream) {
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = split;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(grid);
+    lc.blockDim = dim3(kThreads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = stream;
+    lc.attrs = attr;
+    lc.numAttrs = 2;
+    return dcut_check_cuda(ctx, cudaLaunchKernelEx(&lc, lora_low_kernel<MT, NT, STAGES>, g), "launch lora_low_kernel");
 }
-template <int WR, int MT>
-dcut_status launch(dcut_ctx* ctx, LoraArgs& g, cudaStream_t stream) {
-    const bool few = g.n_slices * g.rank <= 16;
-    if (g.gated) return few ? launch<WR, MT, 2, true>(ctx, g, stream) : launch<WR, MT, 4, true>(ctx, g, stream);
-    return few ? launch<WR, MT, 2, false>(ctx, g, stream) : launch<WR, MT, 4, false>(ctx, g, stream);
+// How the first product of a launch runs
+struct Plan {
+    int wn, stages;
+    size_t smem;
+};
+template <int MT>
+Plan plan_low(int SR) {
+    constexpr int R = 16 * MT, kSet = kWarps / MT;
+    Plan p;
+    for (p.wn = 1; p.wn < kSet && (SR / 8 + p.wn - 1) / p.wn > 4;) p.wn *= 2;             // up to 4 tiles of s per warp, where there are warps for it
+    const int stage = (R + SR) * kRowBytes, sums = kSet / p.wn * R * (SR + 8) * 4;
+    p.stages = 8 * stage <= kMostShared ? 8 : 4 * stage <= kMostShared ? 4 : 2;
+    p.smem = p.stages * stage > sums ? p.stages * stage : sums;
+    return p;
 }
-template <int WR, int MT>
+template <int MT>
+dcut_status launch(dcut_ctx* ctx, LoraArgs& g, int units, cudaStream_t stream) {
+    constexpr int R = 16 * MT, NT = 8;
+    const int SR = g.n_slices * g.rank;
+    const Plan p = plan_low<MT>(SR);
+    g.wn = p.wn;
+    g.part_row = SR + 8;
+    g.tile_bytes = (long long)sizeof(Tile) + (long long)g.n_slices * MT * Low(g.rank).pieces() * 512;
+    int groups = 0;
+    for (int s = 0, lo = 0; s < (g.gated ? 1 : g.n_slices); ++s) {
+        const int end = g.gated ? g.N / 2 : g.end[s];
+        groups += (end - lo + 31) / 32;
+        lo = end;
+    }
+    g.blocks = (groups + kWarps - 1) / kWarps;
+    // the sum of ceil(rows / R) over the units that are cut into tiles, at most; as many of them at a time as the scratch holds
+    const long long tiles = ((long long)g.T_cap + (long long)units * (R - 1)) / R, room = DCUT_LORA_SCRATCH / g.tile_bytes;
+    for (long long t = 0; t < tiles; t += room) {
+        const int n = (int)(tiles - t < room ? tiles - t : room);
+        g.tile0 = (int)t;
+        int split = kMostSplit;                                         // CTAs per tile: one wave of two per SM, where there are tiles for it
+        while (split > 1 && (long long)n * split > 2 * ctx->sm_count) split >>= 1;
+        dcut_status st = p.stages == 8   ? launch_low<MT, NT, 8>(ctx, g, n * split, split, p.smem, stream)
+                         : p.stages == 4 ? launch_low<MT, NT, 4>(ctx, g, n * split, split, p.smem, stream)
+                                         : launch_low<MT, NT, 2>(ctx, g, n * split, split, p.smem, stream);
+        if (st != DCUT_OK) return st;
+        const int steps = Low(g.rank).steps;
+        auto* out = g.gated ? (steps == 1 ? lora_out_kernel<true, 1> : lora_out_kernel<true, 0>)
+                            : (steps == 1 ? lora_out_kernel<false, 1> : steps == 2 ? lora_out_kernel<false, 2> : lora_out_kernel<false, 0>);
+        const long long ctas = (long long)n * g.blocks;
+        const int early = ctas <= 2 * ctx->sm_count;                     // all of them can wait beside the first product
+        st = dcut_check_cuda(ctx, dcut_launch_pdl(out, dim3((unsigned)ctas), dim3(kThreads), 0, stream, g, MT, early), "launch lora_out_kernel");
+        if (st != DCUT_OK) return st;
+    }
+    return DCUT_OK;
+}
+template <int MT>
 cudaError_t allow() {
-    // as many splits of K as there can be with so many ranks: 8 / WR up to 32, half of that up to 64, then a quarter
-    constexpr int R = 16 * MT * WR, kMost = 160 * 1024;
-    constexpr int at32 = 8 / WR * R * 40 * 4 + R * 192, at256 = (2 / WR < 1 ? 1 : 2 / WR) * R * (DCUT_LORA_MAX_RANKS + 8) * 4 + R * (4 * DCUT_LORA_MAX_RANKS + 64);
-    static_assert(at32 + 128 <= kMost && at256 + 128 <= kMost, "fits an SM");
-    cudaError_t e = cudaFuncSetAttribute(lora_kernel<WR, MT, 2, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_kernel<WR, MT, 4, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_kernel<WR, MT, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-    return e == cudaSuccess ? cudaFuncSetAttribute(lora_kernel<WR, MT, 4, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost) : e;
+    constexpr int R = 16 * MT, M = MT > 2 ? DCUT_LORA_MAX_RANKS / 2 : DCUT_LORA_MAX_RANKS, NT = 8;
+    static_assert(2 * (R + M) * kRowBytes <= kMostShared && R * (M + 8) * 4 <= kMostShared && 2 * R * (M / 2 + 8) * 4 <= kMostShared, "two steps and the sums fit");
+    static_assert(M / 8 <= NT * (kWarps / MT), "a warp's tiles of s");
+    cudaError_t e = cudaFuncSetAttribute(lora_low_kernel<MT, NT, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_low_kernel<MT, NT, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    return e == cudaSuccess ? cudaFuncSetAttribute(lora_low_kernel<MT, NT, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared) : e;
 }
 
 }  // namespace
 
 dcut_status dcut_init_lora(dcut_ctx* ctx) {
-    cudaError_t e = allow<1, 1>();
-    if (e == cudaSuccess) e = allow<1, 2>();
-    if (e == cudaSuccess) e = allow<2, 2>();
+    cudaError_t e = allow<1>();
+    if (e == cudaSuccess) e = allow<2>();
+    if (e == cudaSuccess) e = allow<4>();
     return dcut_check_cuda(ctx, e, "cudaFuncSetAttribute(lora)");
 }
 
@@ -515,10 +625,10 @@ dcut_status dcut_launch_lora(dcut_ctx* ctx, const dcut_lora_args* l, const int* 
     g.in_place = l->out == l->base && l->act == DCUT_ACT_NONE && !g.gated;
     auto vec = [](const void* p, long long ld) { return !(reinterpret_cast<uintptr_t>(p) & 15) && ld % 8 == 0; };
     g.vec = vec(l->base, l->ldbase) && vec(l->out, l->ldo);
-    const int SR = g.n_slices * g.rank;
-    g.part_row = SR + 8;
-    g.s_row = (4 * SR + 127) / 128 * 128 + 64;                         // rows 64 bytes apart modulo 128: no two lanes of a 16-byte read meet in a bank
     g.status = ctx->d_status;
-    const long long mean = T_cap / (B <= kThreads && g.n_adapters < B ? g.n_adapters : B);   // rows of a unit, at most, on average
-    return mean <= 8 ? launch<1, 1>(ctx, g, stream) : mean <= 40 ? launch<1, 2>(ctx, g, stream) : launch<2, 2>(ctx, g, stream);
+    g.scratch = ctx->lora_scratch;
+    // units that are cut into tiles: adapters (and the rows without one), or requests
+    const bool grouped = B <= kThreads && g.n_adapters < B;
+    const int units = grouped ? g.n_adapters + 1 : B, mean = T_cap / (grouped ? g.n_adapters : B);     // rows of a unit on average, at most
+    return mean <= 16 ? launch<1>(ctx, g, units, stream) : mean <= 64 || g.n_slices * g.rank > DCUT_LORA_MAX_RANKS / 2 ? launch<2>(ctx, g, units, stream) : launch<4>(ctx, g, units, stream);
 }
