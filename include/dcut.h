@@ -701,7 +701,7 @@ dcut_status dcut_verify_step_host(dcut_ctx* ctx, const dcut_host_step* step, voi
  * dcut_prefix_attn met groups that do not cover the batch, a prefix or own positions that do not fit (nothing was written;
  * 7 there: a cu_q that does not pack the batch), 10 = dcut_linear, dcut_linear8, dcut_rope_append,
  * dcut_rms_norm or dcut_lora met a cu_q[B] above T_cap (rows from T_cap on were left out), 11 = dcut_lora met an adapter >= n_adapters
- * (the request counts as one without). */
+ * (the request counts as one without), 12 = a bounded wait in dcut_lora gave up. */
 dcut_status dcut_poll_device_status(dcut_ctx* ctx, int* code, void* stream);
 
 #ifdef __cplusplus

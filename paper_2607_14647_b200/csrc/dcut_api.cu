@@ -161,6 +161,12 @@ dcut_status dcut_create(dcut_ctx** out, const dcut_limits* lim, int device) {
     if ((st = dmalloc(c, &c->d_bucket_K, DCUT_MAX_BUCKETS, "cudaMalloc(bucket_K)")) != DCUT_OK) return st;
     if ((st = dmalloc(c, &c->d_row_key, max_T, "cudaMalloc(row_key)")) != DCUT_OK) return st;
     if ((st = dmalloc(c, &c->d_status, 4, "cudaMalloc(status)")) != DCUT_OK) return st;
+    {   // the tensor-map encoder
+        cudaDriverEntryPointQueryResult found;
+        const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &c->encode_tiled, cudaEnableDefault, &found);
+        if (e != cudaSuccess || found != cudaDriverEntryPointSuccess || !c->encode_tiled)
+            return dcut_fail(c, DCUT_ECUDA, "cuTensorMapEncodeTiled entry point not available");
+    }
     if (lim->vocab > 0) {   // rejection-sampling acceptance: per-row softmax statistics of vocabulary segments of ~8k tokens
         c->rs_n_seg = (lim->vocab + 8191) / 8192;
         if (c->rs_n_seg > 32) c->rs_n_seg = 32;
@@ -696,6 +702,7 @@ dcut_status dcut_lora(dcut_ctx* c, const dcut_lora_args* l, const int* cu_q, int
         if (l->slice_end[i] <= (i ? l->slice_end[i - 1] : 0)) return dcut_fail(c, DCUT_EINVAL, "slice_end must ascend from above 0");
     const int N = l->slice_end[l->n_slices - 1];
     if (N > (1 << 21) || T_cap > (1 << 21) || l->K > (1 << 30) || B > (1 << 20)) return dcut_fail(c, DCUT_ECAPACITY, "N and T_cap go up to 2^21, K to 2^30, B to 2^20");
+    if (l->n_adapters > (1 << 22)) return dcut_fail(c, DCUT_ECAPACITY, "n_adapters goes up to 2^22");
     if (l->act < DCUT_ACT_NONE || l->act > DCUT_ACT_SILU) return dcut_fail(c, DCUT_EINVAL, "unknown activation %d", l->act);
     if (l->gated && (N % 2 || l->n_slices > 2 || (l->n_slices == 2 && l->slice_end[0] != N / 2)))
         return dcut_fail(c, DCUT_EINVAL, "gated: an even N in one slice or two halves");

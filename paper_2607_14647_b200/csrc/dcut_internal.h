@@ -23,6 +23,7 @@
 #define DCUT_DEV_BAD_APPEND 8           // dcut_rope_append: a token's request, group or position has no place in the block table
 #define DCUT_DEV_BAD_ROWS 10            // dcut_linear(8), dcut_rope_append, dcut_rms_norm, dcut_lora: cu_q[B] above T_cap
 #define DCUT_DEV_BAD_ADAPTER 11        // dcut_lora: an adapter that does not exist
+#define DCUT_DEV_LORA_WAIT_TIMEOUT 12  // a bounded mbarrier wait in dcut_lora gave up
 #define DCUT_DEV_BAD_GROUPS 9           // dcut_prefix_attn: the groups do not cover the batch, a prefix does not fit its table or contexts, or own positions their row of the block table
 
 // One row of the attention work table: a (request, row block of its query tile); it stands for n_kv_heads work items of

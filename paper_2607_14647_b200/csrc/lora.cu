@@ -4,8 +4,7 @@
 //   out = act(base + d), or act(base_gate + d_gate) * (base_up + d_up)
 //
 // Two products with a rank between them; each byte of x, base and out moves once, A and B of an adapter once per tile of rows (from
-// L2 but for the first).  A few multiplications per byte: the memory, and for few rows its latency, bounds it, so both products run on
-// warp-level MMAs.  A tile is up to 16, 32 or 64 rows that share an adapter (of several requests, where those share it).
+// L2 but for the first).  A few multiplications per byte: the memory, and for few rows its latency, bounds it.  A tile is up to 16, 32 or 64 rows that share an adapter (of several requests, where those share it).
 //   lora_low_kernel   s of a tile, by 1 to 8 CTAs (a cluster) that cut K between them: x and A come through asynchronous copies, several steps
 //                     ahead; the partial sums meet through distributed shared memory, added in a fixed order.  s is scaled in fp32 and kept as
 //                     the sum of two bf16 values (off by 2^-17 of it at most; a single one cost the result up to 1.7 times its error where
@@ -18,6 +17,7 @@
 
 #include "activation.cuh"
 #include "dcut_internal.h"
+#include "tcgen05.cuh"
 
 namespace {
 
@@ -35,37 +35,17 @@ struct LoraArgs {
     int in_place;                        // rows without an adapter keep what they have
     int vec;                             // base and out take 16-byte accesses at columns that are multiples of 8
     int end[kMaxSlices];                 // last column + 1 of each slice
-    int wn;                              // first product: warps side by side over the columns of s; the others of a row block split K
     int part_row;                        // floats from a row of s to the next in the partial sums
+    int tile_rows;                       // rows of a tile: 16, 32 or 64
     int tile0, blocks;                   // first tile of this pass; CTAs of the second product per tile
     unsigned char* scratch;              // per tile: a Tile, then its s
     long long tile_bytes;
     int* status;
 };
 
-__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
 __device__ __forceinline__ uint32_t cluster_size() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -79,11 +59,6 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from, int bytes)
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }       // ends a group of copies
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }   // all but the last N groups
-__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ uint32_t shared_at(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-
 // what bf16 rounding took from two values (nothing from an infinity): `high` is their packed rounding
 __device__ __forceinline__ uint32_t low_parts(float x, float y, uint32_t high) {
     const float hx = bf_lo(high), hy = bf_hi(high);
@@ -108,7 +83,7 @@ __device__ __forceinline__ uint4 load_some(const __nv_bfloat16* p, int n) {
 // What a cluster works on: up to R rows of one adapter (of several requests, where they share it).
 struct Tile {
     int rows, adapter;                   // rows = 0: there is no such tile
-    int row[64];
+    int row[64];                         // (kMostRows)
     int pad[14];
 };
 static_assert(sizeof(Tile) % 64 == 0, "s follows in 16-byte pieces");
@@ -223,7 +198,7 @@ struct Low {
 };
 
 constexpr int kChunk = 64;               // elements of K per step of the first product: rows of 128 bytes, 16-byte piece c of row r at c ^ (r & 7)
-constexpr int kRowBytes = 2 * kChunk, kPieces = kRowBytes / 16, kStrideRows = kThreads / kPieces;
+constexpr int kRowBytes = 2 * kChunk, kPieces = kRowBytes / 16, kCopiers = 128, kStrideRows = kCopiers / kPieces, kMostRows = 64;
 constexpr int kEdgeRow = 80;             // bytes of a row of a group's results on their way to rows that take no vectors
 
 // act(v), in place.  The common ones stand here: a call's cost is that of the registers that live across it.
@@ -245,121 +220,144 @@ __device__ __forceinline__ void activate(int act, float (&v)[N]) {
     }
 }
 
-// s of a tile of 16 MT rows.  A warp has 16 rows and up to 8 NT columns; STAGES - 1 steps of K are on their way.
-template <int MT, int NT, int STAGES>
-__global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g) {
-    constexpr int R = 16 * MT, kSet = kWarps / MT;                     // kSet: warps that share 16 rows
-    extern __shared__ __align__(128) unsigned char smem[];
+// s of a tile of R rows: one accumulator of 128 x (columns of s) in tensor memory, of which R rows are used (tcgen05.mma has M = 128; what its other rows
+// read is whatever follows the tile of x in shared memory, and nobody looks at them).  STAGES - 1 steps of K are on their way.
+template <int STAGES>
+__global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g, const __grid_constant__ CUtensorMap a_map) {
+    extern __shared__ unsigned char smem_raw[];
     __shared__ Tile tile;
     __shared__ Search search;
+    __shared__ unsigned long long bars[2 * STAGES + 1];                // a step has arrived; its products have been formed, its place is free; all are formed
+    __shared__ uint32_t tmem_slot;
+    const int R = g.tile_rows, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(smem_u32(bars + s), 1 + kCopiers);               // A's bytes, and the threads that copy x
+            mbar_init(smem_u32(bars + STAGES + s), 1);
+        }
+        mbar_init(smem_u32(bars + 2 * STAGES), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     dcut_pdl_wait();
     dcut_pdl_launch_dependents();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gr = lane >> 2, q = lane & 3;
-    const int rank = (int)cluster_rank(), split = (int)cluster_size(), SR = g.n_slices * g.rank, number = blockIdx.x / split;
+    const int rank = (int)cluster_ctarank(), split = (int)cluster_size(), SR = g.n_slices * g.rank, number = blockIdx.x / split;
     find_tile(g, g.tile0 + number, R, tile, search);
     const int rows = tile.rows, adapter = tile.adapter;
     unsigned char* record = g.scratch + number * g.tile_bytes;
     if (rank == 0 && threadIdx.x < 2 + rows) reinterpret_cast<int*>(record)[threadIdx.x] = reinterpret_cast<const int*>(&tile)[threadIdx.x];
     if (rows == 0 || adapter < 0) return;                              // (the whole cluster)
-    float* sums = reinterpret_cast<float*>(smem);                      // in the ring's place, later: [K split of the warps][R][part_row]; the total in the first
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    float* sums = reinterpret_cast<float*>(smem);                      // in the ring's place, later: [R][part_row]
 
     const int chunks = (g.K + kChunk - 1) / kChunk, c0 = (int)((long long)chunks * rank / split), n_chunks = (int)((long long)chunks * (rank + 1) / split) - c0;
-    const int stage = (R + SR) * kRowBytes;
-    // a thread copies the same 16-byte piece of every 32nd row: of x (zeros where there is no row), then of A
-    const int piece = threadIdx.x % kPieces, r0 = threadIdx.x / kPieces;
-    const uint32_t ring_at = shared_at(smem), to0 = ring_at + r0 * kRowBytes + ((piece ^ (r0 & 7)) << 4);
-    constexpr int kX = (R + kStrideRows - 1) / kStrideRows;
-    const __nv_bfloat16* x_from[kX];                                   // (these two move along K with the steps that are asked for)
+    const int stage = (R + SR) * kRowBytes;                            // (a multiple of 1024, as the swizzle wants: R of 16, SR of 8)
+    const uint32_t ring_at = smem_u32(smem), full = smem_u32(bars), empty = smem_u32(bars + STAGES), done = smem_u32(bars + 2 * STAGES);
+    const int n = (SR + 15) & ~15;                                     // the MMA's N; 8 columns beyond SR read what follows A
+    const uint32_t columns = n <= 32 ? 32u : n <= 64 ? 64u : n <= 128 ? 128u : 256u;
+    bool failed = false;
+    if (warp == 1) {
+        // ---- A, by TMA (zeros behind K)
+        for (int c = 0, slot = 0; c < n_chunks; ++c) {
+            if (c >= STAGES && !__all_sync(0xffffffffu, mbar_wait(empty + 8 * slot, (c / STAGES - 1) & 1))) {
+                failed = true;
+                break;
+            }
+            if (elect_one()) {
+                mbar_arrive_expect_tx(full + 8 * slot, SR * kRowBytes);
+                tma_load_2d(ring_at + slot * stage + R * kRowBytes, &a_map, (c0 + c) * kChunk, adapter * SR, full + 8 * slot);
+            }
+            __syncwarp();
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+        }
+    } else if (warp >= kWarps - kCopiers / 32) {
+        // ---- x, whose rows lie anywhere: a thread copies the same 16-byte piece of every 16th row
+        const int t = threadIdx.x - (kThreads - kCopiers), piece = t % kPieces, r0 = t / kPieces;
+        const uint32_t to0 = ring_at + r0 * kRowBytes + ((piece ^ (r0 & 7)) << 4);
+        const __nv_bfloat16* from[kMostRows / kStrideRows];
 #pragma unroll
-    for (int i = 0; i < kX; ++i) x_from[i] = g.x + (size_t)tile.row[min(r0 + kStrideRows * i, rows - 1)] * g.ldx + (size_t)c0 * kChunk + 8 * piece;
-    const __nv_bfloat16* a_from = g.a + ((size_t)adapter * SR + r0) * g.lda + (size_t)c0 * kChunk + 8 * piece;
-    const long long a_step = kStrideRows * g.lda;
-    int left = 2 * (g.K - c0 * kChunk - 8 * piece), asked = 0;         // bytes from this thread's next piece to the end of its rows; steps asked for
-    auto load = [&](int slot) {
-        if (asked < n_chunks) {
-            const uint32_t to = to0 + slot * stage;
+        for (int i = 0; i < kMostRows / kStrideRows; ++i)
+            from[i] = g.x + (size_t)tile.row[min(r0 + kStrideRows * i, rows - 1)] * g.ldx + (size_t)c0 * kChunk + 8 * piece;
+        int left = 2 * (g.K - c0 * kChunk - 8 * piece);                // bytes from this thread's piece to the end of its rows
+        for (int c = 0, slot = 0; c < n_chunks; ++c) {
+            if (c >= STAGES && !mbar_wait(empty + 8 * slot, (c / STAGES - 1) & 1)) {
+                failed = true;
+                break;
+            }
             const int bytes = min(16, max(0, left));                   // (0: nothing is read, and the address is one that exists)
 #pragma unroll
-            for (int i = 0; i < kX; ++i)
-                if (R % kStrideRows == 0 || r0 + kStrideRows * i < R)
-                    copy16(to + i * kStrideRows * kRowBytes, bytes ? x_from[i] : g.x, r0 + kStrideRows * i < rows ? bytes : 0), x_from[i] += kChunk;
-            const __nv_bfloat16* from = bytes ? a_from : g.a;
-            const long long step = bytes ? a_step : 0;
-            uint32_t to_a = to + R * kRowBytes;
-#pragma unroll 4
-            for (int r = r0; r < SR; r += kStrideRows, to_a += kStrideRows * kRowBytes, from += step) copy16(to_a, from, bytes);
-            a_from += kChunk, left -= kRowBytes, ++asked;
-        }
-        copies_done();
-    };
-    const int wn = min(g.wn, kSet), wk = kSet / wn, m = warp / kSet, in_set = warp % kSet, my_n = in_set % wn, my_k = in_set / wn;
-    const int tiles = SR / 8, per = (tiles + wn - 1) / wn, t0 = my_n * per, nt = min(per, tiles - t0);         // this warp's 8-column tiles of s
-    // this lane's rows for ldmatrix: where they begin in a step, and the swizzle with the half of 16 elements that the lane points to
-    const int x_row = 16 * m + (lane & 15), x_at = x_row * kRowBytes, x_flip = ((x_row & 7) ^ (lane >> 4)) << 4;
-    const int a_flip = ((lane & 7) ^ ((lane >> 3) & 1)) << 4;          // (R and the tiles' first rows are multiples of 8)
-    int a_at[(NT + 1) / 2];                                            // (a tile that does not exist: the last one that does)
-#pragma unroll
-    for (int n = 0; n < NT; n += 2) a_at[n / 2] = (R + 8 * min(t0 + n + (lane >> 4), tiles - 1) + (lane & 7)) * kRowBytes;
-    float acc[NT][4];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < STAGES - 1; ++c) load(c);
-    for (int c = 0, slot = 0, ahead = STAGES - 1; c < n_chunks; ++c) {
-        copies_wait<STAGES - 2>();
-        __syncthreads();                                               // step c has arrived, step c - 1 has been read
-        load(ahead);
-        const uint32_t at = ring_at + slot * stage;
-        auto multiply = [&](int k) {                                   // 16 elements of K
-            uint32_t xf[4];
-            ldmatrix4(xf, at + x_at + ((32 * k) ^ x_flip));
-#pragma unroll
-            for (int n = 0; n < NT; n += 2) {
-                if (n >= nt) break;
-                uint32_t af[4];                                        // two tiles' fragments
-                ldmatrix4(af, at + a_at[n / 2] + ((32 * k) ^ a_flip));
-                mma16816(acc[n], xf[0], xf[1], xf[2], xf[3], af[0], af[1]);
-                if (n + 1 < nt) mma16816(acc[n + 1], xf[0], xf[1], xf[2], xf[3], af[2], af[3]);
+            for (int i = 0; i < kMostRows / kStrideRows; ++i) {
+                if (r0 + kStrideRows * i < rows) copy16(to0 + slot * stage + i * kStrideRows * kRowBytes, bytes ? from[i] : g.x, bytes);
+                from[i] += kChunk;
             }
-        };
-        if (wk == 1) {
-#pragma unroll
-            for (int k = 0; k < kChunk / 16; ++k) multiply(k);
-        } else {                                                       // the warps of a set take turns
-            for (int k = (my_k - c * (kChunk / 16)) & (wk - 1); k < kChunk / 16; k += wk) multiply(k);
+            asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full + 8 * slot) : "memory");
+            left -= kRowBytes;
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
         }
-        slot = slot + 1 == STAGES ? 0 : slot + 1;
-        ahead = ahead + 1 == STAGES ? 0 : ahead + 1;
+    } else if (warp == 0) {
+        // ---- the products (every earlier kernel has ended: whoever held tensor memory on this SM has given it back, or belongs to another stream
+        // and will)
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot), idesc = idesc_no_n<false>(128) | ((uint32_t)(n >> 3) << 17);
+        for (int c = 0, slot = 0; c < n_chunks; ++c) {
+            if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * slot, (c / STAGES) & 1))) {
+                failed = true;
+                break;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the copies of x, for the tensor core
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t at = ring_at + slot * stage;
+                const uint64_t dx = umma_desc_sw128(at), da = umma_desc_sw128(at + R * kRowBytes);
+#pragma unroll
+                for (int k = 0; k < kChunk / 16; ++k) tc_mma<false>(tmem, dx + 2 * k, da + 2 * k, idesc, (c | k) ? 1u : 0u);
+                tc_commit(empty + 8 * slot);
+                if (c == n_chunks - 1) tc_commit(done);
+            }
+            __syncwarp();
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+        }
     }
+    if (n_chunks > 0 && !failed && !mbar_wait(done, 0)) failed = true;
+    copies_done();
     copies_wait<0>();
-    __syncthreads();                                                   // the ring is free
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        if (n >= nt) break;
-        float* p = sums + (my_k * R + 16 * m + gr) * g.part_row + 8 * (t0 + n) + 2 * q;
-        *reinterpret_cast<float2*>(p) = make_float2(acc[n][0], acc[n][1]);
-        *reinterpret_cast<float2*>(p + 8 * g.part_row) = make_float2(acc[n][2], acc[n][3]);
+    if (failed) {
+        atomicExch(g.status, DCUT_DEV_LORA_WAIT_TIMEOUT);
+        if (warp == 1)                                                 // nothing is on its way to this CTA's memory when it leaves
+            for (int s = 0; s < STAGES; ++s) (void)mbar_wait(full + 8 * s, 0), (void)mbar_wait(full + 8 * s, 1);
     }
-    const int quads = SR / 4;
-    if (wk > 1) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < R * quads; e += kThreads) {
-            const int r = e / quads, c = 4 * (e - r * quads);
-            float* p = sums + r * g.part_row + c;
-            float4 s = *reinterpret_cast<const float4*>(p);
-            for (int w = 1; w < wk; ++w) {
-                const float4 v = *reinterpret_cast<const float4*>(p + w * R * g.part_row);
-                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    tc_fence_before();
+    __syncthreads();                                                   // every product is formed, the ring is free
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    {
+        const int quarter = warp & 3, r = 32 * quarter + lane;         // (a warp reads the 32 lanes of tensor memory that its number gives)
+        if (32 * quarter < R) {
+            for (int col = 8 * (warp >> 2); col < SR; col += 16) {
+                uint32_t v[8];
+                asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                             : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                             : "r"(tmem + ((uint32_t)(32 * quarter) << 16) + col));
+                tc_wait_ld();
+                if (r < R) {
+                    uint4* p = reinterpret_cast<uint4*>(sums + r * g.part_row + col);
+                    p[0] = n_chunks > 0 ? make_uint4(v[0], v[1], v[2], v[3]) : make_uint4(0, 0, 0, 0);      // (no share of K: nothing was written)
+                    p[1] = n_chunks > 0 ? make_uint4(v[4], v[5], v[6], v[7]) : make_uint4(0, 0, 0, 0);
+                }
             }
-            *reinterpret_cast<float4*>(p) = s;
         }
     }
-    cluster_sync();                                                    // every CTA's share is complete
+    tc_fence_before();
+    cluster_sync_all();                                                // every CTA's share is complete
+    if (warp == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+    }
     const float scale = g.scale ? g.scale[adapter] : 1.0f;
-    const uint32_t sums_at = shared_at(sums);
+    const uint32_t sums_at = smem_u32(sums);
     const Low low(g.rank);
     unsigned char* s_out = record + sizeof(Tile);
-    const int each = R * quads / split;                                // (R is a multiple of 16, SR of 8, the split of 8 a divisor)
+    const int blocks16 = R / 16, quads = SR / 4, each = R * quads / split;               // (R is a multiple of 16, SR of 8, the split of 8 a divisor)
     for (int e = rank * each + threadIdx.x; e < (rank + 1) * each; e += kThreads) {
         const int r = e / quads, c = 4 * (e - r * quads), slice = c / g.rank, j = c - slice * g.rank;
         float4 s = make_float4(0, 0, 0, 0), v[kMostSplit];
@@ -367,23 +365,23 @@ __global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g) {
         for (int p = 0; p < kMostSplit; ++p)
             if (p < split)
                 asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[p].x), "=f"(v[p].y), "=f"(v[p].z), "=f"(v[p].w)
-                             : "r"(in_cta(sums_at + 4 * (r * g.part_row + c), p)) : "memory");
+                             : "r"(mapa_rank(sums_at + 4 * (r * g.part_row + c), p)) : "memory");
 #pragma unroll
         for (int p = 0; p < kMostSplit; ++p)
             if (p < split) s.x += v[p].x, s.y += v[p].y, s.z += v[p].z, s.w += v[p].w;
         s.x *= scale, s.y *= scale, s.z *= scale, s.w *= scale;
         const uint32_t hi0 = pack_bf16(s.x, s.y), hi1 = pack_bf16(s.z, s.w);
-        *reinterpret_cast<uint2*>(s_out + low.at(MT, g.rank, slice, r, j, 0)) = make_uint2(hi0, hi1);
-        *reinterpret_cast<uint2*>(s_out + low.at(MT, g.rank, slice, r, j, 1)) = make_uint2(low_parts(s.x, s.y, hi0), low_parts(s.z, s.w, hi1));
+        *reinterpret_cast<uint2*>(s_out + low.at(blocks16, g.rank, slice, r, j, 0)) = make_uint2(hi0, hi1);
+        *reinterpret_cast<uint2*>(s_out + low.at(blocks16, g.rank, slice, r, j, 1)) = make_uint2(low_parts(s.x, s.y, hi0), low_parts(s.z, s.w, hi1));
     }
     if (low.parts == 1 && rank == split - 1) {                         // what fills up the last step
         const int rest = (32 * low.steps - 2 * g.rank) / 4;
         for (int e = threadIdx.x; e < g.n_slices * R * rest; e += kThreads) {
             const int sr = e / rest, v = 2 * g.rank + 4 * (e - sr * rest);
-            *reinterpret_cast<uint2*>(s_out + low.at(MT, g.rank, sr / R, sr % R, v, 0)) = make_uint2(0, 0);
+            *reinterpret_cast<uint2*>(s_out + low.at(blocks16, g.rank, sr / R, sr % R, v, 0)) = make_uint2(0, 0);
         }
     }
-    cluster_sync();                                                    // nobody leaves while its sums are read
+    cluster_sync_all();                                                // nobody leaves while its sums are read
 }
 
 // out of a tile: a warp has 32 columns, 16 rows at a time.  The MMA's column n of tile t is column 8 (n >> 1) + 2 t + (n & 1) of the 32, so that
@@ -392,15 +390,16 @@ __global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g) {
 // `early`: the CTA finds its tile itself and asks for B and its first rows of base while the first product runs (what that one waited for is
 // complete once this grid has started); otherwise it reads the tile from the scratch.
 template <bool GATED, int KEEP>
-__global__ void __launch_bounds__(kThreads, GATED || KEEP > 1 ? 2 : 3) lora_out_kernel(LoraArgs g, int blocks16, int early) {
+__global__ void __launch_bounds__(kThreads, GATED || KEEP > 1 ? 2 : 3) lora_out_kernel(LoraArgs g, int early) {
     constexpr int kParts = GATED ? 2 : 1;
+    const int blocks16 = g.tile_rows / 16;
     __shared__ __align__(16) unsigned char edges[kWarps][16 * kEdgeRow];
     __shared__ Tile tile;
     __shared__ Search search;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gr = lane >> 2, q = lane & 3;
     const int number = blockIdx.x / g.blocks;
     const unsigned char* record = g.scratch + number * g.tile_bytes;
-    if (early) find_tile(g, g.tile0 + number, 16 * blocks16, tile, search);
+    if (early) find_tile(g, g.tile0 + number, g.tile_rows, tile, search);
     else {
         dcut_pdl_wait();
         if (threadIdx.x < 66) reinterpret_cast<int*>(&tile)[threadIdx.x] = reinterpret_cast<const int*>(record)[threadIdx.x];
@@ -519,10 +518,13 @@ __global__ void __launch_bounds__(kThreads, GATED || KEEP > 1 ? 2 : 3) lora_out_
     }
 }
 
-constexpr int kMostShared = 110 * 1024;                                 // two CTAs of the first product per SM
+// Two CTAs of the first product per SM, and never three: CTAs of several streams' launches may meet on an SM, and three could want more tensor memory
+// than it has (256 columns at most each).  One would wait for another's, whose cluster might wait for the first one's.  The library's other kernels that
+// hold tensor memory leave no room beside them.
+constexpr int kMostShared = 110 * 1024, kLeastShared = 77 * 1024;
 
-template <int MT, int NT, int STAGES>
-dcut_status launch_low(dcut_ctx* ctx, const LoraArgs& g, int grid, int split, size_t smem, cudaStream_t stream) {
+template <int STAGES>
+dcut_status launch_low(dcut_ctx* ctx, const LoraArgs& g, const CUtensorMap& a_map, int grid, int split, size_t smem, cudaStream_t stream) {
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = split;
@@ -537,31 +539,18 @@ dcut_status launch_low(dcut_ctx* ctx, const LoraArgs& g, int grid, int split, si
     lc.stream = stream;
     lc.attrs = attr;
     lc.numAttrs = 2;
-    return dcut_check_cuda(ctx, cudaLaunchKernelEx(&lc, lora_low_kernel<MT, NT, STAGES>, g), "launch lora_low_kernel");
+    return dcut_check_cuda(ctx, cudaLaunchKernelEx(&lc, lora_low_kernel<STAGES>, g, a_map), "launch lora_low_kernel");
 }
-// How the first product of a launch runs
-struct Plan {
-    int wn, stages;
-    size_t smem;
-};
-template <int MT>
-Plan plan_low(int SR) {
-    constexpr int R = 16 * MT, kSet = kWarps / MT;
-    Plan p;
-    for (p.wn = 1; p.wn < kSet && (SR / 8 + p.wn - 1) / p.wn > 4;) p.wn *= 2;             // up to 4 tiles of s per warp, where there are warps for it
-    const int stage = (R + SR) * kRowBytes, sums = kSet / p.wn * R * (SR + 8) * 4;
-    p.stages = 8 * stage <= kMostShared ? 8 : 4 * stage <= kMostShared ? 4 : 2;
-    p.smem = p.stages * stage > sums ? p.stages * stage : sums;
-    return p;
-}
-template <int MT>
-dcut_status launch(dcut_ctx* ctx, LoraArgs& g, int units, cudaStream_t stream) {
-    constexpr int R = 16 * MT, NT = 8;
-    const int SR = g.n_slices * g.rank;
-    const Plan p = plan_low<MT>(SR);
-    g.wn = p.wn;
+dcut_status launch(dcut_ctx* ctx, LoraArgs& g, const CUtensorMap& a_map, int R, int units, cudaStream_t stream) {
+    const int SR = g.n_slices * g.rank, stage = (R + SR) * kRowBytes, sums = R * (SR + 8) * 4;
+    // behind the last step: 128 rows from the beginning of its x on, 8 more rows of A; and the alignment
+    const int slack = (stage < 128 * kRowBytes ? 128 * kRowBytes - stage : 0) + 1024 + 1024;
+    const int stages = 8 * stage + slack <= kMostShared ? 8 : 4 * stage + slack <= kMostShared ? 4 : 2;
+    const int need = (stages * stage > sums ? stages * stage : sums) + slack;
+    const size_t smem = need > kLeastShared ? need : kLeastShared;
+    g.tile_rows = R;
     g.part_row = SR + 8;
-    g.tile_bytes = (long long)sizeof(Tile) + (long long)g.n_slices * MT * Low(g.rank).pieces() * 512;
+    g.tile_bytes = (long long)sizeof(Tile) + (long long)g.n_slices * (R / 16) * Low(g.rank).pieces() * 512;
     int groups = 0;
     for (int s = 0, lo = 0; s < (g.gated ? 1 : g.n_slices); ++s) {
         const int end = g.gated ? g.N / 2 : g.end[s];
@@ -571,41 +560,33 @@ dcut_status launch(dcut_ctx* ctx, LoraArgs& g, int units, cudaStream_t stream) {
     g.blocks = (groups + kWarps - 1) / kWarps;
     // the sum of ceil(rows / R) over the units that are cut into tiles, at most; as many of them at a time as the scratch holds
     const long long tiles = ((long long)g.T_cap + (long long)units * (R - 1)) / R, room = DCUT_LORA_SCRATCH / g.tile_bytes;
+    const int steps = Low(g.rank).steps;
+    auto* out = g.gated ? (steps == 1 ? lora_out_kernel<true, 1> : lora_out_kernel<true, 0>)
+                        : (steps == 1 ? lora_out_kernel<false, 1> : steps == 2 ? lora_out_kernel<false, 2> : lora_out_kernel<false, 0>);
     for (long long t = 0; t < tiles; t += room) {
         const int n = (int)(tiles - t < room ? tiles - t : room);
         g.tile0 = (int)t;
         int split = kMostSplit;                                         // CTAs per tile: one wave of two per SM, where there are tiles for it
         while (split > 1 && (long long)n * split > 2 * ctx->sm_count) split >>= 1;
-        dcut_status st = p.stages == 8   ? launch_low<MT, NT, 8>(ctx, g, n * split, split, p.smem, stream)
-                         : p.stages == 4 ? launch_low<MT, NT, 4>(ctx, g, n * split, split, p.smem, stream)
-                                         : launch_low<MT, NT, 2>(ctx, g, n * split, split, p.smem, stream);
+        dcut_status st = stages == 8   ? launch_low<8>(ctx, g, a_map, n * split, split, smem, stream)
+                         : stages == 4 ? launch_low<4>(ctx, g, a_map, n * split, split, smem, stream)
+                                       : launch_low<2>(ctx, g, a_map, n * split, split, smem, stream);
         if (st != DCUT_OK) return st;
-        const int steps = Low(g.rank).steps;
-        auto* out = g.gated ? (steps == 1 ? lora_out_kernel<true, 1> : lora_out_kernel<true, 0>)
-                            : (steps == 1 ? lora_out_kernel<false, 1> : steps == 2 ? lora_out_kernel<false, 2> : lora_out_kernel<false, 0>);
-        const long long ctas = (long long)n * g.blocks;
-        const int early = ctas <= 2 * ctx->sm_count;                     // all of them can wait beside the first product
-        st = dcut_check_cuda(ctx, dcut_launch_pdl(out, dim3((unsigned)ctas), dim3(kThreads), 0, stream, g, MT, early), "launch lora_out_kernel");
+        const int early = n * split <= ctx->sm_count;                    // there is room for this kernel's CTAs beside the first one's
+        st = dcut_check_cuda(ctx, dcut_launch_pdl(out, dim3((unsigned)(n * g.blocks)), dim3(kThreads), 0, stream, g, early), "launch lora_out_kernel");
         if (st != DCUT_OK) return st;
     }
     return DCUT_OK;
-}
-template <int MT>
-cudaError_t allow() {
-    constexpr int R = 16 * MT, M = MT > 2 ? DCUT_LORA_MAX_RANKS / 2 : DCUT_LORA_MAX_RANKS, NT = 8;
-    static_assert(2 * (R + M) * kRowBytes <= kMostShared && R * (M + 8) * 4 <= kMostShared && 2 * R * (M / 2 + 8) * 4 <= kMostShared, "two steps and the sums fit");
-    static_assert(M / 8 <= NT * (kWarps / MT), "a warp's tiles of s");
-    cudaError_t e = cudaFuncSetAttribute(lora_low_kernel<MT, NT, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_low_kernel<MT, NT, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
-    return e == cudaSuccess ? cudaFuncSetAttribute(lora_low_kernel<MT, NT, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared) : e;
 }
 
 }  // namespace
 
 dcut_status dcut_init_lora(dcut_ctx* ctx) {
-    cudaError_t e = allow<1>();
-    if (e == cudaSuccess) e = allow<2>();
-    if (e == cudaSuccess) e = allow<4>();
+    constexpr int M = DCUT_LORA_MAX_RANKS;
+    static_assert(2 * (64 + M) * kRowBytes + 2048 <= kMostShared && 64 * (M + 8) * 4 + 2048 <= kMostShared, "two steps and the sums fit");
+    cudaError_t e = cudaFuncSetAttribute(lora_low_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_low_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_low_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     return dcut_check_cuda(ctx, e, "cudaFuncSetAttribute(lora)");
 }
 
@@ -630,5 +611,13 @@ dcut_status dcut_launch_lora(dcut_ctx* ctx, const dcut_lora_args* l, const int* 
     // units that are cut into tiles: adapters (and the rows without one), or requests
     const bool grouped = B <= kThreads && g.n_adapters < B;
     const int units = grouped ? g.n_adapters + 1 : B, mean = T_cap / (grouped ? g.n_adapters : B);     // rows of a unit on average, at most
-    return mean <= 16 ? launch<1>(ctx, g, units, stream) : mean <= 64 || g.n_slices * g.rank > DCUT_LORA_MAX_RANKS / 2 ? launch<2>(ctx, g, units, stream) : launch<4>(ctx, g, units, stream);
+    // A as a matrix of all the adapters' rows; a step takes 64 columns of one adapter's
+    const cuuint64_t dims[2] = {(cuuint64_t)g.K, (cuuint64_t)g.n_adapters * g.n_slices * g.rank}, strides[1] = {(cuuint64_t)g.lda * 2};
+    const cuuint32_t box[2] = {kChunk, (cuuint32_t)(g.n_slices * g.rank)}, ones[2] = {1, 1};
+    CUtensorMap a_map;
+    const CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->encode_tiled)(&a_map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(l->a), dims, strides, box, ones,
+                                                                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return dcut_fail(ctx, DCUT_ECUDA, "cuTensorMapEncodeTiled failed for the adapters (%d)", (int)r);
+    return launch(ctx, g, a_map, mean <= 16 ? 16 : mean <= 64 ? 32 : 64, units, stream);
 }

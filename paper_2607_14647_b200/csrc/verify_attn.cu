@@ -1861,12 +1861,6 @@ dcut_status dcut_init_verify_attn(dcut_ctx* ctx) {
     }
     e = cudaFuncSetAttribute(attn_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * (2 * DCUT_MAX_KEYS + 1) + 4 * (2 * DCUT_MAX_KEYS + 1));
     if (e != cudaSuccess) return dcut_check_cuda(ctx, e, "cudaFuncSetAttribute(attn plan)");
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
-    if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn)
-        return dcut_fail(ctx, DCUT_ECUDA, "cuTensorMapEncodeTiled entry point not available");
-    ctx->encode_tiled = fn;
     return DCUT_OK;
 }
 
