@@ -37,7 +37,7 @@ struct LoraArgs {
     int end[kMaxSlices];                 // last column + 1 of each slice
     int part_row;                        // floats from a row of s to the next in the partial sums
     int tile_rows;                       // rows of a tile: 16, 32 or 64
-    int tile0, blocks;                   // first tile of this pass; CTAs of the second product per tile
+    int tile0, groups, blocks;           // first tile of this pass; groups of columns, and CTAs of the second product, per tile
     unsigned char* scratch;              // per tile: a Tile, then its s
     long long tile_bytes;
     int* status;
@@ -165,23 +165,21 @@ __device__ __forceinline__ void find_tile(const LoraArgs& g, int t, int R, Tile&
     __syncthreads();
 }
 
-// The columns of out that a warp works on at a time: 32 of one slice (gated: of the gate, with the same ones of the up projection).
+// The columns of out that a warp works on at a time: 32 of one slice, or, gated, 16 of the gate and the same ones of the up projection.
 struct Group {
     int col, end, slice;                 // first column; where the slice ends
 };
-__device__ __forceinline__ Group group_of(const LoraArgs& g, int i, bool gated) {
-    int first = 0, end = gated ? g.N / 2 : g.end[0], slice = 0;
-    if (!gated)
-        while (i >= (end - first + 31) / 32) {
-            i -= (end - first + 31) / 32;
-            first = end;
-            end = g.end[++slice];
-        }
+template <bool GATED>
+__device__ __forceinline__ Group group_of(const LoraArgs& g, int i) {
+    if (GATED) return Group{16 * i, g.N / 2, 0};
+    int first = 0, end = g.end[0], slice = 0;
+    while (i >= (end - first + 31) / 32) {
+        i -= (end - first + 31) / 32;
+        first = end;
+        end = g.end[++slice];
+    }
     return Group{first + 32 * i, end, slice};
 }
-
-// whether the group at column `col` is read and written in 16-byte pieces (the same answer in the whole warp)
-__device__ __forceinline__ bool by_vector(const LoraArgs& g, int col, int end) { return g.vec && !(col & 7) && col + 32 <= end; }
 
 // How s lies in the scratch.  A step of the second product is 32 elements, 8 in a lane.  Ranks that are multiples of 32 take a step with the high
 // parts and again with the low ones (parts = 2); others walk the high parts and then the low ones as one row, so that rank 16 fills a step.
@@ -384,14 +382,15 @@ __global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g, const
     cluster_sync_all();                                                // nobody leaves while its sums are read
 }
 
-// out of a tile: a warp has 32 columns, 16 rows at a time.  The MMA's column n of tile t is column 8 (n >> 1) + 2 t + (n & 1) of the 32, so that
-// a lane ends with the 8 neighbouring columns 8 q .. + 7; its 8 neighbouring elements of s and of B serve as its fragments of two MMAs
-// (the order of a sum's terms is free).  KEEP: the rank's steps, where B's fragments stay in registers for all rows; 0: they are read again.
+// out of a tile: a warp has a group of columns, 16 rows at a time.  Column n of the MMA's tile t is column 8 (n >> 1) + 2 t + (n & 1) of the
+// 32, so that a lane ends with the 8 neighbouring columns 8 q .. + 7 (gated: t = 0, 1 the gate's and t = 2, 3 the up projection's columns 4 (n >> 1) +
+// 2 (t & 1) + (n & 1), 4 q .. + 3 of each); a lane's 8 neighbouring elements of s and of B serve as its fragments of two MMAs (the order of a
+// sum's terms is free).  KEEP: the rank's steps, where B's fragments stay in registers for all rows; 0: they are read again for every 16.
 // `early`: the CTA finds its tile itself and asks for B and its first rows of base while the first product runs (what that one waited for is
 // complete once this grid has started); otherwise it reads the tile from the scratch.
 template <bool GATED, int KEEP>
-__global__ void __launch_bounds__(kThreads, GATED || KEEP > 1 ? 2 : 3) lora_out_kernel(LoraArgs g, int early) {
-    constexpr int kParts = GATED ? 2 : 1;
+__global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(LoraArgs g, int early) {
+    constexpr int kCols = GATED ? 16 : 32, kPer = kCols / 4;           // columns of a group, of a lane
     const int blocks16 = g.tile_rows / 16;
     __shared__ __align__(16) unsigned char edges[kWarps][16 * kEdgeRow];
     __shared__ Tile tile;
@@ -402,114 +401,124 @@ __global__ void __launch_bounds__(kThreads, GATED || KEEP > 1 ? 2 : 3) lora_out_
     if (early) find_tile(g, g.tile0 + number, g.tile_rows, tile, search);
     else {
         dcut_pdl_wait();
-        if (threadIdx.x < 66) reinterpret_cast<int*>(&tile)[threadIdx.x] = reinterpret_cast<const int*>(record)[threadIdx.x];
+        if (threadIdx.x < 2 + kMostRows) reinterpret_cast<int*>(&tile)[threadIdx.x] = reinterpret_cast<const int*>(record)[threadIdx.x];
         __syncthreads();
     }
-    const int rows = tile.rows, adapter = tile.adapter;
-    const int width = GATED ? g.N / 2 : g.N;                           // columns of out
-    int groups = 0;
-    if (GATED) groups = (width + 31) / 32;
-    else
-        for (int s = 0, lo = 0; s < g.n_slices; ++s) {
-            groups += (g.end[s] - lo + 31) / 32;
-            lo = g.end[s];
-        }
+    const int rows = tile.rows, adapter = tile.adapter, width = GATED ? g.N / 2 : g.N;       // columns of out
     const int i = (blockIdx.x - number * g.blocks) * kWarps + warp;
-    const bool work = rows > 0 && i < groups, live = work && adapter >= 0;
-    const Group at = group_of(g, work ? i : 0, GATED);
+    const bool work = rows > 0 && i < g.groups, live = work && adapter >= 0;
+    const Group at = group_of<GATED>(g, work ? i : 0);
     const Low low(g.rank);
-    const bool vec = by_vector(g, at.col, at.end), vec_up = GATED && by_vector(g, width + at.col, g.N);
-    // B: rows b_row + 2 t of a part's columns; elements from this lane's first one of a step on (behind both parts s is zero, and so is this)
-    const int b_row = 8 * (gr >> 1) + (gr & 1);
-    const __nv_bfloat16* b = g.b + ((size_t)max(adapter, 0) * g.N + at.col + b_row) * g.rank;
-    const int left = at.end - at.col - b_row, left_up = g.N - width - at.col - b_row;
-    auto load_b = [&](int part, int step, uint4 (&bv)[4]) {
+    // base and out in 8- or 16-byte pieces (the same answer in the whole warp)
+    const bool vec = g.vec && at.col + kCols <= at.end && !((at.col | (GATED ? width : 0)) & (kPer - 1));
+    const int left = at.end - at.col;
+    const __nv_bfloat16* b = g.b + ((size_t)max(adapter, 0) * g.N + at.col) * g.rank;
+    auto load_b = [&](int step, uint4 (&bv)[4]) {                      // (behind both parts s is zero, and so is this)
         const int v = 32 * step + 8 * q, k = v < g.rank ? v : v - g.rank;
-        const __nv_bfloat16* p = b + (part ? (size_t)width * g.rank : 0) + k;
 #pragma unroll
-        for (int t = 0; t < 4; ++t, p += 2 * g.rank) bv[t] = load_if(p, 2 * t < (part ? left_up : left) && v < 2 * g.rank);
+        for (int t = 0; t < 4; ++t) {
+            const int n = kPer * (gr >> 1) + 2 * (GATED ? t & 1 : t) + (gr & 1);
+            bv[t] = load_if(b + (size_t)(GATED && t >= 2 ? width + n : n) * g.rank + k, n < left && v < 2 * g.rank);
+        }
     };
-    // base at this lane's 8 columns of rows gr and gr + 8 of block m (those that do not exist: of the last one that does)
-    auto fetch = [&](int m, int (&row)[2], uint4 (&v)[kParts][2]) {
+    // base at this lane's columns of rows gr and gr + 8 of block m (those that do not exist: of the last one that does)
+    auto fetch = [&](int m, int (&row)[2], uint4 (&v)[2]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             row[h] = tile.row[min(16 * m + 8 * h + gr, rows - 1)];
-            const __nv_bfloat16* p = g.base + (unsigned long long)(unsigned)row[h] * (unsigned)g.ldbase + at.col + 8 * q;
-            v[0][h] = vec ? *reinterpret_cast<const uint4*>(p) : load_some(p, at.end - at.col - 8 * q);
-            if (GATED) v[kParts - 1][h] = vec_up ? *reinterpret_cast<const uint4*>(p + width) : load_some(p + width, at.end - at.col - 8 * q);
+            const __nv_bfloat16* p = g.base + (unsigned long long)(unsigned)row[h] * (unsigned)g.ldbase + at.col + kPer * q;
+            if (!GATED) {
+                v[h] = vec ? *reinterpret_cast<const uint4*>(p) : load_some(p, left - 8 * q);
+            } else if (vec) {
+                const uint2 x = *reinterpret_cast<const uint2*>(p), y = *reinterpret_cast<const uint2*>(p + width);
+                v[h] = make_uint4(x.x, x.y, y.x, y.y);
+            } else {
+                const uint4 x = load_some(p, min(4, left - 4 * q)), y = load_some(p + width, min(4, left - 4 * q));
+                v[h] = make_uint4(x.x, x.y, y.x, y.y);
+            }
         }
     };
-    uint4 kept[KEEP ? kParts * KEEP : 1][4], base[kParts][2];
+    uint4 kept[KEEP ? KEEP : 1][4], base[2];
     int row[2];
     if (work) fetch(0, row, base);
     if (KEEP && live) {
 #pragma unroll
-        for (int part = 0; part < kParts; ++part)
-#pragma unroll
-            for (int step = 0; step < KEEP; ++step) load_b(part, step, kept[part * KEEP + step]);
+        for (int step = 0; step < KEEP; ++step) load_b(step, kept[step]);
     }
     if (early) dcut_pdl_wait();
     dcut_pdl_launch_dependents();
     if (!work) return;
 
     const uint4* s_in = reinterpret_cast<const uint4*>(record + sizeof(Tile)) + lane;
+    const int slice = at.slice, slice_up = GATED && g.n_slices == 2 ? 1 : slice;
     for (int m = 0; 16 * m < rows; ++m) {
-        float y[2][8];
+        float d[4][4];
 #pragma unroll
-        for (int part = 0; part < kParts; ++part) {
-            float d[4][4];
+        for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.0f;
+        if (live) {
+            const uint4 *s_at = s_in + (slice * blocks16 + m) * low.pieces() * 32, *s_up = s_in + (slice_up * blocks16 + m) * low.pieces() * 32;
+            auto multiply = [&](const uint4 (&bv)[4]) {
+                const uint4 s0 = s_at[0], s1 = s_at[32], u0 = GATED ? s_up[0] : s0, u1 = GATED ? s_up[32] : s1;
+                s_at += 64, s_up += 64;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.0f;
-            if (live) {
-                const uint4* s_at = s_in + ((GATED ? (g.n_slices == 2 ? part : 0) : at.slice) * blocks16 + m) * low.pieces() * 32;
-                auto multiply = [&](const uint4 (&bv)[4]) {
-                    const uint4 s0 = s_at[0], s1 = s_at[32];
-                    s_at += 64;
+                for (int t = 0; t < 4; ++t) {
+                    if (GATED && t >= 2) mma16816(d[t], u0.x, u1.x, u0.y, u1.y, bv[t].x, bv[t].y);
+                    else mma16816(d[t], s0.x, s1.x, s0.y, s1.y, bv[t].x, bv[t].y);
+                }
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) mma16816(d[t], s0.x, s1.x, s0.y, s1.y, bv[t].x, bv[t].y);
+                for (int t = 0; t < 4; ++t) {
+                    if (GATED && t >= 2) mma16816(d[t], u0.z, u1.z, u0.w, u1.w, bv[t].z, bv[t].w);
+                    else mma16816(d[t], s0.z, s1.z, s0.w, s1.w, bv[t].z, bv[t].w);
+                }
+            };
+            if (KEEP) {
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) mma16816(d[t], s0.z, s1.z, s0.w, s1.w, bv[t].z, bv[t].w);
-                };
-                if (KEEP) {
-#pragma unroll
-                    for (int step = 0; step < KEEP; ++step) {
-                        multiply(kept[part * KEEP + step]);
-                        if (low.parts == 2) multiply(kept[part * KEEP + step]);
-                    }
-                } else {
+                for (int step = 0; step < KEEP; ++step) {
+                    multiply(kept[step]);
+                    if (low.parts == 2) multiply(kept[step]);
+                }
+            } else {
 #pragma unroll 1
-                    for (int step = 0; step < low.steps; ++step) {
-                        uint4 bv[4];
-                        load_b(part, step, bv);
-                        multiply(bv);
-                        if (low.parts == 2) multiply(bv);
-                    }
+                for (int step = 0; step < low.steps; ++step) {
+                    uint4 bv[4];
+                    load_b(step, bv);
+                    multiply(bv);
+                    if (low.parts == 2) multiply(bv);
                 }
             }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint4 w = base[part][h];
-                float v[8] = {bf_lo(w.x) + d[0][2 * h], bf_hi(w.x) + d[0][2 * h + 1], bf_lo(w.y) + d[1][2 * h], bf_hi(w.y) + d[1][2 * h + 1],
-                              bf_lo(w.z) + d[2][2 * h], bf_hi(w.z) + d[2][2 * h + 1], bf_lo(w.w) + d[3][2 * h], bf_hi(w.w) + d[3][2 * h + 1]};
-                if (part == 0) activate(g.act, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[h][j] = part ? y[h][j] * v[j] : v[j];
-            }
         }
-        const int row_now[2] = {row[0], row[1]};
+        const uint4 was[2] = {base[0], base[1]};
+        const int now[2] = {row[0], row[1]};
         if (16 * (m + 1) < rows) fetch(m + 1, row, base);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const float(&v)[8] = y[h];
-            const uint4 w = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            const uint32_t w[4] = {was[h].x, was[h].y, was[h].z, was[h].w};
+            float v[kPer], u[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const float x = bf_lo(w[t]) + d[t][2 * h], y = bf_hi(w[t]) + d[t][2 * h + 1];
+                if (GATED && t >= 2) u[2 * t - 4] = x, u[2 * t - 3] = y;
+                else v[2 * t] = x, v[2 * t + 1] = y;
+            }
+            activate(g.act, v);
+            if (GATED) {
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) v[j] *= u[j & 3];
+            }
+            uint32_t o[kPer / 2];
+#pragma unroll
+            for (int j = 0; j < kPer / 2; ++j) o[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
             const int r = 8 * h + gr;
-            if (!vec) *reinterpret_cast<uint4*>(edges[warp] + r * kEdgeRow + 16 * q) = w;
-            else if (16 * m + r < rows)
-                *reinterpret_cast<uint4*>(g.out + (unsigned long long)(unsigned)row_now[h] * (unsigned)g.ldo + at.col + 8 * q) = w;
+            unsigned char* to = vec ? reinterpret_cast<unsigned char*>(g.out + (unsigned long long)(unsigned)now[h] * (unsigned)g.ldo + at.col + kPer * q)
+                                    : edges[warp] + r * kEdgeRow + 2 * kPer * q;
+            if (!vec || 16 * m + r < rows) {
+                if (GATED) *reinterpret_cast<uint2*>(to) = make_uint2(o[0], o[1]);
+                else *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[kPer / 2 - 2], o[kPer / 2 - 1]);
+            }
         }
-        if (!vec) {                                                    // a row's 32 columns at a time
+        if (!vec) {                                                    // a row's columns at a time
             __syncwarp();
-            if (at.col + lane < at.end)
+            if (lane < min(kCols, left))
                 for (int r = 0; r < 16 && 16 * m + r < rows; ++r)
                     reinterpret_cast<unsigned short*>(g.out)[(size_t)tile.row[16 * m + r] * g.ldo + at.col + lane] =
                         *reinterpret_cast<const unsigned short*>(edges[warp] + r * kEdgeRow + 2 * lane);
@@ -551,17 +560,16 @@ dcut_status launch(dcut_ctx* ctx, LoraArgs& g, const CUtensorMap& a_map, int R, 
     g.tile_rows = R;
     g.part_row = SR + 8;
     g.tile_bytes = (long long)sizeof(Tile) + (long long)g.n_slices * (R / 16) * Low(g.rank).pieces() * 512;
-    int groups = 0;
-    for (int s = 0, lo = 0; s < (g.gated ? 1 : g.n_slices); ++s) {
-        const int end = g.gated ? g.N / 2 : g.end[s];
-        groups += (end - lo + 31) / 32;
-        lo = end;
+    g.groups = g.gated ? (g.N / 2 + 15) / 16 : 0;
+    for (int s = 0, lo = 0; s < (g.gated ? 0 : g.n_slices); ++s) {
+        g.groups += (g.end[s] - lo + 31) / 32;
+        lo = g.end[s];
     }
-    g.blocks = (groups + kWarps - 1) / kWarps;
+    g.blocks = (g.groups + kWarps - 1) / kWarps;
     // the sum of ceil(rows / R) over the units that are cut into tiles, at most; as many of them at a time as the scratch holds
     const long long tiles = ((long long)g.T_cap + (long long)units * (R - 1)) / R, room = DCUT_LORA_SCRATCH / g.tile_bytes;
     const int steps = Low(g.rank).steps;
-    auto* out = g.gated ? (steps == 1 ? lora_out_kernel<true, 1> : lora_out_kernel<true, 0>)
+    auto* out = g.gated ? (steps == 1 ? lora_out_kernel<true, 1> : steps == 2 ? lora_out_kernel<true, 2> : lora_out_kernel<true, 0>)
                         : (steps == 1 ? lora_out_kernel<false, 1> : steps == 2 ? lora_out_kernel<false, 2> : lora_out_kernel<false, 0>);
     for (long long t = 0; t < tiles; t += room) {
         const int n = (int)(tiles - t < room ? tiles - t : room);
