@@ -395,8 +395,14 @@ __global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(Lo
     __shared__ __align__(16) unsigned char edges[kWarps][16 * kEdgeRow];
     __shared__ Tile tile;
     __shared__ Search search;
+    __shared__ unsigned long long arrived;
+    extern __shared__ __align__(128) unsigned char s_here[];           // s of the slices that this CTA's columns belong to, where the tile has several blocks of rows
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gr = lane >> 2, q = lane & 3;
     const int number = blockIdx.x / g.blocks;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&arrived), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     const unsigned char* record = g.scratch + number * g.tile_bytes;
     if (early) find_tile(g, g.tile0 + number, g.tile_rows, tile, search);
     else {
@@ -445,18 +451,38 @@ __global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(Lo
 #pragma unroll
         for (int step = 0; step < KEEP; ++step) load_b(step, kept[step]);
     }
+    for (int r = 16 + lane; work && r < rows; r += 32) {               // the other rows of base come to L2 meanwhile
+        const __nv_bfloat16* p = g.base + (unsigned long long)(unsigned)tile.row[r] * (unsigned)g.ldbase + at.col;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+        if (GATED) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + width));
+    }
     if (early) dcut_pdl_wait();
     dcut_pdl_launch_dependents();
+    // s comes to shared memory in one piece; a single block of rows reads it where it is
+    const int slice_bytes = blocks16 * low.pieces() * 512, i0 = (blockIdx.x - number * g.blocks) * kWarps;
+    const int first_slice = GATED ? 0 : group_of<GATED>(g, i0).slice, last_slice = GATED ? g.n_slices - 1 : group_of<GATED>(g, min(i0 + kWarps, g.groups) - 1).slice;
+    const unsigned char* s_in = record + sizeof(Tile);
+    if (rows > 16 && adapter >= 0) {
+        if (threadIdx.x == 0) {
+            const uint32_t bytes = (last_slice - first_slice + 1) * slice_bytes;
+            mbar_arrive_expect_tx(smem_u32(&arrived), bytes);
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(smem_u32(s_here)), "l"(s_in + first_slice * slice_bytes), "r"(bytes), "r"(smem_u32(&arrived)) : "memory");
+        }
+        if (mbar_wait(smem_u32(&arrived), 0)) s_in = s_here - first_slice * slice_bytes;
+        else atomicExch(g.status, DCUT_DEV_LORA_WAIT_TIMEOUT);
+    }
     if (!work) return;
 
-    const uint4* s_in = reinterpret_cast<const uint4*>(record + sizeof(Tile)) + lane;
+    s_in += 16 * lane;
     const int slice = at.slice, slice_up = GATED && g.n_slices == 2 ? 1 : slice;
     for (int m = 0; 16 * m < rows; ++m) {
         float d[4][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.0f;
         if (live) {
-            const uint4 *s_at = s_in + (slice * blocks16 + m) * low.pieces() * 32, *s_up = s_in + (slice_up * blocks16 + m) * low.pieces() * 32;
+            const uint4* s_at = reinterpret_cast<const uint4*>(s_in + slice * slice_bytes + m * low.pieces() * 512);
+            const uint4* s_up = reinterpret_cast<const uint4*>(s_in + slice_up * slice_bytes + m * low.pieces() * 512);
             auto multiply = [&](const uint4 (&bv)[4]) {
                 const uint4 s0 = s_at[0], s1 = s_at[32], u0 = GATED ? s_up[0] : s0, u1 = GATED ? s_up[32] : s1;
                 s_at += 64, s_up += 64;
@@ -569,6 +595,7 @@ dcut_status launch(dcut_ctx* ctx, LoraArgs& g, const CUtensorMap& a_map, int R, 
     // the sum of ceil(rows / R) over the units that are cut into tiles, at most; as many of them at a time as the scratch holds
     const long long tiles = ((long long)g.T_cap + (long long)units * (R - 1)) / R, room = DCUT_LORA_SCRATCH / g.tile_bytes;
     const int steps = Low(g.rank).steps;
+    const size_t s_bytes = R > 16 ? (size_t)(g.tile_bytes - (long long)sizeof(Tile)) : 0;
     auto* out = g.gated ? (steps == 1 ? lora_out_kernel<true, 1> : steps == 2 ? lora_out_kernel<true, 2> : lora_out_kernel<true, 0>)
                         : (steps == 1 ? lora_out_kernel<false, 1> : steps == 2 ? lora_out_kernel<false, 2> : lora_out_kernel<false, 0>);
     for (long long t = 0; t < tiles; t += room) {
@@ -581,7 +608,7 @@ dcut_status launch(dcut_ctx* ctx, LoraArgs& g, const CUtensorMap& a_map, int R, 
                                        : launch_low<2>(ctx, g, a_map, n * split, split, smem, stream);
         if (st != DCUT_OK) return st;
         const int early = n * split <= ctx->sm_count;                    // there is room for this kernel's CTAs beside the first one's
-        st = dcut_check_cuda(ctx, dcut_launch_pdl(out, dim3((unsigned)(n * g.blocks)), dim3(kThreads), 0, stream, g, early), "launch lora_out_kernel");
+        st = dcut_check_cuda(ctx, dcut_launch_pdl(out, dim3((unsigned)(n * g.blocks)), dim3(kThreads), s_bytes, stream, g, early), "launch lora_out_kernel");
         if (st != DCUT_OK) return st;
     }
     return DCUT_OK;
@@ -595,6 +622,9 @@ dcut_status dcut_init_lora(dcut_ctx* ctx) {
     cudaError_t e = cudaFuncSetAttribute(lora_low_kernel<8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_low_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_low_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
+    constexpr int kMostLow = 64 * 4 * (M + 96);                         // s of a tile: ranks that are no multiple of 32 fill up to 24 elements of two parts
+    for (auto* out : {lora_out_kernel<false, 0>, lora_out_kernel<false, 1>, lora_out_kernel<false, 2>, lora_out_kernel<true, 0>, lora_out_kernel<true, 1>, lora_out_kernel<true, 2>})
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(out, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostLow);
     return dcut_check_cuda(ctx, e, "cudaFuncSetAttribute(lora)");
 }
 
