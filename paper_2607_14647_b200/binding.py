@@ -201,13 +201,33 @@ def _heads(dev: int, t: Optional[torch.Tensor], n_heads: int, head_dim: int):
     return t.data_ptr(), strides[0] if shape[0] > 1 else 0, strides[1] if n_heads > 1 else 0     # (of a single one the stride says nothing)
 
 
-def _rows(dev: int, t: Optional[torch.Tensor], dtype=torch.bfloat16, step16: int = 8):
-    """(pointer, row stride) of a [rows, columns] view whose rows are dense; step16: elements of 16 bytes."""
+def _rows(dev: int, t: Optional[torch.Tensor]):
+    """(pointer, row stride) of a bf16 [rows, columns] view whose rows are dense."""
     if t is None:
         return None, 0
     (rows, cols), (ld, step) = t.shape, t.stride()
-    assert t.get_device() == dev and t.dtype == dtype and (step == 1 or cols == 1), f"expected a matrix of {dtype} with dense rows on cuda:{dev}"
-    return t.data_ptr(), ld if rows > 1 else (cols + step16 - 1) // step16 * step16      # (one row: its stride says nothing)
+    assert t.get_device() == dev and t.dtype == torch.bfloat16 and (step == 1 or cols == 1), f"expected a bf16 matrix with dense rows on cuda:{dev}"
+    return t.data_ptr(), ld if rows > 1 else (cols + 7) // 8 * 8                         # (one row: its stride says nothing)
+
+
+def _matrix(dev: int, t: Optional[torch.Tensor], dtype, rows: int, cols: int, step16: int):
+    """_rows for any type (step16: its elements in 16 bytes), with at least `rows` rows of `cols` columns (each attribute of a tensor costs a
+    call: they are read once)."""
+    if t is None:
+        return None, 0
+    (n, c), (ld, step) = t.shape, t.stride()
+    assert n >= rows and c == cols, f"expected at least {rows} rows of {cols}, got {tuple(t.shape)}"
+    assert t.get_device() == dev and t.dtype is dtype and (step == 1 or c == 1), f"expected a matrix of {dtype} with dense rows on cuda:{dev}"
+    return t.data_ptr(), ld if n > 1 else (c + step16 - 1) // step16 * step16
+
+
+def _vector(dev: int, t: Optional[torch.Tensor], dtype, n: int, more: bool = False) -> Optional[int]:
+    """The pointer of a dense vector of n elements (more: of at least n)."""
+    if t is None:
+        return None
+    have = t.numel()
+    assert (have == n or more and have > n) and t.get_device() == dev and t.dtype is dtype and t.is_contiguous(), f"expected {n} elements of {dtype} on cuda:{dev}, got {tuple(t.shape)}"
+    return t.data_ptr()
 
 
 def rows8(rows: int, cols: int, device="cuda") -> torch.Tensor:
@@ -644,22 +664,18 @@ class Context:
     def linear8(self, a, a_scale, w, w_scale, cu_q, T_cap: int, out=None, bias=None, act: str = "none", w2=None, w2_scale=None, bias2=None, residual=None):
         """dcut_linear8: linear on e4m3 a [T_cap rows, K] and w [N, K] (rows a multiple of 16 elements apart: rows8, quantize) with
         fp32 scales a_scale [T_cap] and w_scale [N]; bias, residual and out are bf16."""
-        (N, K), dev = w.shape, self.device
-        assert a.shape[1] == K and a.shape[0] >= T_cap, "a must be [T_cap rows, K]"
-        assert a_scale.numel() >= T_cap and w_scale.shape == (N,)
-        assert bias is None or bias.shape == (N,)
-        assert bias2 is None or bias2.shape == (N,)
-        assert residual is None or (residual.shape[0] >= T_cap and residual.shape[1] == N)
+        (N, K), dev, f8, f32, bf16 = w.shape, self.device, torch.float8_e4m3fn, torch.float32, torch.bfloat16
         if out is None:
-            out = torch.empty((T_cap, N), dtype=torch.bfloat16, device=a.device)
-        assert out.shape[0] >= T_cap and out.shape[1] == N
-        (ap, lda), (wp, ldw), (w2p, ldw2) = (_rows(dev, t, torch.float8_e4m3fn, 16) for t in (a, w, w2))
-        (rp, ldr), (op, ldo) = _rows(dev, residual), _rows(dev, out)
-        assert w2 is None or (w2.shape == w.shape and ldw2 == ldw and w2_scale.shape == (N,)), "w2 must have the shape and strides of w"
-        f32, bf16 = torch.float32, torch.bfloat16
-        l = Linear8Args(ap, lda, _on(dev, a_scale, f32), wp, w2p, ldw, _on(dev, w_scale, f32), _on(dev, w2_scale, f32), _on(dev, bias, bf16),
-                        _on(dev, bias2, bf16), rp, ldr, op, ldo, N, K, ACTIVATIONS[act])
-        self._check(_lib.dcut_linear8(self._h, C.byref(l), _on(dev, cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, self._stream()))
+            out = torch.empty((T_cap, N), dtype=bf16, device=a.device)
+        ap, lda = _matrix(dev, a, f8, T_cap, K, 16)
+        wp, ldw = _matrix(dev, w, f8, N, K, 16)
+        w2p, ldw2 = _matrix(dev, w2, f8, N, K, 16)
+        rp, ldr = _matrix(dev, residual, bf16, T_cap, N, 8)
+        op, ldo = _matrix(dev, out, bf16, T_cap, N, 8)
+        assert w2 is None or ldw2 == ldw, "w2 must have the strides of w"
+        l = Linear8Args(ap, lda, _vector(dev, a_scale, f32, T_cap, True), wp, w2p, ldw, _vector(dev, w_scale, f32, N), _vector(dev, w2_scale, f32, N),
+                        _vector(dev, bias, bf16, N), _vector(dev, bias2, bf16, N), rp, ldr, op, ldo, N, K, ACTIVATIONS[act])
+        self._check(_lib.dcut_linear8(self._h, l, _on(dev, cu_q, torch.int32), cu_q.numel() - 1, T_cap, self._stream()))
         return out
 
     def rms_norm(self, x, cu_q, T_cap: int, gain=None, rms_eps: float = 1e-6, residual=None, h_out=None, out=None, out8=None, scale8=None,
@@ -678,38 +694,39 @@ class Context:
         return out8, scale8
 
     def _norm(self, x, cu_q, T_cap, normed, gain, rms_eps, residual, h_out, out, out8, scale8, gain_plus_one):
-        width, dev = x.shape[1], self.device
-        for t in (x, residual, h_out, out, out8):
-            assert t is None or (t.shape[0] >= T_cap and t.shape[1] == width), f"expected [T_cap rows, {width}], got {tuple(t.shape)}"
-        assert gain is None or gain.shape == (width,)
-        assert scale8 is None or scale8.numel() >= T_cap
-        (xp, ldx), (rp, ldr), (hp, ldh), (op, ldo) = _rows(dev, x), _rows(dev, residual), _rows(dev, h_out), _rows(dev, out)
-        p8, ld8 = _rows(dev, out8, torch.float8_e4m3fn, 16)
-        n = NormArgs(xp, ldx, rp, ldr, _on(dev, gain, torch.bfloat16), int(gain_plus_one), int(normed), rms_eps, width, hp, ldh, op, ldo, p8, ld8,
-                     _on(dev, scale8, torch.float32))
-        self._check(_lib.dcut_rms_norm(self._h, C.byref(n), _on(dev, cu_q, torch.int32), 0 if cu_q is None else cu_q.shape[0] - 1, T_cap, self._stream()))
+        width, dev, bf16 = x.shape[1], self.device, torch.bfloat16
+        xp, ldx = _matrix(dev, x, bf16, T_cap, width, 8)
+        rp, ldr = _matrix(dev, residual, bf16, T_cap, width, 8)
+        hp, ldh = _matrix(dev, h_out, bf16, T_cap, width, 8)
+        op, ldo = _matrix(dev, out, bf16, T_cap, width, 8)
+        p8, ld8 = _matrix(dev, out8, torch.float8_e4m3fn, T_cap, width, 16)
+        n = NormArgs(xp, ldx, rp, ldr, _vector(dev, gain, bf16, width), gain_plus_one, normed, rms_eps, width, hp, ldh, op, ldo, p8, ld8,
+                     _vector(dev, scale8, torch.float32, T_cap, True))
+        B = 0 if cu_q is None else cu_q.numel() - 1
+        self._check(_lib.dcut_rms_norm(self._h, n, _on(dev, cu_q, torch.int32), B, T_cap, self._stream()))
 
     def lora(self, x, a, b, adapter, base, cu_q, T_cap: int, out=None, scale=None, slices: Optional[Sequence[int]] = None, act: str = "none", gated: bool = False):
         """dcut_lora: out = act(base + scale (x a^T) b^T) with the adapter of each request (`adapter` int32 [B], below 0: none).  a [adapters, slices *
         rank, K] (a view with padded rows serves), b [adapters, N, rank], base [T_cap rows, N]; `slices`: the columns at which the slices
         end (None: one slice).  gated: the first half of the columns, activated, times the second.  out may be base."""
-        (m, N, rank), dev = b.shape, self.device
+        (m, N, rank), dev, bf16 = b.shape, self.device, torch.bfloat16
         ends = (N,) if slices is None else slices
-        K, width = x.shape[1], N // 2 if gated else N
-        assert len(ends) <= 4 and ends[-1] == N, "at most 4 slices, the last one ending at N"
-        assert a.shape == (m, len(ends) * rank, K), f"a must be [{m}, {len(ends) * rank}, {K}], got {tuple(a.shape)}"
-        lda = a.stride(1) if a.shape[1] > 1 else K
-        assert a.get_device() == dev and a.dtype == torch.bfloat16 and (a.stride(2) == 1 or K == 1) and (m == 1 or a.stride(0) == a.shape[1] * lda), \
+        K, width, S = x.shape[1], N // 2 if gated else N, len(ends)
+        assert S <= 4 and ends[-1] == N, "at most 4 slices, the last one ending at N"
+        (am, ar, ak), (a0, a1, a2) = a.shape, a.stride()
+        assert am == m and ar == S * rank and ak == K, f"a must be [{m}, {S * rank}, {K}], got {tuple(a.shape)}"
+        lda = a1 if ar > 1 else K
+        assert a.get_device() == dev and a.dtype is bf16 and (a2 == 1 or K == 1) and (m == 1 or a0 == ar * lda), \
             f"a must be a bf16 tensor on cuda:{dev} with dense rows, one after the other"
-        assert x.shape[0] >= T_cap and base.shape[0] >= T_cap and base.shape[1] == N
-        assert adapter.shape[0] == cu_q.shape[0] - 1 and (scale is None or scale.shape == (m,))
+        B = cu_q.numel() - 1
         if out is None:
-            out = torch.empty((T_cap, width), dtype=torch.bfloat16, device=x.device)
-        assert out.shape[0] >= T_cap and out.shape[1] == width
-        (xp, ldx), (bp, ldb), (op, ldo) = _rows(dev, x), _rows(dev, base), _rows(dev, out)
-        l = LoraArgs(xp, ldx, a.data_ptr(), lda, _on(dev, b, torch.bfloat16), _on(dev, scale, torch.float32), _on(dev, adapter, torch.int32), m, rank, len(ends),
-                     (_i * 4)(*ends), K, ACTIVATIONS[act], int(gated), bp, ldb, op, ldo)
-        self._check(_lib.dcut_lora(self._h, C.byref(l), _on(dev, cu_q, torch.int32), cu_q.shape[0] - 1, T_cap, self._stream()))
+            out = torch.empty((T_cap, width), dtype=bf16, device=x.device)
+        xp, ldx = _matrix(dev, x, bf16, T_cap, K, 8)
+        bp, ldb = _matrix(dev, base, bf16, T_cap, N, 8)
+        op, ldo = _matrix(dev, out, bf16, T_cap, width, 8)
+        l = LoraArgs(xp, ldx, a.data_ptr(), lda, _on(dev, b, bf16), _vector(dev, scale, torch.float32, m), _vector(dev, adapter, torch.int32, B), m, rank, S,
+                     tuple(ends), K, ACTIVATIONS[act], gated, bp, ldb, op, ldo)
+        self._check(_lib.dcut_lora(self._h, l, _on(dev, cu_q, torch.int32), B, T_cap, self._stream()))
         return out
 
     def make_model(self, layers: list, embed, g_final, w_lm, k_caches: list, v_caches: list, rms_eps: float = 1e-6,
