@@ -58,10 +58,14 @@ __device__ __forceinline__ uint32_t e4m3x2(float first, float second) {
     return r;
 }
 
-// Where slot i of a thread lies: VEC: 8 neighbouring elements, read and written as vectors (the row's last one may be partly
-// used); otherwise element j of the slot is `threads` elements after element j - 1, so that a warp's 2-byte accesses are neighbours.
-template <bool VEC>
+// How rows are read and written.  kVector: a slot of a thread is 8 neighbouring elements, a vector (the row's last one may be partly used).
+// kShifted: the same, but bf16 outputs begin anywhere (rows of an odd width one after the other, say; 7698 x 2789 50 us against 69 without it; the code
+// for it slows aligned rows down, so it is a form of its own).  kSingle: inputs begin anywhere too; element j of a slot is `threads` elements after
+// element j - 1, so that a warp's 2-byte accesses are neighbours.
+enum Access { kVector, kShifted, kSingle };
+template <Access ACCESS>
 struct Place {
+    static constexpr bool VEC = ACCESS != kSingle;
     int first, step, live;                             // live: elements of the slot that exist
     __device__ __forceinline__ Place(int slot, int tid, int threads, int width) {
         if (VEC) {
@@ -81,16 +85,44 @@ struct Place {
             if (j < live) w[j >> 1] |= (uint32_t)p[j * step] << (16 * (j & 1));
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    // (called by whole warps)
     __device__ __forceinline__ void store(__nv_bfloat16* row, const float (&v)[8]) const {
         const uint32_t w[4] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-        if (VEC && live == 8) {
-            *reinterpret_cast<uint4*>(row + first) = make_uint4(w[0], w[1], w[2], w[3]);
+        unsigned short* p = reinterpret_cast<unsigned short*>(row) + first;
+        auto some = [&](int from, int to) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j >= from && j < to) p[j * step] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+        };
+        const int s = ACCESS == kShifted ? (int)(reinterpret_cast<uintptr_t>(row) >> 1) & 7 : 0;      // elements from the 16-byte boundary before the row on
+        if (ACCESS != kShifted || !__all_sync(0xffffffffu, live == 8)) {
+            if (VEC && live == 8 && s == 0) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+            else some(0, live);
             return;
         }
-        unsigned short* p = reinterpret_cast<unsigned short*>(row) + first;
+        if (s == 0) {
+            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+            return;
+        }
+        // Rows that begin elsewhere: a lane stores the vector on the boundary before its first element, whose first s elements are the last ones of the
+        // lane before it.  The warp's first lane has none before it, and its last lane's last s elements are nobody else's.
+        uint32_t x[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < live) p[j * step] = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+        for (int j = 0; j < 4; ++j) x[j] = __shfl_up_sync(0xffffffffu, w[j], 1), x[4 + j] = w[j];
+        const int skip = 8 - s, lane = threadIdx.x & 31;               // elements of x that are left out
+#pragma unroll
+        for (int bit = 4; bit >= 2; bit >>= 1)
+            if (skip & bit) {
+#pragma unroll
+                for (int j = 0; j + bit / 2 < 8; ++j) x[j] = x[j + bit / 2];
+            }
+        if (skip & 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = __funnelshift_r(x[j], x[j + 1], 16);
+        }
+        if (lane > 0) *reinterpret_cast<uint4*>(p - s) = make_uint4(x[0], x[1], x[2], x[3]);
+        else some(0, skip);
+        if (lane == 31) some(skip, 8);
     }
     __device__ __forceinline__ void store8(unsigned char* row, const float (&v)[8]) const {
         const uint32_t w[2] = {e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16};
@@ -131,7 +163,7 @@ __device__ __forceinline__ Stats over_row(Stats s, Stats* warps) {
 
 // V slots per thread; ALONE: the CTA has one row, otherwise every warp its own; PLAIN: neither residual nor gain (what a row only quantised
 // needs: with their registers fewer CTAs fit an SM, 1088 x 12288 14 us against 11).
-template <int V, bool VEC, bool ALONE, bool PLAIN>
+template <int V, Access ACCESS, bool ALONE, bool PLAIN>
 __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
     __shared__ Stats warps[2][32];
     dcut_pdl_wait();
@@ -148,7 +180,7 @@ __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
     uint4 xv[V], rv[PLAIN ? 1 : V], gv[PLAIN ? 1 : V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const Place<VEC> at(i, tid, threads, a.width);
+        const Place<ACCESS> at(i, tid, threads, a.width);
         xv[i] = at.load(x_row);
         if (r_row) rv[PLAIN ? 0 : i] = at.load(r_row);
         if (has_gain) gv[PLAIN ? 0 : i] = at.load(a.gain);
@@ -179,7 +211,7 @@ __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[i][j] += r[j];
         }
-        if (a.h_out) Place<VEC>(i, tid, threads, a.width).store(a.h_out + (size_t)row * a.ldh, h[i]);
+        if (a.h_out) Place<ACCESS>(i, tid, threads, a.width).store(a.h_out + (size_t)row * a.ldh, h[i]);
         take(i);
     }
     s = over_row<ALONE>(s, warps[0]);
@@ -205,7 +237,7 @@ __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
     if (a.out8 && tid == 0) a.scale8[row] = most / kE4m3Max;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const Place<VEC> at(i, tid, threads, a.width);
+        const Place<ACCESS> at(i, tid, threads, a.width);
         float g[8], y[8];
         factor(i, g);
 #pragma unroll
@@ -219,14 +251,17 @@ __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
     }
 }
 
-template <int V, bool ALONE>
-cudaError_t launch(const NormArgs& a, bool vec, int rows_per_cta, int threads, cudaStream_t stream) {
+template <int V, bool ALONE, Access ACCESS>
+cudaError_t launch(const NormArgs& a, int rows_per_cta, int threads, cudaStream_t stream) {
     const dim3 grid((a.T_cap + rows_per_cta - 1) / rows_per_cta), block(threads);
-    if (a.residual || a.gain)
-        return vec ? dcut_launch_pdl(rms_norm_kernel<V, true, ALONE, false>, grid, block, 0, stream, a)
-                   : dcut_launch_pdl(rms_norm_kernel<V, false, ALONE, false>, grid, block, 0, stream, a);
-    return vec ? dcut_launch_pdl(rms_norm_kernel<V, true, ALONE, true>, grid, block, 0, stream, a)
-               : dcut_launch_pdl(rms_norm_kernel<V, false, ALONE, true>, grid, block, 0, stream, a);
+    return a.residual || a.gain ? dcut_launch_pdl(rms_norm_kernel<V, ACCESS, ALONE, false>, grid, block, 0, stream, a)
+                                : dcut_launch_pdl(rms_norm_kernel<V, ACCESS, ALONE, true>, grid, block, 0, stream, a);
+}
+template <int V, bool ALONE>
+cudaError_t launch(const NormArgs& a, Access access, int rows_per_cta, int threads, cudaStream_t stream) {
+    return access == kVector    ? launch<V, ALONE, kVector>(a, rows_per_cta, threads, stream)
+           : access == kShifted ? launch<V, ALONE, kShifted>(a, rows_per_cta, threads, stream)
+                                : launch<V, ALONE, kSingle>(a, rows_per_cta, threads, stream);
 }
 
 }  // namespace
@@ -245,15 +280,16 @@ dcut_status dcut_launch_rms_norm(dcut_ctx* ctx, const dcut_norm_args* n, const i
     a.eps = n->rms_eps, a.gain_add = n->gain_plus_one ? 1.0f : 0.0f;
     a.status = ctx->d_status;
     auto rows16 = [](const void* p, long long ld) { return !p || (!(reinterpret_cast<uintptr_t>(p) & 15) && ld % 8 == 0); };
-    const bool vec = rows16(a.x, a.ldx) && rows16(a.residual, a.ldr) && rows16(a.gain, 0) && rows16(a.h_out, a.ldh) && rows16(a.out, a.ldo) &&
-                     !((reinterpret_cast<uintptr_t>(a.out8) | (uintptr_t)(a.out8 ? a.ld8 : 0)) & 7);
+    const bool in16 = rows16(a.x, a.ldx) && rows16(a.residual, a.ldr) && rows16(a.gain, 0) &&
+                      !((reinterpret_cast<uintptr_t>(a.out8) | (uintptr_t)(a.out8 ? a.ld8 : 0)) & 7);
+    const Access access = !in16 ? kSingle : rows16(a.h_out, a.ldh) && rows16(a.out, a.ldo) ? kVector : kShifted;
     const int slots = (a.width + 7) / 8;
     const int per = slots <= 256 ? 1 : slots <= 768 ? 2 : slots <= 2048 ? 4 : 8;
     const int threads = ((slots + per - 1) / per + 31) & ~31;
-    cudaError_t e = threads == 32 ? launch<1, false>(a, vec, 4, 128, stream)
-                    : per == 1    ? launch<1, true>(a, vec, 1, threads, stream)
-                    : per == 2    ? launch<2, true>(a, vec, 1, threads, stream)
-                    : per == 4    ? launch<4, true>(a, vec, 1, threads, stream)
-                                  : launch<8, true>(a, vec, 1, threads, stream);
+    cudaError_t e = threads == 32 ? launch<1, false>(a, access, 4, 128, stream)
+                    : per == 1    ? launch<1, true>(a, access, 1, threads, stream)
+                    : per == 2    ? launch<2, true>(a, access, 1, threads, stream)
+                    : per == 4    ? launch<4, true>(a, access, 1, threads, stream)
+                                  : launch<8, true>(a, access, 1, threads, stream);
     return dcut_check_cuda(ctx, e, "launch rms_norm_kernel");
 }

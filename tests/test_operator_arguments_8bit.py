@@ -28,7 +28,7 @@ def test_good_arguments_pass(ctx8):
     ctx8.rms_norm(**NORM)
     ctx8.linear8(**LINEAR8)
     ctx8.lora(**LORA)
-    n, l, a = (c[1] for c in ctx8.calls)
+    n, l, a = (t.from_buffer_copy(c[1]) for t, c in zip((b.NormArgs, b.Linear8Args, b.LoraArgs), ctx8.calls))
     assert (n.width, n.ldx, n.ld8, n.normed, n.gain_plus_one) == (40, 40, 48, 1, 0)
     assert (l.N, l.K, l.lda, l.ldw, l.ldo) == (24, 40, 48, 48, 24)
     assert (a.n_adapters, a.rank, a.n_slices, list(a.slice_end)[:2], a.K, a.lda, a.ldbase) == (2, 8, 2, [10, 24], 40, 40, 24)
@@ -66,7 +66,7 @@ def test_lora_refuses(ctx8, wrong):
 
 def test_rows_of_single_rows_and_padded_views(ctx8):
     ctx8.rms_norm(z(2, 43)[:, :40][:1], CU, 1, out=z(1, 40))
-    assert ctx8.calls[-1][1].ldx == 40
+    assert b.NormArgs.from_buffer_copy(ctx8.calls[-1][1]).ldx == 40
     ctx8.lora(**dict(LORA, x=z(T, 56)[:, :40], a=z(2, 16, 48)[:, :, :40], base=z(T, 31)[:, :24], out=z(T, 27)[:, :24]))
-    a = ctx8.calls[-1][1]
+    a = b.LoraArgs.from_buffer_copy(ctx8.calls[-1][1])
     assert (a.ldx, a.lda, a.ldbase, a.ldo) == (56, 48, 31, 27)
