@@ -15,6 +15,8 @@
 #include <cuda_bf16.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "activation.cuh"
 #include "dcut_internal.h"
 #include "tcgen05.cuh"
@@ -48,9 +50,9 @@ __device__ __forceinline__ uint32_t cluster_size() {
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint4& a, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
 }
 // Asynchronous copies to shared memory; `bytes` of the 16 are read, the rest is filled with zeros.
 __device__ __forceinline__ void copy16(uint32_t to, const void* from, int bytes) {
@@ -181,17 +183,18 @@ __device__ __forceinline__ Group group_of(const LoraArgs& g, int i) {
     return Group{first + 32 * i, end, slice};
 }
 
-// How s lies in the scratch.  A step of the second product is 32 elements, 8 in a lane.  Ranks that are multiples of 32 take a step with the high
-// parts and again with the low ones (parts = 2); others walk the high parts and then the low ones as one row, so that rank 16 fills a step.
-// Per slice, 16 rows, step and part: rows gr and gr + 8 of the 16, a 16-byte piece per lane each.
+// How s lies in the scratch: as the fragments of the second product.  A step of that is 32 elements (two MMAs), 8 neighbouring ones in a lane.
+// Ranks that are multiples of 32 take a step with the high parts and again with the low ones (parts = 2); others walk the high parts and then the
+// low ones as one row, so that rank 16 fills a step.  Per slice, 16 rows, step, part and MMA: 16 bytes per lane, pairs of rows gr and gr + 8 in turn.
 struct Low {
     int steps, parts;
     __host__ __device__ Low(int rank) : steps(rank % 32 ? (2 * rank + 31) / 32 : rank / 32), parts(rank % 32 ? 1 : 2) {}
     __host__ __device__ int pieces() const { return steps * parts * 2; }                 // of 512 bytes, per slice and 16 rows
-    // the piece and the byte within it of element j (high or low part) of row r of a tile of MT blocks of 16 rows
+    // the byte where the pair of elements (j, j + 1) (high or low parts) of row r lies; the next pair of the MMA is 8 bytes on
     __device__ __forceinline__ int at(int blocks16, int rank, int slice, int r, int j, int low) const {
-        const int v = parts == 1 && low ? rank + j : j, part = parts == 1 ? 0 : low;
-        return ((((slice * blocks16 + (r >> 4)) * steps + (v >> 5)) * parts + part) * 2 + ((r >> 3) & 1)) * 512 + (((r & 7) << 2) + ((v >> 3) & 3)) * 16 + (v & 7) * 2;
+        const int v = parts == 1 && low ? rank + j : j, part = parts == 1 ? 0 : low, pair = (v & 7) >> 1;
+        return ((((slice * blocks16 + (r >> 4)) * steps + (v >> 5)) * parts + part) * 2 + (pair >> 1)) * 512 + (((r & 7) << 2) + ((v >> 3) & 3)) * 16 +
+               ((pair & 1) * 2 + ((r >> 3) & 1)) * 4;
     }
 };
 
@@ -369,14 +372,17 @@ __global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g, const
             if (p < split) s.x += v[p].x, s.y += v[p].y, s.z += v[p].z, s.w += v[p].w;
         s.x *= scale, s.y *= scale, s.z *= scale, s.w *= scale;
         const uint32_t hi0 = pack_bf16(s.x, s.y), hi1 = pack_bf16(s.z, s.w);
-        *reinterpret_cast<uint2*>(s_out + low.at(blocks16, g.rank, slice, r, j, 0)) = make_uint2(hi0, hi1);
-        *reinterpret_cast<uint2*>(s_out + low.at(blocks16, g.rank, slice, r, j, 1)) = make_uint2(low_parts(s.x, s.y, hi0), low_parts(s.z, s.w, hi1));
+        uint32_t* high = reinterpret_cast<uint32_t*>(s_out + low.at(blocks16, g.rank, slice, r, j, 0));
+        uint32_t* rest = reinterpret_cast<uint32_t*>(s_out + low.at(blocks16, g.rank, slice, r, j, 1));
+        high[0] = hi0, high[2] = hi1;
+        rest[0] = low_parts(s.x, s.y, hi0), rest[2] = low_parts(s.z, s.w, hi1);
     }
     if (low.parts == 1 && rank == split - 1) {                         // what fills up the last step
         const int rest = (32 * low.steps - 2 * g.rank) / 4;
         for (int e = threadIdx.x; e < g.n_slices * R * rest; e += kThreads) {
             const int sr = e / rest, v = 2 * g.rank + 4 * (e - sr * rest);
-            *reinterpret_cast<uint2*>(s_out + low.at(blocks16, g.rank, sr / R, sr % R, v, 0)) = make_uint2(0, 0);
+            uint32_t* p = reinterpret_cast<uint32_t*>(s_out + low.at(blocks16, g.rank, sr / R, sr % R, v, 0));
+            p[0] = p[2] = 0;
         }
     }
     cluster_sync_all();                                                // nobody leaves while its sums are read
@@ -427,15 +433,19 @@ __global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(Lo
             bv[t] = load_if(b + (size_t)(GATED && t >= 2 ? width + n : n) * g.rank + k, n < left && v < 2 * g.rank);
         }
     };
-    // base at this lane's columns of rows gr and gr + 8 of block m (those that do not exist: of the last one that does)
-    auto fetch = [&](int m, int (&row)[2], uint4 (&v)[2]) {
+    // base at this lane's columns of rows gr and gr + 8 of block m (those that do not exist: of the last one that does); `row`: twice their numbers,
+    // so that an address is one 32 x 32 + 64 bit operation
+    const unsigned char* base_at = reinterpret_cast<const unsigned char*>(g.base + at.col + kPer * q);
+    unsigned char* out_at = reinterpret_cast<unsigned char*>(g.out + at.col + kPer * q);
+    auto fetch = [&](auto vector, int m, int (&row)[2], uint4 (&v)[2]) {
+        constexpr bool VEC = decltype(vector)::value;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            row[h] = tile.row[min(16 * m + 8 * h + gr, rows - 1)];
-            const __nv_bfloat16* p = g.base + (unsigned long long)(unsigned)row[h] * (unsigned)g.ldbase + at.col + kPer * q;
+            row[h] = 2 * tile.row[min(16 * m + 8 * h + gr, rows - 1)];
+            const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(base_at + (unsigned long long)(unsigned)row[h] * (unsigned)g.ldbase);
             if (!GATED) {
-                v[h] = vec ? *reinterpret_cast<const uint4*>(p) : load_some(p, left - 8 * q);
-            } else if (vec) {
+                v[h] = VEC ? *reinterpret_cast<const uint4*>(p) : load_some(p, left - 8 * q);
+            } else if (VEC) {
                 const uint2 x = *reinterpret_cast<const uint2*>(p), y = *reinterpret_cast<const uint2*>(p + width);
                 v[h] = make_uint4(x.x, x.y, y.x, y.y);
             } else {
@@ -446,7 +456,8 @@ __global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(Lo
     };
     uint4 kept[KEEP ? KEEP : 1][4], base[2];
     int row[2];
-    if (work) fetch(0, row, base);
+    if (work && vec) fetch(std::true_type{}, 0, row, base);
+    if (work && !vec) fetch(std::false_type{}, 0, row, base);
     if (KEEP && live) {
 #pragma unroll
         for (int step = 0; step < KEEP; ++step) load_b(step, kept[step]);
@@ -476,81 +487,87 @@ __global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(Lo
 
     s_in += 16 * lane;
     const int slice = at.slice, slice_up = GATED && g.n_slices == 2 ? 1 : slice;
-    for (int m = 0; 16 * m < rows; ++m) {
-        float d[4][4];
+    // (a body for either way of access: with both in one, the predicated single accesses were half of its instructions)
+    auto all_rows = [&](auto vector) {
+        constexpr bool VEC = decltype(vector)::value;
+        for (int m = 0; 16 * m < rows; ++m) {
+            float d[4][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.0f;
-        if (live) {
-            const uint4* s_at = reinterpret_cast<const uint4*>(s_in + slice * slice_bytes + m * low.pieces() * 512);
-            const uint4* s_up = reinterpret_cast<const uint4*>(s_in + slice_up * slice_bytes + m * low.pieces() * 512);
-            auto multiply = [&](const uint4 (&bv)[4]) {
-                const uint4 s0 = s_at[0], s1 = s_at[32], u0 = GATED ? s_up[0] : s0, u1 = GATED ? s_up[32] : s1;
-                s_at += 64, s_up += 64;
+            for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.0f;
+            if (live) {
+                const uint4* s_at = reinterpret_cast<const uint4*>(s_in + slice * slice_bytes + m * low.pieces() * 512);
+                const uint4* s_up = reinterpret_cast<const uint4*>(s_in + slice_up * slice_bytes + m * low.pieces() * 512);
+                auto multiply = [&](const uint4 (&bv)[4]) {
+                    const uint4 s0 = s_at[0], s1 = s_at[32], u0 = GATED ? s_up[0] : s0, u1 = GATED ? s_up[32] : s1;       // (of its two MMAs)
+                    s_at += 64, s_up += 64;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    if (GATED && t >= 2) mma16816(d[t], u0.x, u1.x, u0.y, u1.y, bv[t].x, bv[t].y);
-                    else mma16816(d[t], s0.x, s1.x, s0.y, s1.y, bv[t].x, bv[t].y);
-                }
+                    for (int t = 0; t < 4; ++t) {
+                        if (GATED && t >= 2) mma16816(d[t], u0, bv[t].x, bv[t].y);
+                        else mma16816(d[t], s0, bv[t].x, bv[t].y);
+                    }
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    if (GATED && t >= 2) mma16816(d[t], u0.z, u1.z, u0.w, u1.w, bv[t].z, bv[t].w);
-                    else mma16816(d[t], s0.z, s1.z, s0.w, s1.w, bv[t].z, bv[t].w);
-                }
-            };
-            if (KEEP) {
+                    for (int t = 0; t < 4; ++t) {
+                        if (GATED && t >= 2) mma16816(d[t], u1, bv[t].z, bv[t].w);
+                        else mma16816(d[t], s1, bv[t].z, bv[t].w);
+                    }
+                };
+                if (KEEP) {
 #pragma unroll
-                for (int step = 0; step < KEEP; ++step) {
-                    multiply(kept[step]);
-                    if (low.parts == 2) multiply(kept[step]);
-                }
-            } else {
+                    for (int step = 0; step < KEEP; ++step) {
+                        multiply(kept[step]);
+                        if (low.parts == 2) multiply(kept[step]);
+                    }
+                } else {
 #pragma unroll 1
-                for (int step = 0; step < low.steps; ++step) {
-                    uint4 bv[4];
-                    load_b(step, bv);
-                    multiply(bv);
-                    if (low.parts == 2) multiply(bv);
+                    for (int step = 0; step < low.steps; ++step) {
+                        uint4 bv[4];
+                        load_b(step, bv);
+                        multiply(bv);
+                        if (low.parts == 2) multiply(bv);
+                    }
                 }
             }
-        }
-        const uint4 was[2] = {base[0], base[1]};
-        const int now[2] = {row[0], row[1]};
-        if (16 * (m + 1) < rows) fetch(m + 1, row, base);
+            const uint4 was[2] = {base[0], base[1]};
+            const int now[2] = {row[0], row[1]};
+            if (16 * (m + 1) < rows) fetch(vector, m + 1, row, base);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t w[4] = {was[h].x, was[h].y, was[h].z, was[h].w};
-            float v[kPer], u[4];
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t w[4] = {was[h].x, was[h].y, was[h].z, was[h].w};
+                float v[kPer], u[4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const float x = bf_lo(w[t]) + d[t][2 * h], y = bf_hi(w[t]) + d[t][2 * h + 1];
-                if (GATED && t >= 2) u[2 * t - 4] = x, u[2 * t - 3] = y;
-                else v[2 * t] = x, v[2 * t + 1] = y;
+                for (int t = 0; t < 4; ++t) {
+                    const float x = bf_lo(w[t]) + d[t][2 * h], y = bf_hi(w[t]) + d[t][2 * h + 1];
+                    if (GATED && t >= 2) u[2 * t - 4] = x, u[2 * t - 3] = y;
+                    else v[2 * t] = x, v[2 * t + 1] = y;
+                }
+                activate(g.act, v);
+                if (GATED) {
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) v[j] *= u[j & 3];
+                }
+                uint32_t o[kPer / 2];
+#pragma unroll
+                for (int j = 0; j < kPer / 2; ++j) o[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+                const int r = 8 * h + gr;
+                unsigned char* to = VEC ? out_at + (unsigned long long)(unsigned)now[h] * (unsigned)g.ldo
+                                        : edges[warp] + r * kEdgeRow + 2 * kPer * q;
+                if (!VEC || 16 * m + r < rows) {
+                    if (GATED) *reinterpret_cast<uint2*>(to) = make_uint2(o[0], o[1]);
+                    else *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[kPer / 2 - 2], o[kPer / 2 - 1]);
+                }
             }
-            activate(g.act, v);
-            if (GATED) {
-#pragma unroll
-                for (int j = 0; j < kPer; ++j) v[j] *= u[j & 3];
-            }
-            uint32_t o[kPer / 2];
-#pragma unroll
-            for (int j = 0; j < kPer / 2; ++j) o[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-            const int r = 8 * h + gr;
-            unsigned char* to = vec ? reinterpret_cast<unsigned char*>(g.out + (unsigned long long)(unsigned)now[h] * (unsigned)g.ldo + at.col + kPer * q)
-                                    : edges[warp] + r * kEdgeRow + 2 * kPer * q;
-            if (!vec || 16 * m + r < rows) {
-                if (GATED) *reinterpret_cast<uint2*>(to) = make_uint2(o[0], o[1]);
-                else *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[kPer / 2 - 2], o[kPer / 2 - 1]);
+            if (!VEC) {                                                    // a row's columns at a time
+                __syncwarp();
+                if (lane < min(kCols, left))
+                    for (int r = 0; r < 16 && 16 * m + r < rows; ++r)
+                        reinterpret_cast<unsigned short*>(g.out)[(size_t)tile.row[16 * m + r] * g.ldo + at.col + lane] =
+                            *reinterpret_cast<const unsigned short*>(edges[warp] + r * kEdgeRow + 2 * lane);
+                __syncwarp();
             }
         }
-        if (!vec) {                                                    // a row's columns at a time
-            __syncwarp();
-            if (lane < min(kCols, left))
-                for (int r = 0; r < 16 && 16 * m + r < rows; ++r)
-                    reinterpret_cast<unsigned short*>(g.out)[(size_t)tile.row[16 * m + r] * g.ldo + at.col + lane] =
-                        *reinterpret_cast<const unsigned short*>(edges[warp] + r * kEdgeRow + 2 * lane);
-            __syncwarp();
-        }
-    }
+    };
+    if (vec) all_rows(std::true_type{});
+    else all_rows(std::false_type{});
 }
 
 // Two CTAs of the first product per SM, and never three: CTAs of several streams' launches may meet on an SM, and three could want more tensor memory
