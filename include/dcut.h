@@ -516,7 +516,7 @@ dcut_status dcut_linear(dcut_ctx* ctx, const dcut_linear_args* args, const int* 
  * DEVICE in: x, residual bf16 [T_cap, width], gain bf16 [width].  DEVICE out: h_out, out bf16, out8 e4m3 (1 byte) [T_cap, width], scale8
  * fp32 [T_cap].  ld*: elements from row to row, >= width; any of them and any alignment of the type serve, but rows that start on
  * 16 bytes (out8: 8) are moved in vectors.  h_out may be x or the residual, out may be x, each with that one's stride; nothing else may overlap.
- * cu_q int32 [B+1], or NULL: all T_cap rows (B is not looked at).  width up to 32768; T_cap is not bound by dcut_limits.  A
+ * cu_q int32 [B+1], or NULL: all T_cap rows (B is not looked at).  width up to 32768; T_cap up to 2^30, not bound by dcut_limits.  A
  * cu_q[B] above T_cap sets device status 10; rows from cu_q[B] on are not touched.  The struct is HOST memory, read during the call.
  */
 typedef struct {
@@ -576,8 +576,9 @@ dcut_status dcut_linear8(dcut_ctx* ctx, const dcut_linear8_args* args, const int
  * one ends at N), with rows of `a` of their own: q|k|v or gate|up of one projection; s(n) is the slice of column n.
  *   out = act(base + d)                                                                    [T, N]
  *   out[:, j] = act((base + d)[:, j]) * (base + d)[:, N/2 + j],   gated != 0               [T, N/2] (N even; one slice, or two halves)
- * fp32 sums; x . a^T enters the second product with 16 bits (two bf16 values); one rounding of out.  Needs no scratch and
- * no context shapes; requests of any length, T_cap is not bound by dcut_limits.
+ * fp32 sums; x . a^T enters the second product with 16 bits (two bf16 values); one rounding of out.  Needs no context shapes;
+ * requests of any length, B up to DCUT_LORA_MAX_B, T_cap not bound by dcut_limits (x . a^T lies in 8 MB of the context's scratch, a part of
+ * the rows at a time where they need more).  Requests that share an adapter share its reads.
  * DEVICE in: x bf16 [T_cap, K] with ldx elements from row to row; a bf16 [n_adapters, n_slices * rank, K] with lda elements from row to row
  *   (adapters follow one another: n_slices * rank * lda); b bf16 [n_adapters, N, rank] dense; scale fp32 [n_adapters] or NULL (1);
  *   adapter int32 [B]; base bf16 [T_cap, N] with ldbase; cu_q int32 [B+1].  x, a, b 16-byte aligned, ldx and lda multiples of 8; base and out of any
@@ -589,6 +590,7 @@ dcut_status dcut_linear8(dcut_ctx* ctx, const dcut_linear8_args* args, const int
  */
 #define DCUT_LORA_MAX_SLICES 4
 #define DCUT_LORA_MAX_RANKS 256
+#define DCUT_LORA_MAX_B 8192
 typedef struct {
     const void* x;
     long long ldx;

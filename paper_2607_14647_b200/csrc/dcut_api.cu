@@ -675,6 +675,7 @@ dcut_status dcut_rms_norm(dcut_ctx* c, const dcut_norm_args* n, const int* cu_q,
     if (!n->h_out && !n->out && !n->out8) return dcut_fail(c, DCUT_EINVAL, "no output");
     if (n->gain && !n->normed) return dcut_fail(c, DCUT_EINVAL, "a gain goes with the norm");
     if ((cu_q && B < 1) || T_cap < 1 || n->width < 1) return dcut_fail(c, DCUT_EINVAL, "need B, T_cap, width >= 1");
+    if (T_cap > (1 << 30)) return dcut_fail(c, DCUT_ECAPACITY, "T_cap goes up to 2^30");
     if (n->width > DCUT_NORM_MAX_WIDTH) return dcut_fail(c, DCUT_ECAPACITY, "width = %d exceeds %d", n->width, DCUT_NORM_MAX_WIDTH);
     if (n->normed && (!(n->rms_eps > 0.0f) || isinf(n->rms_eps))) return dcut_fail(c, DCUT_EINVAL, "rms_eps must be > 0 and finite");
     const void* rows[5] = {n->x, n->residual, n->h_out, n->out, n->out8};
@@ -701,7 +702,8 @@ dcut_status dcut_lora(dcut_ctx* c, const dcut_lora_args* l, const int* cu_q, int
     for (int i = 0; i < l->n_slices; ++i)
         if (l->slice_end[i] <= (i ? l->slice_end[i - 1] : 0)) return dcut_fail(c, DCUT_EINVAL, "slice_end must ascend from above 0");
     const int N = l->slice_end[l->n_slices - 1];
-    if (N > (1 << 21) || T_cap > (1 << 21) || l->K > (1 << 30) || B > (1 << 20)) return dcut_fail(c, DCUT_ECAPACITY, "N and T_cap go up to 2^21, K to 2^30, B to 2^20");
+    if (N > (1 << 21) || T_cap > (1 << 21) || l->K > (1 << 30) || B > DCUT_LORA_MAX_B)
+        return dcut_fail(c, DCUT_ECAPACITY, "N and T_cap go up to 2^21, K to 2^30, B to %d", DCUT_LORA_MAX_B);
     if (l->n_adapters > (1 << 22)) return dcut_fail(c, DCUT_ECAPACITY, "n_adapters goes up to 2^22");
     if (l->act < DCUT_ACT_NONE || l->act > DCUT_ACT_SILU) return dcut_fail(c, DCUT_EINVAL, "unknown activation %d", l->act);
     if (l->gated && (N % 2 || l->n_slices > 2 || (l->n_slices == 2 && l->slice_end[0] != N / 2)))

@@ -140,7 +140,9 @@ struct dcut_ctx {
 // Programmatic dependent launch: the kernel may be scheduled while its predecessor in the stream is still running
 // (its CTAs take SMs as the predecessor's CTAs leave), which hides launch latency and the kernel's own set-up.  Every
 // kernel launched this way calls dcut_pdl_wait() before it touches global memory: the wait returns when the
-// predecessor grid has completed, and since the predecessor did the same, everything earlier has completed too.
+// predecessor grid has completed, and since the predecessor did the same, everything earlier has completed too.  (One kernel, the second of dcut_lora,
+// reads before its wait what its predecessor has waited for and does not write: a grid starts early only once every CTA of its predecessor has
+// asked for that, which each does behind its own wait.)
 template <typename... KArgs, typename... Args>
 inline cudaError_t dcut_launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream,
                                    Args&&... args) {

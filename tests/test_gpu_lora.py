@@ -198,6 +198,14 @@ def test_the_most_ranks(n_slices, rank):
         check(c, run(context(), c))
 
 
+@pytest.mark.parametrize("counts,rank,n_slices", [([9000], 256, 1), ([5000, 0, 4100], 64, 4), ([1] * 8000, 8, 1)])
+def test_more_rows_than_the_scratch_holds_at_a_time(counts, rank, n_slices):
+    c = make(rank, counts, sum(counts) + 2, 64, [24 * (i + 1) for i in range(n_slices)], rank, 2, ids=[i % 2 for i in range(len(counts))])
+    ctx = context()
+    check(c, run(ctx, c))
+    assert ctx.poll_device_status() == 0
+
+
 def test_an_adapter_that_does_not_exist_and_a_packing_above_the_cap():
     ctx, c = context(), make(9, [2, 3, 4], 9, 64, [40], 16, 3, ids=[0, 1, 2])
     c["adapter"][1] = 3

@@ -28,7 +28,7 @@ BAD = [(dict([(n, None)]), b.EINVAL) for n in ("x", "a", "b", "adapter", "base",
     (dict(ldx=100), b.EINVAL), (dict(ldx=96), b.EINVAL), (dict(lda=101), b.EINVAL), (dict(lda=-104), b.EINVAL), (dict(lda=(1 << 32) + 8), b.EINVAL),
     (dict(ldbase=43), b.EINVAL), (dict(ldo=43), b.EINVAL), (dict(out=P, ldo=48), b.EINVAL), (dict(out=P, gated=1, slice_end=(22, 44)), b.EINVAL),
     (dict(out=P, base=P + 4096), b.EINVAL), (dict(slice_end=(20, (1 << 21) + 1), ldbase=1 << 22, ldo=1 << 22), b.ECAPACITY), (dict(T_cap=(1 << 21) + 1), b.ECAPACITY),
-    (dict(B=(1 << 20) + 1), b.ECAPACITY), (dict(n_adapters=(1 << 22) + 1), b.ECAPACITY), (dict(ldo=1 << 32), b.EINVAL), (dict(ldbase=1 << 32), b.EINVAL)]
+    (dict(B=8193), b.ECAPACITY), (dict(n_adapters=(1 << 22) + 1), b.ECAPACITY), (dict(ldo=1 << 32), b.EINVAL), (dict(ldbase=1 << 32), b.EINVAL)]
 
 
 @pytest.mark.parametrize("kw,status", BAD)

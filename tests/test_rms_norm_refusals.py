@@ -22,7 +22,7 @@ BAD = [(dict(x=None), b.EINVAL), (dict(out=None), b.EINVAL), (dict(out8=P, ld8=1
        (dict(h_out=P + 8192, ldh=96), b.EINVAL), (dict(out8=P + 8192, ld8=96, scale8=P), b.EINVAL), (dict(x=P + 1), b.EINVAL), (dict(gain=P + 1), b.EINVAL),
        (dict(out=P + 4097), b.EINVAL), (dict(out8=P + 8193, ld8=112, scale8=P + 2), b.EINVAL), (dict(h_out=P, ldh=112), b.EINVAL),
        (dict(out=P, ldo=112), b.EINVAL), (dict(residual=P + 8192, ldr=104, h_out=P + 8192, ldh=112), b.EINVAL), (dict(h_out=P + 4096, ldh=100), b.EINVAL),
-       (dict(residual=P + 4096, ldr=100), b.EINVAL), (dict(width=32769, ldx=40000, ldo=40000), b.ECAPACITY)] + [
+       (dict(residual=P + 4096, ldr=100), b.EINVAL), (dict(width=32769, ldx=40000, ldo=40000), b.ECAPACITY), (dict(T_cap=(1 << 30) + 1), b.ECAPACITY)] + [
     (dict([(n, v)]), b.EINVAL) for n in ("B", "T_cap", "width") for v in (0, -1)]
 
 
