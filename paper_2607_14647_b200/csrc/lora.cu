@@ -13,10 +13,10 @@
 //   lora_out_kernel   a few columns of a tile per warp, 16 rows at a time, on warp-level MMAs: the base, the sum and the result stay in one lane.
 // Measured on the device (floors in brackets: bytes at the copy rate): 16 single tokens with an adapter each, rank 16, 4096 -> 6144 in three slices 11 us
 // (1.4); 603 tokens of 64 requests with 24 adapters, 4096 -> 4096 14 us (3); gate and up projection of 1088 tokens, 8 adapters of rank 64,
-// 4096 -> 2 x 12288 with SiLU 64 us (18); 8191 tokens of three prompts, rank 32, 4096 -> 6144 75 us (42).  The small ones are two launches and their
+// 4096 -> 2 x 12288 with SiLU 63 us (18); 8191 tokens of three prompts, rank 32, 4096 -> 6144 75 us (42).  The small ones are two launches and their
 // chains of loads (find the tile 1.5 us, x and A 2.3, the sums' way between CTAs 2); at length the first product takes a third (L2 to shared memory),
-// the second is bound by instructions and their latency (0.5 issued per cycle and scheduler, two to three CTAs per SM by their registers).
-// One kernel for both, whose clusters kept s to themselves and took an eighth of the columns per CTA each, took 200 and 175 us where these take 64
+// the second is bound by instructions and their latency (0.41 to 0.44 issued per active cycle and scheduler, two to three CTAs per SM by their registers).
+// One kernel for both, whose clusters kept s to themselves and took an eighth of the columns per CTA each, took 200 and 175 us where these take 63
 // and 75: 8 to 16 warps per SM, and every step waited for its loads.
 #include <cuda_bf16.h>
 #include <math.h>
