@@ -10,7 +10,8 @@
 // 8191 rows of 4096 with a residual and both outputs (302 MB) 52 us, 5.8 TB/s of reads and writes; 16 rows 2.6 us.  A thread has 1 to 8 pieces of 16 bytes, by
 // the width: more of them mean fewer threads per row and more rows per SM (12288 wide: 2 pieces 19 us, 4 pieces 14), fewer a shorter
 // chain for a single row.
-// A sum of squares that overflows (|h| above about 10^18) is formed again from h * 2^-80.  The maximum keeps a NaN.
+// A sum of squares that overflows (|h| above about 10^18) is formed again from h * 2^-80.  Where it does, or h * gain does, h is normalised ahead of
+// the gain (2^-80 would make the squares of ordinary values vanish).  The maximum keeps a NaN.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -165,7 +166,7 @@ __device__ __forceinline__ Stats over_row(Stats s, Stats* warps) {
 // needs: with their registers fewer CTAs fit an SM, 1088 x 12288 14 us against 11).
 template <int V, Access ACCESS, bool ALONE, bool PLAIN>
 __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
-    __shared__ Stats warps[2][32];
+    __shared__ Stats warps[3][32];
     dcut_pdl_wait();
     dcut_pdl_launch_dependents();
     const int T = a.cu_q ? a.cu_q[a.B] : a.T_cap;
@@ -218,18 +219,26 @@ __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
     float r = 1.0f;
     if (a.normed) {
         float eps = a.eps;
-        if (!(s.sum < INFINITY) || !(fabsf(s.top) < INFINITY)) {      // (the same answer in every thread of the row)
+        auto again = [&](float by, Stats* at) {                        // the statistics of h * by
             s = {0.0f, 0.0f};
 #pragma unroll
             for (int i = 0; i < V; ++i) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) h[i][j] *= 0x1p-80f;
+                for (int j = 0; j < 8; ++j) h[i][j] *= by;
                 take(i);
             }
-            s = over_row<ALONE>(s, warps[1]);
+            s = over_row<ALONE>(s, at);
+        };
+        const bool far = !(s.sum < INFINITY) || !(fabsf(s.top) < INFINITY);          // (the same answer in every thread of the row)
+        if (!(s.sum < INFINITY)) {
+            again(0x1p-80f, warps[1]);
             eps = eps * 0x1p-80f * 0x1p-80f;
         }
         r = 1.0f / sqrtf(s.sum / (float)a.width + eps);
+        if (far) {
+            again(r, warps[2]);
+            r = 1.0f;
+        }
     }
     const float top = fabsf(s.top) * r;
     const float most = top < INFINITY ? fmaxf(top, kLeast) : NAN;     // a row with a value that is no number has no scale

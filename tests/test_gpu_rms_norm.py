@@ -227,3 +227,13 @@ def test_another_stream_and_a_captured_call():
         graph.replay()
         assert torch.equal(out[:T], eager["b"][:T]) and (out[T:] == 0).all()
         assert torch.equal(out8[:T].view(torch.uint8), eager["8"][:T].view(torch.uint8))
+
+
+@pytest.mark.parametrize("scale,gain_scale", [(100.0, 5e36), (1e10, 1e36), (1e-3, 5e36), (1e37, 1e20), (1e37, 1e30)])
+def test_gains_whose_product_with_h_overflows_where_y_does_not(scale, gain_scale):
+    """h gain is above fp32's largest value, its squares' sum is not (or is too): y is an ordinary number of bf16."""
+    g = torch.Generator("cuda").manual_seed(12)
+    for width in (77, 256, 5000, 20000):
+        x, gain = view(g, 4, width, -width % 8, scale), (gain_scale * torch.randn(width, generator=g, device="cuda")).to(BF16)
+        o, buf = run(context(), x, 4, 4, gain=gain)
+        check(o, buf, x, 4, gain=gain)
