@@ -52,7 +52,7 @@ def run(ctx, c, act="none", out=None, pad=0):
     return out
 
 
-def expected(c, act="none", base=None):
+def expected(c, act="none", base=None, s_rounding=2.0 ** -8, parts=1):
     """(want, tolerance) of the rows that requests own."""
     N, ends, r = c["ends"][-1], c["ends"], c["b"].shape[2]
     lo, hi = int(c["hcu"][0]), int(c["hcu"][-1])
@@ -66,12 +66,12 @@ def expected(c, act="none", base=None):
         f = 1.0 if c["scale"] is None else float(c["scale"][t])
         K = a.shape[1]
         s, es = f * (x[p:q] @ a.T), f * K * 2.0 ** -23 * (np.abs(x[p:q]) @ np.abs(a).T)
-        es = es * (1 + 2.0 ** -7) + (2.0 ** -8 + 2.0 ** -24) * np.abs(s)
+        es = es * (1 + 2.0 ** -7) + (s_rounding + 2.0 ** -24) * np.abs(s)
         first = 0
         for j, end in enumerate(ends):
             k, n = slice(j * r, (j + 1) * r), slice(first, end)
             z[p - lo:q - lo, n] += s[:, k] @ b[n].T
-            e[p - lo:q - lo, n] = es[:, k] @ np.abs(b[n]).T + r * 2.0 ** -23 * 1.01 * (np.abs(s[:, k]) @ np.abs(b[n]).T)
+            e[p - lo:q - lo, n] = es[:, k] @ np.abs(b[n]).T + parts * r * 2.0 ** -23 * 1.01 * (np.abs(s[:, k]) @ np.abs(b[n]).T)
             first = end
     e += 2.0 ** -24 * np.abs(z)
     one = np.eye(1)
@@ -315,3 +315,31 @@ def test_refusals_through_the_context():
         ctx.lora(c["x"], c["a"], c["b"], c["adapter"], c["base"], c["cu"], 5, slices=[20, 39])
     with pytest.raises(KeyError):
         ctx.lora(c["x"], c["a"], c["b"], c["adapter"], c["base"], c["cu"], 5, act="tanh")
+
+
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 64, 96])
+@pytest.mark.parametrize("counts,gated", [([1], False), (RAGGED, False), ([150, 64], False), ([150, 64], True)])
+def test_the_low_rank_product_keeps_16_bits(rank, counts, gated):
+    """s enters the second product as two bf16 values: the first is off by half a step, at most 2^(e-8) where |s| is in [2^e, 2^(e+1)); that rest lies
+    in a binade no higher than 2^(e-9) (2^(e-8) itself is exact), so its rounding is off by 2^(e-17) at most: 2^-17 |s|.  No base, so that sums
+    that cancel show it: without the low parts this term would be 2^9 times as large.  The second sum has twice the rank's terms."""
+    c = make(1000 + rank, counts, sum(counts) + 1, 64, [80, 160] if gated else [96, 200], rank, 3, ids=[i % 3 for i in range(len(counts))], gated=gated)
+    c["base"].zero_()
+    lo, hi = int(c["hcu"][0]), int(c["hcu"][-1])
+    want, tol = expected(c, "none", s_rounding=2.0 ** -17, parts=2)
+    got = bf16_values(run(context(), c))[lo:hi, :c["width"]]
+    assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
+    # the same sums from one bf16 value would not pass (formed here, in 64 bits, where nothing follows the sum)
+    if gated or sum(counts) < 100:
+        return
+    x, z = bf16_values(c["x"])[lo:hi], np.zeros_like(want)
+    for i, t in enumerate(c["ids"]):
+        rows = slice(int(c["hcu"][i]) - lo, int(c["hcu"][i + 1]) - lo)
+        if t >= 0:
+            f = 1.0 if c["scale"] is None else float(c["scale"][t])
+            s = bf16_values(torch.from_numpy(f * (x[rows] @ bf16_values(c["a"][t]).T)).to(torch.bfloat16))
+            first = 0
+            for j, end in enumerate(c["ends"]):
+                z[rows, first:end] = s[:, j * rank:(j + 1) * rank] @ bf16_values(c["b"][t])[first:end].T
+                first = end
+    assert (np.abs(z - want) > tol).any()
