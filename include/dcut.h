@@ -577,16 +577,17 @@ dcut_status dcut_linear8(dcut_ctx* ctx, const dcut_linear8_args* args, const int
  *   out = act(base + d)                                                                    [T, N]
  *   out[:, j] = act((base + d)[:, j]) * (base + d)[:, N/2 + j],   gated != 0               [T, N/2] (N even; one slice, or two halves)
  * fp32 sums; x . a^T enters the second product with 16 bits (two bf16 values); one rounding of out.  Needs no context shapes;
- * requests of any length, B up to DCUT_LORA_MAX_B, T_cap not bound by dcut_limits (x . a^T lies in 8 MB of the context's scratch, a part of
+ * requests of any length, B up to DCUT_LORA_MAX_B, T_cap up to 2^21 and not bound by dcut_limits (x . a^T lies in 8 MB of the context's scratch, a part of
  * the rows at a time where they need more).  Requests that share an adapter share its reads.
  * DEVICE in: x bf16 [T_cap, K] with ldx elements from row to row; a bf16 [n_adapters, n_slices * rank, K] with lda elements from row to row
  *   (adapters follow one another: n_slices * rank * lda); b bf16 [n_adapters, N, rank] dense; scale fp32 [n_adapters] or NULL (1);
  *   adapter int32 [B]; base bf16 [T_cap, N] with ldbase; cu_q int32 [B+1].  x, a, b 16-byte aligned, ldx and lda multiples of 8; base and out of any
  *   stride and alignment (rows and slices that start on 16 bytes are moved in vectors).
- * DEVICE out: out bf16 with ldo.  It may be base (same stride, not gated): rows without an adapter then stay as they are; nothing else
- *   may overlap.  Rows that no request owns are not touched.
+ * DEVICE out: out bf16 with ldo.  It may be base (same stride, not gated): without an activation rows without an adapter are then not touched,
+ *   with one they become act(base); nothing else may overlap.  Rows that no request owns are not touched.
  * rank a multiple of 8 (smaller ones: pad with zeros), n_slices * rank <= DCUT_LORA_MAX_RANKS.  An adapter >= n_adapters sets device status 11
- * and counts as none; a cu_q[B] above T_cap sets status 10.  The struct is HOST memory, read during the call.
+ * and counts as none; a cu_q[B] above T_cap sets status 10.  An infinite element of b can give NaN where the formula gives an infinity (the low part
+ * of x . a^T may be 0).  The struct is HOST memory, read during the call.
  */
 #define DCUT_LORA_MAX_SLICES 4
 #define DCUT_LORA_MAX_RANKS 256
