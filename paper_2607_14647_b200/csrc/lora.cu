@@ -11,7 +11,7 @@
 //                     added in a fixed order.  s is scaled in fp32 and kept as the sum of two bf16 values (off by 2^-17 of it at most; a single one
 //                     cost the result up to 1.7 times its error where d outweighs base).
 //   lora_out_kernel   a few columns of a tile per warp, 16 rows at a time, on warp-level MMAs: the base, the sum and the result stay in one lane.
-// Measured on the device (floors in brackets: bytes at the copy rate): 16 single tokens with an adapter each, rank 16, 4096 -> 6144 in three slices 11 us
+// Measured on the device (floors in brackets: bytes at the copy rate): 16 single tokens with an adapter each, rank 16, 4096 -> 6144 in three slices 10 us
 // (1.4); 603 tokens of 64 requests with 24 adapters, 4096 -> 4096 14 us (3); gate and up projection of 1088 tokens, 8 adapters of rank 64,
 // 4096 -> 2 x 12288 with SiLU 63 us (18); 8191 tokens of three prompts, rank 32, 4096 -> 6144 75 us (42).  The small ones are two launches and their
 // chains of loads (find the tile 1.5 us, x and A 2.3, the sums' way between CTAs 2); at length the first product takes a third (L2 to shared memory),
@@ -400,8 +400,14 @@ __global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g, const
 // sum's terms is free).  KEEP: the rank's steps, where B's fragments stay in registers for all rows; 0: they are read again for every 16.
 // `early`: the CTA finds its tile itself and asks for B and its first rows of base while the first product runs (what that one waited for is
 // complete once this grid has started); otherwise it reads the tile from the scratch.
-template <bool GATED, int KEEP>
-__global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(LoraArgs g, int early) {
+// FEW: tiles of 16 rows, one block of them: a body without what the others need.  CTAs per SM (registers): of long tiles 2 with two steps in
+// registers, else 3 (4 took 87 us where 3 take 75 for 8191 tokens).  Tiles of 16 rows have more to wait for and less to do: 4 against 3, 16 tokens with
+// an adapter each, gated, 4096 -> 2 x 12288, rank 16 18.7 us against 20.2, 64 tokens of rank 96 93 against 104; two steps in registers 3 against 2, 64
+// tokens of rank 64, 4096 -> 12288 37 against 42 (4: 46; gated 64 tokens 78 either way, 4: 84); B read again, no gate: 3, 4 spills
+// (16 tokens of rank 128, 4096 -> 6144 21 against 18).
+constexpr int out_ctas(bool gated, int keep, bool few) { return few ? (keep == 2 || (keep == 0 && !gated) ? 3 : 4) : keep == 2 ? 2 : 3; }
+template <bool GATED, int KEEP, bool FEW>
+__global__ void __launch_bounds__(kThreads, out_ctas(GATED, KEEP, FEW)) lora_out_kernel(LoraArgs g, int early) {
     constexpr int kCols = GATED ? 16 : 32, kPer = kCols / 4;           // columns of a group, of a lane
     const int blocks16 = g.tile_rows / 16;
     __shared__ __align__(16) unsigned char edges[kWarps][16 * kEdgeRow];
@@ -468,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(Lo
 #pragma unroll
         for (int step = 0; step < KEEP; ++step) load_b(step, kept[step]);
     }
-    for (int r = 16 + lane; work && r < rows; r += 32) {               // the other rows of base come to L2 meanwhile
+    for (int r = 16 + lane; !FEW && work && r < rows; r += 32) {               // the other rows of base come to L2 meanwhile
         const __nv_bfloat16* p = g.base + (unsigned long long)(unsigned)tile.row[r] * (unsigned)g.ldbase + at.col;
         asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
         if (GATED) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + width));
@@ -479,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(Lo
     const int slice_bytes = blocks16 * low.pieces() * 512, i0 = (blockIdx.x - number * g.blocks) * kWarps;
     const int first_slice = GATED ? 0 : group_of<GATED>(g, i0).slice, last_slice = GATED ? g.n_slices - 1 : group_of<GATED>(g, min(i0 + kWarps, g.groups) - 1).slice;
     const unsigned char* s_in = record + sizeof(Tile);
-    if (rows > 16 && adapter >= 0) {
+    if (!FEW && rows > 16 && adapter >= 0) {
         if (threadIdx.x == 0) {
             const uint32_t bytes = (last_slice - first_slice + 1) * slice_bytes;
             mbar_arrive_expect_tx(smem_u32(&arrived), bytes);
@@ -496,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(Lo
     // (a body for either way of access: with both in one, the predicated single accesses were half of its instructions)
     auto all_rows = [&](auto vector) {
         constexpr bool VEC = decltype(vector)::value;
-        for (int m = 0; 16 * m < rows; ++m) {
+        for (int m = 0; FEW ? m < 1 : 16 * m < rows; ++m) {
             float d[4][4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.0f;
@@ -535,7 +541,7 @@ __global__ void __launch_bounds__(kThreads, KEEP > 1 ? 2 : 3) lora_out_kernel(Lo
             }
             const uint4 was[2] = {base[0], base[1]};
             const int now[2] = {row[0], row[1]};
-            if (16 * (m + 1) < rows) fetch(vector, m + 1, row, base);
+            if (!FEW && 16 * (m + 1) < rows) fetch(vector, m + 1, row, base);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const uint32_t w[4] = {was[h].x, was[h].y, was[h].z, was[h].w};
@@ -599,6 +605,11 @@ dcut_status launch_low(dcut_ctx* ctx, const LoraArgs& g, const CUtensorMap& a_ma
     lc.numAttrs = 2;
     return dcut_check_cuda(ctx, cudaLaunchKernelEx(&lc, lora_low_kernel<STAGES>, g, a_map), "launch lora_low_kernel");
 }
+template <bool FEW>
+auto out_kernel(bool gated, int steps) {
+    return gated ? (steps == 1 ? lora_out_kernel<true, 1, FEW> : steps == 2 ? lora_out_kernel<true, 2, FEW> : lora_out_kernel<true, 0, FEW>)
+                 : (steps == 1 ? lora_out_kernel<false, 1, FEW> : steps == 2 ? lora_out_kernel<false, 2, FEW> : lora_out_kernel<false, 0, FEW>);
+}
 dcut_status launch(dcut_ctx* ctx, LoraArgs& g, const CUtensorMap& a_map, int R, int units, cudaStream_t stream) {
     const int SR = g.n_slices * g.rank, stage = (R + SR) * kRowBytes, sums = R * (SR + 8) * 4;
     // behind the last step: 128 rows from the beginning of its x on, 8 more rows of A; and the alignment
@@ -619,8 +630,7 @@ dcut_status launch(dcut_ctx* ctx, LoraArgs& g, const CUtensorMap& a_map, int R, 
     const long long tiles = ((long long)g.T_cap + (long long)units * (R - 1)) / R, room = DCUT_LORA_SCRATCH / g.tile_bytes;
     const int steps = Low(g.rank).steps;
     const size_t s_bytes = R > 16 ? (size_t)(g.tile_bytes - (long long)sizeof(Tile)) : 0;
-    auto* out = g.gated ? (steps == 1 ? lora_out_kernel<true, 1> : steps == 2 ? lora_out_kernel<true, 2> : lora_out_kernel<true, 0>)
-                        : (steps == 1 ? lora_out_kernel<false, 1> : steps == 2 ? lora_out_kernel<false, 2> : lora_out_kernel<false, 0>);
+    auto* out = R == 16 ? out_kernel<true>(g.gated != 0, steps) : out_kernel<false>(g.gated != 0, steps);
     for (long long t = 0; t < tiles; t += room) {
         const int n = (int)(tiles - t < room ? tiles - t : room);
         g.tile0 = (int)t;
@@ -646,8 +656,8 @@ dcut_status dcut_init_lora(dcut_ctx* ctx) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_low_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_low_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     constexpr int kMostLow = 64 * 4 * (M + 96);                         // s of a tile: ranks that are no multiple of 32 fill up to 24 elements of two parts
-    for (auto* out : {lora_out_kernel<false, 0>, lora_out_kernel<false, 1>, lora_out_kernel<false, 2>, lora_out_kernel<true, 0>, lora_out_kernel<true, 1>, lora_out_kernel<true, 2>})
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(out, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostLow);
+    for (int i = 0; i < 6; ++i)                                         // (tiles of 16 rows read s where it lies)
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(out_kernel<false>(i >= 3, i % 3), cudaFuncAttributeMaxDynamicSharedMemorySize, kMostLow);
     return dcut_check_cuda(ctx, e, "cudaFuncSetAttribute(lora)");
 }
 
