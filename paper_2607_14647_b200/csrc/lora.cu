@@ -13,10 +13,10 @@
 //   lora_out_kernel   a few columns of a tile per warp, 16 rows at a time, on warp-level MMAs: the base, the sum and the result stay in one lane.
 // Measured on the device (floors in brackets: bytes at the copy rate): 16 single tokens with an adapter each, rank 16, 4096 -> 6144 in three slices 10 us
 // (1.4); 603 tokens of 64 requests with 24 adapters, 4096 -> 4096 14 us (3); gate and up projection of 1088 tokens, 8 adapters of rank 64,
-// 4096 -> 2 x 12288 with SiLU 63 us (18); 8191 tokens of three prompts, rank 32, 4096 -> 6144 75 us (42).  The small ones are two launches and their
+// 4096 -> 2 x 12288 with SiLU 58 us (18); 8191 tokens of three prompts, rank 32, 4096 -> 6144 75 us (42).  The small ones are two launches and their
 // chains of loads (find the tile 1.5 us, x and A 2.3, the sums' way between CTAs 2); at length the first product takes a third (L2 to shared memory),
 // the second is bound by instructions and their latency (0.41 to 0.44 issued per active cycle and scheduler, two to three CTAs per SM by their registers).
-// One kernel for both, whose clusters kept s to themselves and took an eighth of the columns per CTA each, took 200 and 175 us where these take 63
+// One kernel for both, whose clusters kept s to themselves and took an eighth of the columns per CTA each, took 200 and 175 us where these take 58
 // and 75: 8 to 16 warps per SM, and every step waited for its loads.
 #include <cuda_bf16.h>
 #include <math.h>
@@ -48,6 +48,7 @@ struct LoraArgs {
     int tile0, groups, blocks;           // first tile of this pass; groups of columns, and CTAs of the second product, per tile
     unsigned char* scratch;              // per tile: a Tile, then its s
     long long tile_bytes;
+    int b_at;                            // where B follows the second product's s in shared memory
     int* status;
 };
 
@@ -406,7 +407,11 @@ __global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g, const
 // tokens of rank 64, 4096 -> 12288 37 against 42 (4: 46; gated 64 tokens 78 either way, 4: 84); B read again, no gate: 3, 4 spills
 // (16 tokens of rank 128, 4096 -> 6144 21 against 18).
 constexpr int out_ctas(bool gated, int keep, bool few) { return few ? (keep == 2 || (keep == 0 && !gated) ? 3 : 4) : keep == 2 ? 2 : 3; }
-template <bool GATED, int KEEP, bool FEW>
+// STAGED: the kept B comes by way of shared memory (a lane's own pieces: nobody else looks at them).  For two steps of long tiles, of ranks that are
+// multiples of 32: gated 1088 tokens of rank 64 63.1 us -> 57.9, 2800 tokens 4096 -> 2 x 4096 57.4 -> 53.7 (600 tokens 54.2 -> 54.7), both kernels
+// together; the second one alone takes the same 50 us either way.  Other ranks ask for the same pieces twice: rank 24 52 us, staged 59 (55 with copies
+// through L1, which cost rank 64 its gain and more).
+template <bool GATED, int KEEP, bool FEW, bool STAGED>
 __global__ void __launch_bounds__(kThreads, out_ctas(GATED, KEEP, FEW)) lora_out_kernel(LoraArgs g, int early) {
     constexpr int kCols = GATED ? 16 : 32, kPer = kCols / 4;           // columns of a group, of a lane
     const int blocks16 = g.tile_rows / 16;
@@ -437,12 +442,18 @@ __global__ void __launch_bounds__(kThreads, out_ctas(GATED, KEEP, FEW)) lora_out
     const bool vec = g.vec && at.col + kCols <= at.end && !((at.col | (GATED ? width : 0)) & (kPer - 1));
     const int left = at.end - at.col;
     const __nv_bfloat16* b = g.b + ((size_t)max(adapter, 0) * g.N + at.col) * g.rank;
-    auto load_b = [&](int step, uint4 (&bv)[4]) {                      // (behind both parts s is zero, and so is this)
-        const int v = 32 * step + 8 * q, k = v < g.rank ? v : v - g.rank;
+    // the place of a lane's piece t of a step in B, and whether there is one (behind both parts s is zero, and so is this)
+    auto b_place = [&](int step, int t, bool& there) {
+        const int v = 32 * step + 8 * q, k = v < g.rank ? v : v - g.rank, n = kPer * (gr >> 1) + 2 * (GATED ? t & 1 : t) + (gr & 1);
+        there = n < left && v < 2 * g.rank;
+        return b + (size_t)(GATED && t >= 2 ? width + n : n) * g.rank + k;
+    };
+    auto load_b = [&](int step, uint4 (&bv)[4]) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const int n = kPer * (gr >> 1) + 2 * (GATED ? t & 1 : t) + (gr & 1);
-            bv[t] = load_if(b + (size_t)(GATED && t >= 2 ? width + n : n) * g.rank + k, n < left && v < 2 * g.rank);
+            bool there;
+            const __nv_bfloat16* p = b_place(step, t, there);
+            bv[t] = load_if(p, there);
         }
     };
     // base at this lane's columns of rows gr and gr + 8 of block m (those that do not exist: of the last one that does); `row`: twice their numbers,
@@ -470,7 +481,16 @@ __global__ void __launch_bounds__(kThreads, out_ctas(GATED, KEEP, FEW)) lora_out
     int row[2];
     if (work && vec) fetch(std::true_type{}, 0, row, base);
     if (work && !vec) fetch(std::false_type{}, 0, row, base);
-    if (KEEP && live) {
+    const uint32_t b_here = smem_u32(s_here) + g.b_at + (warp * KEEP * 4 * 32 + lane) * 16;
+    if (STAGED && live) {
+#pragma unroll
+        for (int e = 0; e < KEEP * 4; ++e) {
+            bool there;
+            const __nv_bfloat16* p = b_place(e / 4, e % 4, there);
+            copy16(b_here + e * 512, there ? p : g.b, there ? 16 : 0);
+        }
+        copies_done();
+    } else if (KEEP && live) {
 #pragma unroll
         for (int step = 0; step < KEEP; ++step) load_b(step, kept[step]);
     }
@@ -496,6 +516,14 @@ __global__ void __launch_bounds__(kThreads, out_ctas(GATED, KEEP, FEW)) lora_out
         else atomicExch(g.status, DCUT_DEV_LORA_WAIT_TIMEOUT);
     }
     if (!work) return;
+    if (STAGED && live) {
+        copies_wait<0>();
+#pragma unroll
+        for (int e = 0; e < KEEP * 4; ++e) {
+            uint4& v = kept[e / 4][e % 4];
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(b_here + e * 512) : "memory");
+        }
+    }
 
     s_in += 16 * lane;
     const int slice = at.slice, slice_up = GATED && g.n_slices == 2 ? 1 : slice;
@@ -585,6 +613,7 @@ __global__ void __launch_bounds__(kThreads, out_ctas(GATED, KEEP, FEW)) lora_out
 // Two CTAs of the first product per SM, and never three: CTAs of several streams' launches may meet on an SM, and three could want more tensor memory
 // than it has (256 columns at most each).  One would wait for another's, whose cluster might wait for the first one's.  The library's other kernels that
 // hold tensor memory leave no room beside them.
+constexpr int kStagedB = kWarps * 2 * 4 * 512;                        // two steps of a CTA's columns
 constexpr int kMostShared = 110 * 1024, kLeastShared = 77 * 1024;
 
 template <int STAGES>
@@ -605,10 +634,12 @@ dcut_status launch_low(dcut_ctx* ctx, const LoraArgs& g, const CUtensorMap& a_ma
     lc.numAttrs = 2;
     return dcut_check_cuda(ctx, cudaLaunchKernelEx(&lc, lora_low_kernel<STAGES>, g, a_map), "launch lora_low_kernel");
 }
-template <bool FEW>
-auto out_kernel(bool gated, int steps) {
-    return gated ? (steps == 1 ? lora_out_kernel<true, 1, FEW> : steps == 2 ? lora_out_kernel<true, 2, FEW> : lora_out_kernel<true, 0, FEW>)
-                 : (steps == 1 ? lora_out_kernel<false, 1, FEW> : steps == 2 ? lora_out_kernel<false, 2, FEW> : lora_out_kernel<false, 0, FEW>);
+template <bool GATED>
+auto out_kernel(int rank, bool few) {
+    const Low low(rank);
+    if (few) return low.steps == 1 ? lora_out_kernel<GATED, 1, true, false> : low.steps == 2 ? lora_out_kernel<GATED, 2, true, false> : lora_out_kernel<GATED, 0, true, false>;
+    if (low.steps == 2) return low.parts == 2 ? lora_out_kernel<GATED, 2, false, true> : lora_out_kernel<GATED, 2, false, false>;
+    return low.steps == 1 ? lora_out_kernel<GATED, 1, false, false> : lora_out_kernel<GATED, 0, false, false>;
 }
 dcut_status launch(dcut_ctx* ctx, LoraArgs& g, const CUtensorMap& a_map, int R, int units, cudaStream_t stream) {
     const int SR = g.n_slices * g.rank, stage = (R + SR) * kRowBytes, sums = R * (SR + 8) * 4;
@@ -628,9 +659,10 @@ dcut_status launch(dcut_ctx* ctx, LoraArgs& g, const CUtensorMap& a_map, int R, 
     g.blocks = (g.groups + kWarps - 1) / kWarps;
     // the sum of ceil(rows / R) over the units that are cut into tiles, at most; as many of them at a time as the scratch holds
     const long long tiles = ((long long)g.T_cap + (long long)units * (R - 1)) / R, room = DCUT_LORA_SCRATCH / g.tile_bytes;
-    const int steps = Low(g.rank).steps;
-    const size_t s_bytes = R > 16 ? (size_t)(g.tile_bytes - (long long)sizeof(Tile)) : 0;
-    auto* out = R == 16 ? out_kernel<true>(g.gated != 0, steps) : out_kernel<false>(g.gated != 0, steps);
+    const Low low(g.rank);
+    g.b_at = R > 16 ? (int)(g.tile_bytes - (long long)sizeof(Tile)) : 0;
+    const size_t s_bytes = g.b_at + (R > 16 && low.steps == 2 && low.parts == 2 ? kStagedB : 0);
+    auto* out = g.gated ? out_kernel<true>(g.rank, R == 16) : out_kernel<false>(g.rank, R == 16);
     for (long long t = 0; t < tiles; t += room) {
         const int n = (int)(tiles - t < room ? tiles - t : room);
         g.tile0 = (int)t;
@@ -656,8 +688,9 @@ dcut_status dcut_init_lora(dcut_ctx* ctx) {
     if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_low_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_low_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     constexpr int kMostLow = 64 * 4 * (M + 96);                         // s of a tile: ranks that are no multiple of 32 fill up to 24 elements of two parts
-    for (int i = 0; i < 6; ++i)                                         // (tiles of 16 rows read s where it lies)
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(out_kernel<false>(i >= 3, i % 3), cudaFuncAttributeMaxDynamicSharedMemorySize, kMostLow);
+    for (int rank : {8, 24, 64, 128})                                   // one for each form (tiles of 16 rows read s where it lies)
+        for (auto* out : {out_kernel<false>(rank, false), out_kernel<true>(rank, false)})
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(out, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostLow + kStagedB);
     return dcut_check_cuda(ctx, e, "cudaFuncSetAttribute(lora)");
 }
 
