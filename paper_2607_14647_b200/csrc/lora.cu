@@ -285,20 +285,20 @@ __global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g, const
 #pragma unroll
         for (int i = 0; i < kMostRows / kStrideRows; ++i)
             from[i] = g.x + (size_t)tile.row[min(r0 + kStrideRows * i, rows - 1)] * g.ldx + (size_t)c0 * kChunk + 8 * piece;
-        int left = 2 * (g.K - c0 * kChunk - 8 * piece);                // bytes from this thread's piece to the end of its rows
+        int left = g.K - c0 * kChunk - 8 * piece;                      // elements from this thread's piece to the end of its rows (their bytes may not fit 31 bits)
         for (int c = 0, slot = 0; c < n_chunks; ++c) {
             if (c >= STAGES && !mbar_wait(empty + 8 * slot, (c / STAGES - 1) & 1)) {
                 failed = true;
                 break;
             }
-            const int bytes = min(16, max(0, left));                   // (0: nothing is read, and the address is one that exists)
+            const int bytes = 2 * min(8, max(0, left));                // (0: nothing is read, and the address is one that exists)
 #pragma unroll
             for (int i = 0; i < kMostRows / kStrideRows; ++i) {
                 if (r0 + kStrideRows * i < rows) copy16(to0 + slot * stage + i * kStrideRows * kRowBytes, bytes ? from[i] : g.x, bytes);
                 from[i] += kChunk;
             }
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full + 8 * slot) : "memory");
-            left -= kRowBytes;
+            left -= kChunk;
             slot = slot + 1 == STAGES ? 0 : slot + 1;
         }
     } else if (warp == 0) {
