@@ -545,7 +545,7 @@ dcut_status dcut_rms_norm(dcut_ctx* ctx, const dcut_norm_args* args, const int* 
  *   out[r, :] = residual[r, :] + act((a8[r, :] . w8^T) a_scale[r] w_scale + bias)                                           w2 NULL
  *   out[r, :] = residual[r, :] + act((a8[r, :] . w8^T) a_scale[r] w_scale + bias) * ((a8[r, :] . w2^T) a_scale[r] w2_scale + bias2)
  * a, w, w2: e4m3 [T_cap, K], [N, K], [N, K]; a_scale fp32 [T_cap], w_scale and w2_scale fp32 [N]; everything else as dcut_linear:
- * products accumulated in fp32, scales, bias, activation, gate and residual in fp32, one rounding to bf16.
+ * products accumulated in fp32, scales, bias, activation, gate and residual in fp32, one rounding to bf16.  Needs a context with attention shapes.
  * lda and ldw are multiples of 16 elements (bytes), bases 16-byte aligned (scales 4-byte).
  */
 typedef struct {

@@ -103,7 +103,7 @@ void free_all(dcut_ctx* c) {
 // What dcut_linear and dcut_linear8 ask of their arguments; `step`: elements of 16 bytes.
 template <typename ARGS>
 dcut_status check_linear(dcut_ctx* c, const ARGS* l, int step, const int* cu_q, int B, int T_cap) {
-    if (c->lim.n_q_heads <= 0) return dcut_fail(c, DCUT_EINVAL, "context was created without attention shapes (no tensor-map encoder)");
+    if (c->lim.n_q_heads <= 0) return dcut_fail(c, DCUT_EINVAL, "context was created without attention shapes (the matrix products are set up with them)");
     if (!l || !l->a || !l->w || !l->out || !cu_q || (l->bias2 && !l->w2)) return dcut_fail(c, DCUT_EINVAL, "null pointer argument (bias2 goes with w2)");
     if (B < 1 || T_cap < 1 || l->N < 1 || l->K < 1) return dcut_fail(c, DCUT_EINVAL, "need B, T_cap, N, K >= 1");
     if (l->N > (1 << 21) || l->K > (1 << 30) || T_cap > (1 << 21)) return dcut_fail(c, DCUT_ECAPACITY, "N and T_cap go up to 2^21, K to 2^30");
@@ -450,7 +450,7 @@ dcut_status dcut_gemm_bf16(dcut_ctx* c, const void* a, const void* w, const void
                            const int* cu_q, int B, int T_cap, void* out, const void* residual, void* stream) {
     if (!c) return DCUT_EINVAL;
     DCUT_ON_DEVICE(c);
-    if (!c->layer_maps) return dcut_fail(c, DCUT_EINVAL, "context was created without attention shapes (no tensor-map encoder)");
+    if (!c->layer_maps) return dcut_fail(c, DCUT_EINVAL, "context was created without attention shapes (the matrix products are set up with them)");
     if (!a || !w || !cu_q || !out || (mode == 2 && !w2) || (mode == 1 && !residual) || mode < 0 || mode > 2)
         return dcut_fail(c, DCUT_EINVAL, "null pointer or bad mode");
     if (B < 1 || T_cap < 1 || K < 64 || K % 64 || N < 1 || N % (mode == 2 ? 128 : 256))
