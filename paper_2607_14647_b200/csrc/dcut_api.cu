@@ -161,11 +161,14 @@ dcut_status dcut_create(dcut_ctx** out, const dcut_limits* lim, int device) {
     if ((st = dmalloc(c, &c->d_bucket_K, DCUT_MAX_BUCKETS, "cudaMalloc(bucket_K)")) != DCUT_OK) return st;
     if ((st = dmalloc(c, &c->d_row_key, max_T, "cudaMalloc(row_key)")) != DCUT_OK) return st;
     if ((st = dmalloc(c, &c->d_status, 4, "cudaMalloc(status)")) != DCUT_OK) return st;
-    {   // the tensor-map encoder
+    {   // the tensor-map encoder: attention and matrix products need it; elsewhere dcut_lora alone does, and says so itself
         cudaDriverEntryPointQueryResult found;
         const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &c->encode_tiled, cudaEnableDefault, &found);
-        if (e != cudaSuccess || found != cudaDriverEntryPointSuccess || !c->encode_tiled)
-            return dcut_fail(c, DCUT_ECUDA, "cuTensorMapEncodeTiled entry point not available");
+        if (e != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            (void)cudaGetLastError();
+            c->encode_tiled = nullptr;
+        }
+        if (has_attn && !c->encode_tiled) return dcut_fail(c, DCUT_ECUDA, "cuTensorMapEncodeTiled entry point not available");
     }
     if (lim->vocab > 0) {   // rejection-sampling acceptance: per-row softmax statistics of vocabulary segments of ~8k tokens
         c->rs_n_seg = (lim->vocab + 8191) / 8192;
@@ -718,6 +721,7 @@ dcut_status dcut_lora(dcut_ctx* c, const dcut_lora_args* l, const int* cu_q, int
         return dcut_fail(c, DCUT_EINVAL, "base and out must be 2-byte aligned, scale and adapter 4-byte");
     if (l->out == l->base && (l->gated || l->ldo != l->ldbase)) return dcut_fail(c, DCUT_EINVAL, "out over base needs the same stride and no gate");
     if (l->out == l->x) return dcut_fail(c, DCUT_EINVAL, "out must not be x");
+    if (!c->encode_tiled) return dcut_fail(c, DCUT_ECUDA, "cuTensorMapEncodeTiled entry point not available");
     DCUT_ON_DEVICE(c);
     return dcut_launch_lora(c, l, cu_q, B, T_cap, static_cast<cudaStream_t>(stream));
 }
