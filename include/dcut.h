@@ -476,10 +476,10 @@ dcut_status dcut_prefix_attn(dcut_ctx* ctx, const void* q, const void* k_cache, 
  *   out[r, :] = residual[r, :] + act(a[r, :] . w^T + bias)                                    w2 NULL
  *   out[r, :] = residual[r, :] + act(a[r, :] . w^T + bias) * (a[r, :] . w2^T + bias2)         gated
  * for rows r < cu_q[B] (rows from there on are not touched).  bf16 in, fp32 accumulation, bias, activation, gate and residual
- * in fp32, one rounding to bf16.  Any N, K >= 1.
+ * in fp32, one rounding to bf16.  Any N from 1 to 2^21, K from 1 to 2^30, T_cap from 1 to 2^21.
  *   act: none; relu; gelu = x Phi(x); gelu_tanh = x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2; silu = x / (1 + e^-x).
- * DEVICE: a [T_cap rows readable, K] with lda elements from row to row, w and w2 [N, K] with ldw; both strides multiples of 8
- * and >= K, bases 16-byte aligned.  bias, bias2 [N] or NULL; residual [T, N] with ldr or NULL; out [T, N] with ldo (>= N; any
+ * DEVICE: a [T_cap rows readable, K] with lda elements from row to row, w and w2 [N, K] with ldw; both strides multiples of 8,
+ * >= K and <= 2^32, bases 16-byte aligned.  bias, bias2 [N] or NULL; residual [T, N] with ldr or NULL; out [T, N] with ldo (>= N; any
  * alignment: 16-byte aligned rows are stored in vectors).  out may be the residual itself (same stride); it must not
  * overlap the inputs in any other way.  The struct is HOST memory, read during the call.  Needs a context with attention shapes;
  * N, K and T_cap are not bound by dcut_limits.
@@ -514,7 +514,7 @@ dcut_status dcut_linear(dcut_ctx* ctx, const dcut_linear_args* args, const int* 
  * normed = 0 quantises rows: the attention's output ahead of the O projection, an MLP's activation, or a weight at load
  * time (its rows are output channels: dcut_linear8's w_scale).
  * DEVICE in: x, residual bf16 [T_cap, width], gain bf16 [width].  DEVICE out: h_out, out bf16, out8 e4m3 (1 byte) [T_cap, width], scale8
- * fp32 [T_cap].  ld*: elements from row to row, >= width; any of them and any alignment of the type serve, but rows that start on
+ * fp32 [T_cap].  ld*: elements from row to row, >= width and <= 2^32; any of them and any alignment of the type serve, but rows that start on
  * 16 bytes (out8: 8) are moved in vectors.  h_out may be x or the residual, out may be x, each with that one's stride; nothing else may overlap.
  * cu_q int32 [B+1], or NULL: all T_cap rows (B is not looked at).  width up to 32768; T_cap up to 2^30, not bound by dcut_limits.  A
  * cu_q[B] above T_cap sets device status 10; rows from cu_q[B] on are not touched.  The struct is HOST memory, read during the call.
@@ -546,7 +546,7 @@ dcut_status dcut_rms_norm(dcut_ctx* ctx, const dcut_norm_args* args, const int* 
  *   out[r, :] = residual[r, :] + act((a8[r, :] . w8^T) a_scale[r] w_scale + bias) * ((a8[r, :] . w2^T) a_scale[r] w2_scale + bias2)
  * a, w, w2: e4m3 [T_cap, K], [N, K], [N, K]; a_scale fp32 [T_cap], w_scale and w2_scale fp32 [N]; everything else as dcut_linear:
  * products accumulated in fp32, scales, bias, activation, gate and residual in fp32, one rounding to bf16.  Needs a context with attention shapes.
- * lda and ldw are multiples of 16 elements (bytes), bases 16-byte aligned (scales 4-byte).
+ * lda and ldw are multiples of 16 elements (bytes), >= K and <= 2^32, bases 16-byte aligned (scales 4-byte); N, K and T_cap go as far as there.
  */
 typedef struct {
     const void* a;
@@ -577,12 +577,12 @@ dcut_status dcut_linear8(dcut_ctx* ctx, const dcut_linear8_args* args, const int
  *   out = act(base + d)                                                                    [T, N]
  *   out[:, j] = act((base + d)[:, j]) * (base + d)[:, N/2 + j],   gated != 0               [T, N/2] (N even; one slice, or two halves)
  * fp32 sums; x . a^T enters the second product with 16 bits (two bf16 values); one rounding of out.  Needs no context shapes;
- * requests of any length, B up to DCUT_LORA_MAX_B, T_cap up to 2^21 and not bound by dcut_limits (x . a^T lies in 8 MB of the context's scratch, a part of
- * the rows at a time where they need more).  Requests that share an adapter share its reads.
+ * requests of any length, B up to DCUT_LORA_MAX_B, N and T_cap up to 2^21, K up to 2^30, n_adapters up to 2^22, not bound by dcut_limits (x . a^T lies in 8 MB of
+ * the context's scratch, a part of the rows at a time where they need more).  Requests that share an adapter share its reads.
  * DEVICE in: x bf16 [T_cap, K] with ldx elements from row to row; a bf16 [n_adapters, n_slices * rank, K] with lda elements from row to row
  *   (adapters follow one another: n_slices * rank * lda); b bf16 [n_adapters, N, rank] dense; scale fp32 [n_adapters] or NULL (1);
- *   adapter int32 [B]; base bf16 [T_cap, N] with ldbase; cu_q int32 [B+1].  x, a, b 16-byte aligned, ldx and lda multiples of 8; base and out of any
- *   stride and alignment (rows and slices that start on 16 bytes are moved in vectors).
+ *   adapter int32 [B]; base bf16 [T_cap, N] with ldbase; cu_q int32 [B+1].  x, a, b 16-byte aligned, ldx and lda multiples of 8, <= 2^32; base and out of any
+ *   stride below 2^32 and any alignment (rows and slices that start on 16 bytes are moved in vectors).
  * DEVICE out: out bf16 with ldo.  It may be base (same stride, not gated): without an activation rows without an adapter are then not touched,
  *   with one they become act(base); nothing else may overlap.  Rows that no request owns are not touched.
  * rank a multiple of 8 (smaller ones: pad with zeros), n_slices * rank <= DCUT_LORA_MAX_RANKS.  An adapter >= n_adapters sets device status 11
