@@ -716,7 +716,7 @@ class Context:
         (m, N, rank), dev, bf16 = b.shape, self.device, torch.bfloat16
         ends = (N,) if slices is None else slices
         K, width, S = x.shape[1], N // 2 if gated else N, len(ends)
-        assert S <= 4 and ends[-1] == N, "at most 4 slices, the last one ending at N"
+        assert 1 <= S <= 4 and ends[-1] == N, "1 to 4 slices, the last one ending at N"
         (am, ar, ak), (a0, a1, a2) = a.shape, a.stride()
         assert am == m and ar == S * rank and ak == K, f"a must be [{m}, {S * rank}, {K}], got {tuple(a.shape)}"
         lda = a1 if ar > 1 else K
