@@ -60,10 +60,10 @@ __device__ __forceinline__ uint32_t e4m3x2(float first, float second) {
 }
 
 // Quotients of neighbours by a scale, two at a time: a product with the scale's reciprocal and its remainder's correction (P. Markstein, 1990).  The product
-// alone, half an ulp of the reciprocal off, put one code in 2500 of bf16 rows beside the one of y / scale; an fp32 division for each element took 15
-// to 48 % longer.  Scales below 2^-80 are lifted, so that the remainder of whatever e4m3 does not round to 0 is exact.  A zero keeps its sign.
+// alone, half an ulp of the reciprocal off, put one code in 1500 to 4300 of bf16 rows beside the one of y / scale; an fp32 division for each element took
+// 15 to 48 % longer than the product.  Scales below 2^-80 are lifted, so that the remainder of whatever e4m3 does not round to 0 is exact.  A zero keeps its sign.
 struct Quotient {
-    uint64_t factor, inv, by;                          // both halves of each: -lift r, -1 / (lift scale), lift scale
+    uint64_t factor, inv, by, plain;                   // both halves of each: -lift r, -1 / (lift scale), lift scale, r
     static __device__ __forceinline__ uint64_t pack(float lo, float hi) {
         uint64_t v;
         asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
@@ -81,7 +81,12 @@ struct Quotient {
     }
     __device__ __forceinline__ Quotient(float r, float scale) {
         const float lift = scale < 0x1p-80f ? 0x1p40f : 1.0f, s = scale * lift, i = -1.0f / s, f = -r * lift;
-        factor = pack(f, f), inv = pack(i, i), by = pack(s, s);
+        factor = pack(f, f), inv = pack(i, i), by = pack(s, s), plain = pack(r, r);
+    }
+    // x r
+    __device__ __forceinline__ void times(float x0, float x1, float& y0, float& y1) const {
+        const uint64_t v = mul(pack(x0, x1), plain);
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(y0), "=f"(y1) : "l"(v));
     }
     // x r / scale
     __device__ __forceinline__ void of(float& x0, float& x1) const {
@@ -173,11 +178,11 @@ struct Stats {
     float sum, top;
 };
 // Over the threads of a row, in a fixed order: a warp's by shuffles, then (ALONE: a row per CTA) the warps'.
-template <bool ALONE>
+template <bool ALONE, bool SUM>
 __device__ __forceinline__ Stats over_row(Stats s, Stats* warps) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        s.sum += __shfl_xor_sync(0xffffffffu, s.sum, o);
+        if (SUM) s.sum += __shfl_xor_sync(0xffffffffu, s.sum, o);
         s.top = larger(s.top, __shfl_xor_sync(0xffffffffu, s.top, o));
     }
     if (!ALONE) return s;
@@ -187,16 +192,19 @@ __device__ __forceinline__ Stats over_row(Stats s, Stats* warps) {
     s = lane < n_warps ? warps[lane] : Stats{0.0f, 0.0f};
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        s.sum += __shfl_xor_sync(0xffffffffu, s.sum, o);
+        if (SUM) s.sum += __shfl_xor_sync(0xffffffffu, s.sum, o);
         s.top = larger(s.top, __shfl_xor_sync(0xffffffffu, s.top, o));
     }
     return s;
 }
 
-// V slots per thread; ALONE: the CTA has one row, otherwise every warp its own; PLAIN: neither residual nor gain (what a row only quantised
-// needs: with their registers fewer CTAs fit an SM, 1088 x 12288 14 us against 11).
-template <int V, Access ACCESS, bool ALONE, bool PLAIN>
+// V slots per thread; ALONE: the CTA has one row, otherwise every warp its own.  kBare: neither residual nor gain (with their registers
+// fewer CTAs fit an SM, 1088 x 12288 14 us against 11); kRows: no norm either, rows that are only quantised
+// (without the sum of squares: 1088 x 12288 10.8 us against 11.4, 8191 x 4096 22.8 against 24.5).
+enum Form { kFull, kBare, kRows };
+template <int V, Access ACCESS, bool ALONE, Form FORM>
 __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
+    constexpr bool PLAIN = FORM != kFull, NORM = FORM != kRows;
     __shared__ Stats warps[3][32];
     dcut_pdl_wait();
     dcut_pdl_launch_dependents();
@@ -230,7 +238,7 @@ __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
         factor(i, g);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            s.sum = fmaf(h[i][j], h[i][j], s.sum);
+            if (NORM) s.sum = fmaf(h[i][j], h[i][j], s.sum);
             s.top = larger(s.top, has_gain ? h[i][j] * g[j] : h[i][j]);
         }
     };
@@ -246,9 +254,9 @@ __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
         if (a.h_out) Place<ACCESS>(i, tid, threads, a.width).store(a.h_out + (size_t)row * a.ldh, h[i]);
         take(i);
     }
-    s = over_row<ALONE>(s, warps[0]);
+    s = over_row<ALONE, NORM>(s, warps[0]);
     float r = 1.0f;
-    if (a.normed) {
+    if (NORM && a.normed) {
         float eps = a.eps;
         auto again = [&](float by, Stats* at) {                        // the statistics of h * by
             s = {0.0f, 0.0f};
@@ -258,7 +266,7 @@ __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
                 for (int j = 0; j < 8; ++j) h[i][j] *= by;
                 take(i);
             }
-            s = over_row<ALONE>(s, at);
+            s = over_row<ALONE, NORM>(s, at);
         };
         const bool far = !(s.sum < INFINITY) || !(fabsf(s.top) < INFINITY);          // (the same answer in every thread of the row)
         if (!(s.sum < INFINITY)) {
@@ -285,7 +293,7 @@ __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
         for (int j = 0; j < 8; ++j) h[i][j] = has_gain ? h[i][j] * g[j] : h[i][j];
         if (a.out) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = h[i][j] * r;
+            for (int j = 0; j < 8; j += 2) over.times(h[i][j], h[i][j + 1], y[j], y[j + 1]);
             at.store(a.out + (size_t)row * a.ldo, y);
         }
         if (a.out8) {
@@ -299,8 +307,9 @@ __global__ void __launch_bounds__(kMaxThreads) rms_norm_kernel(NormArgs a) {
 template <int V, bool ALONE, Access ACCESS>
 cudaError_t launch(const NormArgs& a, int rows_per_cta, int threads, cudaStream_t stream) {
     const dim3 grid((a.T_cap + rows_per_cta - 1) / rows_per_cta), block(threads);
-    return a.residual || a.gain ? dcut_launch_pdl(rms_norm_kernel<V, ACCESS, ALONE, false>, grid, block, 0, stream, a)
-                                : dcut_launch_pdl(rms_norm_kernel<V, ACCESS, ALONE, true>, grid, block, 0, stream, a);
+    return a.residual || a.gain ? dcut_launch_pdl(rms_norm_kernel<V, ACCESS, ALONE, kFull>, grid, block, 0, stream, a)
+           : a.normed           ? dcut_launch_pdl(rms_norm_kernel<V, ACCESS, ALONE, kBare>, grid, block, 0, stream, a)
+                                : dcut_launch_pdl(rms_norm_kernel<V, ACCESS, ALONE, kRows>, grid, block, 0, stream, a);
 }
 template <int V, bool ALONE>
 cudaError_t launch(const NormArgs& a, Access access, int rows_per_cta, int threads, cudaStream_t stream) {
