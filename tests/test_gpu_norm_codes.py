@@ -58,3 +58,25 @@ def test_normed_rows(width):
     out8, scale8 = binding.rows8(T, width), torch.empty(T, device="cuda")
     context().rms_norm(x, None, T, gain=gain, rms_eps=3.0, out8=out8, scale8=scale8)
     same(out8, scale8, x.float() * gain.float() * 0.5)
+
+
+def test_zeros_keep_their_sign():
+    x = torch.tensor([0.0, -0.0, 1.0, -1.0] * 70, device="cuda").to(BF16).view(1, -1).expand(3, -1).contiguous()
+    x[1] *= 2.0 ** -120
+    x[2].mul_(0)                                                         # only zeros, of both signs
+    out8, scale8 = context().quantize(x, None, 3)
+    same(out8, scale8, x.float())
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_many_sums(seed):
+    """33 million fp32 values of rows of all sizes, against fp32 division by the stored scales."""
+    g = torch.Generator("cuda").manual_seed(seed)
+    T, width = 4096, 8192
+    size = 2.0 ** torch.randint(-90, 90, (T, 1), generator=g, device="cuda").float()
+    x, r = ((size * torch.randn((T, width), generator=g, device="cuda") * f).to(BF16) for f in (1.0, 2.0 ** -seed))
+    out8, scale8 = context().quantize(x, None, T, residual=r)
+    y = x.float() + r.float()
+    assert torch.equal(scale8.cpu(), y.abs().amax(1).cpu() / 448)
+    want = (y / scale8[:, None]).clamp(-448, 448).to(F8).view(torch.uint8)
+    assert torch.equal(out8.contiguous().view(torch.uint8), want)
