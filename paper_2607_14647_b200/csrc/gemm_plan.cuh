@@ -27,6 +27,9 @@ constexpr int kSplitCost = 50;             // what the exchange of partial sums 
 // its epilogue and the start, which pairs and split K make dearer.  One SM against the plan's choice with them, us, no
 // activation: K = 64, 8 x 6147 6.0 / 8.1, 333 x 6147 9.1 / 12.3; K = 384, 333 x 2048 6.0 / 7.0, 8 x 2048 5.6 / 5.2; K = 640,
 // 8 x 2048 6.5 / 5.7, 700 x 6147 18.2 / 19.0.
+// e4m3 operands have twice the elements in as many k-blocks, so the rule holds up to K = 1024 there.  The same comparison, geometric mean over 25 shapes
+// of 8 to 1088 rows and 1024 to 12288 columns: pairs take 1.20 of the time of one SM per tile at K = 256 (gated 1.14), 1.14 at 512 (1.14), 1.11 at 768
+// (1.13), 1.08 at 1024 (1.12); at K = 1024 8 x 2048 6.1 / 5.7, 64 x 1024 6.0 / 5.7 (the most that the rule loses), 333 x 6144 8.3 / 10.9, 1088 x 2048 8.4 / 10.8.
 constexpr int kShortK = 512;
 constexpr int kPlanPair = 8, kPlanSplit = 16;
 

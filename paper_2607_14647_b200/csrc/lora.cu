@@ -404,8 +404,9 @@ __global__ void __launch_bounds__(kThreads, 2) lora_low_kernel(LoraArgs g, const
 // FEW: tiles of 16 rows, one block of them: a body without what the others need.  CTAs per SM (registers): of long tiles 2 with two steps in
 // registers, else 3 (4 took 87 us where 3 take 75 for 8191 tokens).  Tiles of 16 rows have more to wait for and less to do: 4 against 3, 16 tokens with
 // an adapter each, gated, 4096 -> 2 x 12288, rank 16 18.7 us against 20.2, 64 tokens of rank 96 93 against 104; two steps in registers 3 against 2, 64
-// tokens of rank 64, 4096 -> 12288 37 against 42 (4: 46; gated 64 tokens 78 either way, 4: 84); B read again, no gate: 3, 4 spills
-// (16 tokens of rank 128, 4096 -> 6144 21 against 18).
+// tokens of rank 64, 4096 -> 12288 37 against 42 (4: 46; gated 64 tokens 78 either way, 4: 84); B read again, no gate: 3, for at 4 it spills too much
+// (16 tokens of rank 128, 4096 -> 6144 21 against 18).  These limits cost spills in every form but the one with two steps of long tiles: of long tiles with one
+// step 44 bytes (gated 56), with B read again 152 (68), of tiles of 16 rows 8 to 16 (gated 24 to 88).
 constexpr int out_ctas(bool gated, int keep, bool few) { return few ? (keep == 2 || (keep == 0 && !gated) ? 3 : 4) : keep == 2 ? 2 : 3; }
 // STAGED: the kept B comes by way of shared memory (a lane's own pieces: nobody else looks at them).  For two steps of long tiles, of ranks that are
 // multiples of 32: gated 1088 tokens of rank 64 63.1 us -> 57.9, 2800 tokens 4096 -> 2 x 4096 57.4 -> 53.7 (600 tokens 54.2 -> 54.7), both kernels
@@ -723,5 +724,11 @@ dcut_status dcut_launch_lora(dcut_ctx* ctx, const dcut_lora_args* l, const int* 
                                                                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                                                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return dcut_fail(ctx, DCUT_ECUDA, "cuTensorMapEncodeTiled failed for the adapters (%d)", (int)r);
+    // Rows of a tile.  The packed lengths are on the device: the mean is that of T_cap.  us on the device with 16 / 32 / 64 rows, requests with an adapter each, K = 4096:
+    //                       64 of 16     64 of 17        24 of 40        16 of 64        16 of 65        8 of 136
+    //   rank 16, 3 slices   26 / 27 / 28 34 / 31 / 32    24 / 23 / 21    23 / 19 / 19    27 / 23 / 25    23 / 22 / 21
+    //   rank 64, gated     100 / 103 / 100 140 / 117 / 116 88 / 77 / 65  81 / 65 / 59    95 / 78 / 71    86 / 69 / 60
+    //   rank 128            40 / 45 / 54 52 / 56 / 65    34 / 37 / 36    32 / 34 / 34    36 / 36 / 45    32 / 35 / 37
+    // So 64 rows would do from some 33 on at ranks up to 64, and 16 rows are best for rank 128 up to 300 (3 of 2730: 165 / 139 / 133); the rule does not go by the rank.
     return launch(ctx, g, a_map, mean <= 16 ? 16 : mean <= 64 ? 32 : 64, units, stream);
 }

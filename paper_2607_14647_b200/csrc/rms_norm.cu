@@ -7,9 +7,8 @@
 // A row stays in registers.  max|y| = r * max|h * gain| (rounding is monotone, r > 0), so the sum of squares and the maximum
 // leave through one reduction and the row is finished behind a single barrier.  Sum and statistics are fp32, h is normalised
 // before it is rounded to bf16; each output is rounded once.
-// 8191 rows of 4096 with a residual and both outputs (302 MB) 52 us, 5.8 TB/s of reads and writes; 16 rows 2.6 us.  A thread has 1 to 8 pieces of 16 bytes, by
-// the width: more of them mean fewer threads per row and more rows per SM (12288 wide: 2 pieces 19 us, 4 pieces 14), fewer a shorter
-// chain for a single row.
+// 8191 rows of 4096 with a residual and both outputs (302 MB) 53 us, 5.6 TB/s of reads and writes; 16 rows 2.6 us.  A thread has 1 to 8 pieces of 16 bytes, by
+// the width: more of them mean fewer threads per row and more rows per SM, fewer a shorter chain for a single row.
 // A sum of squares that overflows (|h| above about 10^18) is formed again from h * 2^-80.  Where it does, or h * gain does, h is normalised ahead of
 // the gain (2^-80 would make the squares of ordinary values vanish).  The maximum keeps a NaN.
 #include <cuda_bf16.h>
@@ -96,7 +95,7 @@ struct Quotient {
 };
 
 // How rows are read and written.  kVector: a slot of a thread is 8 neighbouring elements, a vector (the row's last one may be partly used).
-// kShifted: the same, but bf16 outputs begin anywhere (rows of an odd width one after the other, say; 7698 x 2789 50 us against 69 without it; the code
+// kShifted: the same, but bf16 outputs begin anywhere (rows of an odd width one after the other, say; 7698 x 2789 54 us, 69 with 2-byte stores; the code
 // for it slows aligned rows down, so it is a form of its own).  kSingle: inputs begin anywhere too; element j of a slot is `threads` elements after
 // element j - 1, so that a warp's 2-byte accesses are neighbours.
 enum Access { kVector, kShifted, kSingle };
@@ -338,6 +337,15 @@ dcut_status dcut_launch_rms_norm(dcut_ctx* ctx, const dcut_norm_args* n, const i
                       !((reinterpret_cast<uintptr_t>(a.out8) | (uintptr_t)(a.out8 ? a.ld8 : 0)) & 7);
     const Access access = !in16 ? kSingle : rows16(a.h_out, a.ldh) && rows16(a.out, a.ldo) ? kVector : kShifted;
     const int slots = (a.width + 7) / 8;
+    // Pieces of a thread, us on the device with 1 / 2 / 4 / 8 of them (norm with every output, and quantising):
+    //                 16 rows                   quantising               8191 rows                  quantising
+    //   2048 wide     2.2 / 2.5 / 3.4           1.7 / 1.8 / 2.2          28.5 / 26.4 / 27.0         14.9 / 11.9 / 11.3
+    //   4096          2.4 / 2.7 / 3.4 / 5.6     1.9 / 1.9 / 2.2 / 3.1    55.0 / 52.8 / 49.9 / 55.3  29.5 / 22.4 / 19.6 / 22.0
+    //   6144          - / 2.9 / 3.6 / 5.5       - / 2.0 / 2.3 / 3.1      - / 75.2 / 72.9 / 81.7     - / 33.2 / 28.9 / 33.1
+    //   8192          - / 3.0 / 3.7 / 5.5       - / 2.0 / 2.3 / 3.2      - / 105 / 96.3 / 102       - / 44.7 / 39.8 / 40.7
+    //   12288         - / - / 4.0 / 5.5         - / - / 2.5 / 3.2        - / - / 143 / 172          - / - / 57.0 / 65.3
+    // (none: more than 512 threads).  Few rows want few pieces and many rows more of them; the rule goes by the width and lies between
+    // (of the rows it could know T_cap alone, not the packed length).  Above 16384 only 8 pieces hold a row.
     const int per = slots <= 256 ? 1 : slots <= 768 ? 2 : slots <= 2048 ? 4 : 8;
     const int threads = ((slots + per - 1) / per + 31) & ~31;
     cudaError_t e = threads == 32 ? launch<1, false>(a, access, 4, 128, stream)
